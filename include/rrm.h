@@ -61,7 +61,8 @@ typedef enum {
     RRM_ERR_STATE = -6,  /* call not valid in the handle's current state */
     RRM_ERR_RANGE = -7,  /* an int8 difference did not fit int8 (sticky, see rrm_get_stats) */
     RRM_ERR_OPTION = -8, /* unknown option key or value */
-    RRM_ERR_ALIGN = -9   /* a device pointer is not 16-byte aligned */
+    RRM_ERR_ALIGN = -9,  /* a device pointer is not aligned (16 bytes, where a call does not say otherwise) */
+    RRM_ERR_WORKSPACE = -10 /* the caller's workspace is smaller than the call needs */
 } rrm_status;
 
 typedef enum { RRM_CONV = 0, RRM_FC = 1 } rrm_kind;
@@ -275,6 +276,105 @@ rrm_status rrm_aux_relu_requant_pool_changed_i8(rrm_layer* layer, void* out, int
  * Errors: RRM_ERR_NULL, RRM_ERR_DTYPE, RRM_ERR_SHAPE (counts out of range), RRM_ERR_ALIGN, RRM_ERR_HIP. */
 rrm_status rrm_aux_probe_mfma(int dtype, void* sink, int iters, int workgroups, void* hip_stream);
 rrm_status rrm_aux_probe_copy(void* dst, const void* src, size_t bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators between and behind the linear layers of a video network (not part of the paper's method): the map f of a
+ * bf16 layer that ends in a group norm, a gated recurrence over the frames' features, and a gated feed-forward block on
+ * them, each with its backward pass.  They keep no handle and no state of their own: every pointer is a DEVICE pointer
+ * that the caller owns, borrowed until the work enqueued on hip_stream has run, and aligned to its element.  Scratch
+ * is the caller's `workspace` (256-byte aligned, at least as large as the *_workspace function says, contents
+ * irrelevant before and after; NULL where that is 0); calls that overlap in time need one each.  Nothing
+ * synchronises, allocates or depends on the host, so all of it can be captured into a HIP graph.  Inputs and outputs of
+ * one call must not overlap unless a call says otherwise.  A tensor without elements may be NULL.
+ *
+ * Strides count elements; the innermost axis (channels) is adjacent, the two outer ones lie as the strides say (no two
+ * elements of an output at one place).  Strides of tensors that a call does not take are not looked at.
+ *
+ * Sums, statistics, states and gates are held in 32 bits whatever the element type; a result is rounded once, to
+ * nearest even.  No atomics: the same call gives the same bits.
+ *
+ * Errors of all of them: RRM_ERR_NULL, RRM_ERR_SHAPE (sizes, strides), RRM_ERR_DTYPE (element types), RRM_ERR_OPTION
+ * (activation, eps), RRM_ERR_STATE (h_last given as h0), RRM_ERR_ALIGN, RRM_ERR_WORKSPACE (too small), RRM_ERR_HIP. */
+typedef enum { RRM_F32 = 0, RRM_BF16 = 1 } rrm_elem;
+
+/* act(z): z; max(z, 0); z * sigmoid(z); z * Phi(z) with the normal distribution function Phi (erf form) */
+typedef enum { RRM_ACT_NONE = 0, RRM_ACT_RELU = 1, RRM_ACT_SILU = 2, RRM_ACT_GELU = 3 } rrm_act;
+
+/* Group norm with an activation, channels last: over a sample's positions and the c / groups channels of a group
+ *      mean, var = the mean and the (biased) variance      r = 1 / sqrt(var + eps)
+ *      y = act(gamma_c * (x - mean) * r + beta_c)
+ * x may be a convolution's stored projection (rrm_snapshot), y the next layer's input. */
+typedef struct {
+    int n, positions, c, groups; /* groups divides c; n or positions may be 0 */
+    int x_elem, y_elem, act;     /* rrm_elem of x and dx, of y and dy; rrm_act */
+    float eps;                   /* > 0 */
+    int64_t x_sample, x_position, y_sample, y_position, dx_sample, dx_position; /* strides; dy lies by those of y */
+} rrm_norm_desc;
+
+size_t rrm_group_norm_workspace(const rrm_norm_desc* desc, int backward);
+
+/* gamma, beta  float32 [c]; NULL = 1, 0
+ * stats        float32 [n][groups][2] or NULL: receives mean and r, which the backward pass reads */
+rrm_status rrm_group_norm_act(const rrm_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                              float* stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* With dz = dy * act'(z), xh = (x - mean) * r and the means over a group's values (ReLU: act'(0) = 0):
+ *      dgamma_c = sum dz * xh       dbeta_c = sum dz       dx = r * (gamma dz - mean(gamma dz) - xh * mean(gamma dz xh))
+ * dx, dgamma, dbeta (float32 [c]) may each be NULL. */
+rrm_status rrm_group_norm_act_backward(const rrm_norm_desc* desc, const void* x, const float* stats, const float* gamma,
+                                       const float* beta, const void* dy, void* dx, float* dgamma, float* dbeta,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gated linear recurrence over the t frames of n videos, each of the c features by itself:
+ *      a_t = sigmoid(f_t)        h_t = a_t * h_{t-1} + (1 - a_t) * x_t        y_t = h_t
+ * A video of lengths[i] < t frames ends there: what x, f and dy hold behind is not looked at (not-a-numbers included),
+ * y, dx and df are 0 there, and h_last is the state after its last frame (h0 for a video of no frames).
+ * One frame of live videos is t = 1, with h0 the state before and h_last the state after it; there h_last may be h0. */
+typedef struct {
+    int n, t, c; /* each may be 0 */
+    int elem;    /* rrm_elem of x, f, y and their gradients */
+    int64_t x_video, x_frame, f_video, f_frame, y_video, y_frame; /* strides; dy lies by those of y */
+    int64_t dx_video, dx_frame, df_video, df_frame;
+} rrm_scan_desc;
+
+/* frames between two states that a forward pass of training keeps in `marks`, float32 [n][rrm_scan_marks(t)][c] */
+#define RRM_SCAN_MARK_FRAMES 64
+int rrm_scan_marks(int t); /* ceil(t / RRM_SCAN_MARK_FRAMES) */
+size_t rrm_gated_scan_workspace(const rrm_scan_desc* desc, int backward);
+
+/* h0       float32 [n][c], NULL = 0           lengths  int32 [n], NULL = t each (held to [0, t])
+ * h_last   float32 [n][c] or NULL             marks    see above, or NULL: the state before every 64th frame */
+rrm_status rrm_gated_scan(const rrm_scan_desc* desc, const void* x, const void* f, const float* h0, const int32_t* lengths,
+                          void* y, float* h_last, float* marks, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* With g_t = dy_t + a_{t+1} g_{t+1}, from g = dy + dh_last at a video's last frame:
+ *      dx_t = (1 - a_t) g_t        df_t = g_t (h_{t-1} - x_t) a_t (1 - a_t)        dh0 = a_1 g_1 (no frames: dh_last)
+ * marks    as the forward pass on the same x, f, h0 and lengths left it (h is recomputed from it, not read back)
+ * dh_last  float32 [n][c] or NULL (= 0)        dh0  float32 [n][c] or NULL */
+rrm_status rrm_gated_scan_backward(const rrm_scan_desc* desc, const void* x, const void* f, const float* marks,
+                                   const int32_t* lengths, const void* dy, const float* dh_last, void* dx, void* df,
+                                   float* dh0, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gated feed-forward block on m rows of k features, bfloat16 throughout:
+ *      G = X Wg^T        U = X Wu^T        H = act(G) * U            X [m][k], Wg and Wu [f][k], H, G, U [m][f]
+ * both projections, the activation and the product in one pass; the weights lie as an FC layer's do. */
+typedef struct {
+    int m, k, f; /* m may be 0 */
+    int act;     /* rrm_act */
+    int64_t x_row, wg_row, wu_row, h_row, gu_row, dx_row, dwg_row, dwu_row; /* strides; dh lies by h_row */
+} rrm_ff_desc;
+
+size_t rrm_gated_ff_workspace(const rrm_ff_desc* desc, int backward);
+
+/* g, u: both or neither; for a backward pass they receive G and U, rounded to bfloat16 */
+rrm_status rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*      dG = dH * U * act'(G)     dU = dH * act(G)     dX = dG Wg + dU Wu     dWg = dG^T X     dWu = dU^T X
+ * dG and dU enter the products in bfloat16.  dx, or dwg and dwu together, may be NULL. */
+rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const void* g,
+                                 const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -8,3 +8,6 @@ it raises.
 from .binding import (  # noqa: F401
     BF16, BIN, CONV, FC, I8, Layer, RRMError, Shape, StackEntry, Stats, lib, lib_path, probe_copy, probe_mfma, relu_requant_pool_i8, stack_step,
 )
+from .operators import (  # noqa: F401
+    gated_ff, gated_ff_backward, gated_scan, gated_scan_backward, gated_scan_marks, group_norm_act, group_norm_act_backward,
+)

@@ -97,6 +97,19 @@ def lib():
                   "rrm_get_stats", "rrm_get_kernel_times", "rrm_aux_relu_requant_pool_i8",
                   "rrm_aux_relu_requant_pool_changed_i8", "rrm_set_threshold", "rrm_step_from_projection", "rrm_stack_step"):
             getattr(L, f).restype = I
+        S, B = ctypes.c_size_t, ctypes.c_void_p  # (B: a descriptor by reference)
+        L.rrm_group_norm_workspace.argtypes = L.rrm_gated_scan_workspace.argtypes = L.rrm_gated_ff_workspace.argtypes = [B, I]
+        L.rrm_group_norm_workspace.restype = L.rrm_gated_scan_workspace.restype = L.rrm_gated_ff_workspace.restype = S
+        L.rrm_group_norm_act.argtypes = [B, P, P, P, P, P, P, S, P]
+        L.rrm_group_norm_act_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_gated_scan.argtypes = [B, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_gated_scan_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_gated_ff.argtypes = [B, P, P, P, P, P, P, P, S, P]
+        L.rrm_gated_ff_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_scan_marks.argtypes = [I]
+        for f in ("rrm_group_norm_act", "rrm_group_norm_act_backward", "rrm_gated_scan", "rrm_gated_scan_backward", "rrm_gated_ff",
+                  "rrm_gated_ff_backward", "rrm_scan_marks"):
+            getattr(L, f).restype = I
         _lib = L
     return _lib
 

@@ -40,6 +40,18 @@ size_t round16(size_t b) { return (b + 15) & ~size_t(15); }
 
 }  // namespace
 
+namespace rrm {
+
+rrm_status record_failure(rrm_status st, const char* msg) noexcept {
+    try {
+        g_last_error = msg;
+    } catch (...) {  // (no memory for the text: the status still says what failed)
+    }
+    return st;
+}
+
+}  // namespace rrm
+
 struct rrm_layer {
     rrm_shape shape{};
     int dtype = 0;
@@ -1293,6 +1305,7 @@ const char* rrm_status_string(int status) {
         case RRM_ERR_RANGE: return "int8 difference out of range";
         case RRM_ERR_OPTION: return "unknown option";
         case RRM_ERR_ALIGN: return "misaligned pointer";
+        case RRM_ERR_WORKSPACE: return "workspace too small";
         default: return "unknown status";
     }
 }
