@@ -63,6 +63,8 @@ rrm_status check(const rrm_ff_desc* d) {
     if (!d) return record_failure(RRM_ERR_NULL, "desc is NULL");
     if (d->m < 0 || d->k < 1 || d->f < 1) return record_failure(RRM_ERR_SHAPE, "feed-forward: m not negative, k and f positive");
     if (d->m > (1 << 27) || d->k > (1 << 24) || d->f > (1 << 24)) return record_failure(RRM_ERR_SHAPE, "feed-forward: m up to 2^27, k and f up to 2^24");
+    if ((int64_t)d->m * d->k > (1ll << 40) || (int64_t)d->m * d->f > (1ll << 40) || (int64_t)d->f * d->k > (1ll << 40))
+        return record_failure(RRM_ERR_SHAPE, "feed-forward: tensors of up to 2^40 elements");
     return check_act(d->act);
 }
 
