@@ -362,6 +362,8 @@ typedef struct {
     int m, k, f; /* m may be 0 */
     int act;     /* rrm_act */
     int64_t x_row, wg_row, wu_row, h_row, gu_row, dx_row, dwg_row, dwu_row; /* strides; dh lies by h_row */
+    int unaligned; /* 0: x, wg and wu begin at whole 16 bytes; 1: at whole elements (the workspace then holds copies of
+                      them, as it does where k or a row is not a multiple of 8 elements) */
 } rrm_ff_desc;
 
 size_t rrm_gated_ff_workspace(const rrm_ff_desc* desc, int backward);

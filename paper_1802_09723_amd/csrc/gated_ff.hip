@@ -33,8 +33,7 @@ struct Product {
     int splits;             // parts of the summed axis, one workgroup each; more than one: sums to `part`
     __bf16 *out, *out2, *out3;  // gated: H, G, U (G and U may be nullptr); halves: out2 belongs to p[1]
     int64_t out_row, out2_row;
-    float* part;            // [splits][rows][cols]
-    int vec_out;            // results may be stored 16 bytes at a time
+    float* part;            // [splits][rows][cols, to whole fours] (gated: [splits][2][rows][..])
 };
 
 enum Kind : int { GATED = 0, PLAIN = 1, HALVES = 2 };
@@ -45,32 +44,40 @@ __device__ __forceinline__ int window_turn(int k) {
     return WINDOWS >= 8 ? (k & 3) | ((k >> 1) & 4) : WINDOWS == 4 ? (k & 3) : WINDOWS == 2 ? ((k >> 1) & 1) : 0;
 }
 
-// eight elements of a row of `len`, from element k on, at any alignment; zeros behind the end
+// Until at most N of this wavefront's copies to LDS are on their way (they end in the order of their start), and its LDS accesses are done
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    static_assert(N < 64);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+// no waits of its own: those are the callers'
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Eight elements at the alignment of one.
+struct __attribute__((packed, aligned(2))) Loose {
+    u32x4 v;
+};
+__device__ __forceinline__ u32x4 loose_chunk(src_t p) { return reinterpret_cast<const Loose*>(p)->v; }
+// eight elements of a row of `len`, from element k on; zeros behind the end
 __device__ __forceinline__ u32x4 ragged_chunk(src_t row, int k, int len) {
-    struct __attribute__((packed, aligned(2))) loose {
-        u32x4 v;
-    };
-    u32x4 w = {0, 0, 0, 0};
-    if (k + 8 <= len) {
-        w = reinterpret_cast<const loose*>(row + k)->v;
-    } else if (k < len) {
-        unsigned short e[8];
+    if (k + 8 <= len) return loose_chunk(row + k);
+    unsigned short e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = k + i < len ? __builtin_bit_cast(unsigned short, row[k + i]) : (unsigned short)0;
+    for (int i = 0; i < 8; ++i) e[i] = k + i < len ? __builtin_bit_cast(unsigned short, row[k + i]) : (unsigned short)0;
+    u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (unsigned int)e[2 * i] | ((unsigned int)e[2 * i + 1] << 16);
-    }
+    for (int i = 0; i < 4; ++i) w[i] = (unsigned int)e[2 * i] | ((unsigned int)e[2 * i + 1] << 16);
     return w;
 }
 
 // Tile product on the matrix cores.  (comment to come)
-template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, bool RAGGED>
-__global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(Product a) {
+template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_kernel(Product a) {
     constexpr int THREADS = WM * WN * 64, BM = MT * 32 * WM, BN = NT * 32 * WN;
     constexpr int PB = BM * STEP * 2, QB = BN * STEP * 2;                       // bytes of a staged tile
     constexpr int NP = PB / (THREADS * 16), NQ = QB / (THREADS * 16);          // 16-byte chunks a thread stages
     constexpr int OUT_COLS = KIND == GATED ? BN / 2 : BN;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * (PB + QB)];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[STAGES * (PB + QB)];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int wm = wave % WM, wn = wave / WM;
 
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
             pr[i] = m0 + (((c >> 2) ^ window_turn<PW>(k)) * 4 + (c & 3)) * 8;
         } else {
             const int r = at / 128;
-            pk[i] = (((at % 128) / 16) ^ (r & 7)) * 8;
+            pk[i] = (((at % 128) / 16) ^ ((r >> 1) & 7)) * 8;
             pr[i] = m0 + r;
         }
     }
@@ -127,7 +134,7 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
             qr[i] = n0 + (((c >> 2) ^ window_turn<QW>(k)) * 4 + (c & 3)) * 8;
         } else {
             const int r = at / 128;
-            qk[i] = (((at % 128) / 16) ^ (r & 7)) * 8;
+            qk[i] = (((at % 128) / 16) ^ ((r >> 1) & 7)) * 8;
             qr[i] = row_of_q(r);
         }
     }
@@ -154,31 +161,17 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
         }
     };
     const src_t zeros = reinterpret_cast<src_t>(&g_zeros);
-    u32x4 pv[RAGGED ? NP : 1], qv[RAGGED ? NQ : 1];
-    auto stage = [&](int s, int buf) {  // starts the copies of step s
+    auto stage = [&](int s, int buf) __attribute__((always_inline)) {  // starts the copies of step s
         const int pair = KIND == PLAIN && s >= steps_of ? 1 : 0;
         const int rem = a.len - (s - pair * steps_of) * STEP;
         unsigned char* dp = lds + buf * (PB + QB);
         unsigned char* dq = dp + PB;
-        if (RAGGED) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i)
-                pv[i] = PT ? (pk[i] < rem ? ragged_chunk(pp[i], 0, a.rows - (pr[i] < p_last ? pr[i] : p_last)) : u32x4{0, 0, 0, 0})
-                           : ragged_chunk(pp[i] - pk[i], pk[i], rem);
+        for (int i = 0; i < NP; ++i)
+            __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || pk[i] < rem ? pp[i] : zeros), (lptr_t)(dp + (i * THREADS + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                qv[i] = QT ? (qk[i] < rem ? ragged_chunk(qp[i], 0, a.cols - (qr[i] < q_last ? qr[i] : q_last)) : u32x4{0, 0, 0, 0})
-                           : ragged_chunk(qp[i] - qk[i], qk[i], rem);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-                __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || pk[i] < rem ? pp[i] : zeros),
-                                                 (lptr_t)(dp + (i * THREADS + wave * 64) * 16), 16, 0, 0);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || qk[i] < rem ? qp[i] : zeros),
-                                                 (lptr_t)(dq + (i * THREADS + wave * 64) * 16), 16, 0, 0);
-        }
+        for (int i = 0; i < NQ; ++i)
+            __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || qk[i] < rem ? qp[i] : zeros), (lptr_t)(dq + (i * THREADS + wave * 64) * 16), 16, 0, 0);
         if (KIND == PLAIN && s + 1 == steps_of && s + 1 < s1) {
             point(s + 1);
         } else {
@@ -186,15 +179,6 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
             for (int i = 0; i < NP; ++i) pp[i] += p_step;
 #pragma unroll
             for (int i = 0; i < NQ; ++i) qp[i] += q_step;
-        }
-    };
-    auto land = [&](int buf) {  // ragged: what stage() has fetched goes to LDS
-        if (RAGGED) {
-            unsigned char* dp = lds + buf * (PB + QB);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) *reinterpret_cast<u32x4*>(dp + (i * THREADS + tid) * 16) = pv[i];
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) *reinterpret_cast<u32x4*>(dp + PB + (i * THREADS + tid) * 16) = qv[i];
         }
     };
 
@@ -207,7 +191,7 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
     // Fragment reads: lane l holds row l % 32 and eight of the summed axis, (l / 32) * 8 on in a step of 16
-    const int flat = (lane & 31) * 128 + (((lane >> 5) ^ (lane & 7)) << 4);
+    const int flat = (lane & 31) * 128 + (((lane >> 5) ^ ((lane >> 1) & 7)) << 4);
     const int turn = ((lane >> 2) & 3) | ((lane >> 5) << 2), tk = (lane >> 5) * 8 + ((lane >> 2) & 3), tin = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     auto frag = [&](const unsigned char* tile, int r0, int ks, auto turned, auto rows) -> v8bf {
         constexpr int ROWS = decltype(rows)::value;
@@ -231,57 +215,95 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
     const auto p_rows = std::integral_constant<int, BM>{};
     const auto q_rows = std::integral_constant<int, BN>{};
 
+    // Fragments of 16 of the summed axis are read while those before are multiplied, across steps as well: the barrier that publishes
+    // the next step stands before the last products of this one.
+    v8bf fp[2][MT], fq[2][NT];
+    auto fragments = [&](int set, int place, int ks) __attribute__((always_inline)) {
+        const unsigned char* tp = lds + place * (PB + QB);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fq[set][j] = frag(tp + PB, (wn * NT + j) * 32, ks, q_turned, q_rows);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fp[set][i] = frag(tp, (wm * MT + i) * 32, ks, p_turned, p_rows);
+    };
+    auto products = [&](int set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[set][j], fp[set][i], acc[i][j], 0, 0, 0);
+        // one product, one read, ..
+        constexpr int READS = MT * (PT ? 2 : 1) + NT * (QT ? 2 : 1), ALL = MT * NT, EACH = (2 * READS + ALL - 1) / ALL;
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        }
+    };
     if (s0 < s1) {
         point(s0);
-        stage(s0, 0);
-        land(0);
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i)
+            if (s0 + i < s1) stage(s0 + i, i);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        fragments(0, 0, 0);
     }
-    for (int s = s0; s < s1; ++s) {
-        const int buf = (s - s0) & 1;
-        __builtin_amdgcn_s_waitcnt(0);  // this wavefront's copies have landed
-        __syncthreads();                // everybody's have; and everybody is done with the other buffer
-        if (s + 1 < s1) stage(s + 1, buf ^ 1);
-        const unsigned char* tp = lds + buf * (PB + QB);
-        const unsigned char* tq = tp + PB;
-#pragma unroll
-        for (int ks = 0; ks < STEP / 16; ++ks) {
-            v8bf fp[MT], fq[NT];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) fq[j] = frag(tq, (wn * NT + j) * 32, ks, q_turned, q_rows);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fp[i] = frag(tp, (wm * MT + i) * 32, ks, p_turned, p_rows);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[j], fp[i], acc[i][j], 0, 0, 0);
+    int buf = 0;  // place of the step at hand
+    auto first_three = [&]() __attribute__((always_inline)) {
+        fragments(1, buf, 1);
+        products(0);
+        fragments(0, buf, 2);
+        products(1);
+        fragments(1, buf, 3);
+        products(0);
+    };
+    for (int s = s0; s + 1 < s1; ++s) {
+        const int after = buf + 1 == STAGES ? 0 : buf + 1;
+        first_three();
+        // this wavefront's copies of the next step have landed (those of later steps may still be on their way), and its reads
+        // of this one are done ..
+        if (STAGES > 2 && s + STAGES <= s1) {
+            wait_copies<(STAGES - 2) * (NP + NQ)>();
+        } else {
+            wait_copies<0>();
         }
-        if (s + 1 < s1) land(buf ^ 1);
+        barrier();  // .. and so are everybody's
+        if (s + STAGES < s1) stage(s + STAGES, buf);
+        fragments(0, after, 0);
+        products(1);
+        buf = after;
+    }
+    if (s0 < s1) {
+        first_three();
+        products(1);
     }
 
     // acc[i][j][4 q + e] of lane l: row (wm MT + i) 32 + l % 32, column (wn NT + j) 32 + 8 q + 4 (l / 32) + e
     const int lr = lane & 31, lc = (lane >> 5) * 4;
-    if (KIND == PLAIN && a.splits > 1) {
-        float* part = a.part + (int64_t)split * a.rows * a.cols;
+    if (KIND != HALVES && a.splits > 1) {
+        constexpr int WAYS = KIND == GATED ? 2 : 1;
+        const int pitch = (a.cols + 3) & ~3;
+        const int64_t plane = (int64_t)a.rows * pitch;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int r = m0 + (wm * MT + i) * 32 + lr;
+            if (r >= a.rows) continue;
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+            for (int j = 0; j < NT; ++j) {
+                float* to = a.part + (int64_t)(split * WAYS + j % WAYS) * plane + r * (int64_t)pitch;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int c = n0 + (wn * NT + j) * 32 + 8 * q + lc;
-                    if (r >= a.rows) continue;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < a.cols) part[(int64_t)r * a.cols + c + e] = acc[i][j][4 * q + e];
+                    const int c = n0 + (wn * NT + j) / WAYS * 32 + 8 * q + lc;
+                    if (c < pitch)
+                        *reinterpret_cast<float4*>(to + c) = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
                 }
+            }
         }
         return;
     }
     // Results go through LDS, 32 rows of a wavefront at a time, so that they leave 16 bytes a lane in whole runs.
     __syncthreads();
-    constexpr int RUN = KIND == GATED ? 32 : NT * 32, PITCH = RUN * 2 + 16;  // columns of a row; bytes between rows
-    static_assert(WM * WN * 32 * PITCH <= 2 * (PB + QB), "the results' staging fits the tiles' place");
+    constexpr int RUN = (KIND == GATED ? NT / 2 : NT) * 32, PITCH = RUN * 2 + 16;  // columns of a row; bytes between rows
+    static_assert(WM * WN * 32 * PITCH <= STAGES * (PB + QB), "the results' staging fits the tiles' place");
     unsigned char* mine = lds + wave * 32 * PITCH;
     const int c0 = n0 + wn * RUN;
     auto leave = [&](int i, __bf16* out, int64_t row, auto value) {  // value(j, e): result e of block j
@@ -303,8 +325,8 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
             const int gr = m0 + (wm * MT + i) * 32 + r, gc = c0 + c;
             if (gr >= a.rows) continue;
             __bf16* to = out + gr * row + gc;
-            if (a.vec_out && gc + 8 <= a.cols) {
-                *reinterpret_cast<u32x4*>(to) = w;
+            if (gc + 8 <= a.cols) {
+                reinterpret_cast<Loose*>(to)->v = w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -316,11 +338,11 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         if constexpr (KIND == GATED) {
-            static_assert(KIND != GATED || NT == 2, "a wavefront holds both projections of its columns");
-            leave(i, a.out, a.out_row, [&](int, int e) { return act_value<ACT>(acc[i][0][e]) * acc[i][NT - 1][e]; });
+            static_assert(KIND != GATED || NT % 2 == 0, "a wavefront holds both projections of its columns");
+            leave(i, a.out, a.out_row, [&](int j, int e) { return act_value<ACT>(acc[i][2 * j][e]) * acc[i][2 * j + 1][e]; });
             if (a.out2) {
-                leave(i, a.out2, a.out2_row, [&](int, int e) { return acc[i][0][e]; });
-                leave(i, a.out3, a.out2_row, [&](int, int e) { return acc[i][NT - 1][e]; });
+                leave(i, a.out2, a.out2_row, [&](int j, int e) { return acc[i][2 * j][e]; });
+                leave(i, a.out3, a.out2_row, [&](int j, int e) { return acc[i][2 * j + 1][e]; });
             }
         } else {
             leave(i, half ? a.out2 : a.out, half ? a.out2_row : a.out_row, [&](int j, int e) { return acc[i][j][e]; });
@@ -328,14 +350,144 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void tile_kernel(
     }
 }
 
-// out = the splits' sums, in their order
+// Few rows (up to 16): the weights are the traffic, and each is read once, from memory straight into the fragments of the
+// matrix cores.  A workgroup makes 16 hidden features; its eight wavefronts take eight parts of the summed axis and meet in LDS.
+constexpr int FEW_WAVES = 8, FEW_F = 16, FEW_ROWS = 16;
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+template <int ACT>
+__global__ __launch_bounds__(FEW_WAVES * 64, 4) void few_rows_kernel(rrm_ff_desc d, src_t x, src_t wg, src_t wu, __bf16* h, __bf16* g, __bf16* u) {
+    __shared__ float sums[FEW_WAVES][2][FEW_F][FEW_ROWS + 1];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int f0 = (int)blockIdx.x * FEW_F;
+    // lane l: row l % 16 of the weights (and of x), eight of the summed axis from (l / 16) * 8 on in a step of 32
+    const int lr = lane & 15, lk = (lane >> 4) * 8;
+    const int fr = f0 + lr < d.f ? f0 + lr : d.f - 1;
+    const int steps = (d.k + 31) / 32, s0 = steps * wave / FEW_WAVES, s1 = steps * (wave + 1) / FEW_WAVES;
+    const int whole = s1 * 32 <= d.k ? s1 : s1 - 1;  // steps without a ragged end
+    const src_t pg = wg + fr * d.wg_row, pu = wu + fr * d.wu_row, px = x + (lr < d.m ? lr : d.m - 1) * d.x_row;
+    v4f ag = {0, 0, 0, 0}, au = {0, 0, 0, 0};
+    auto some = [&](int s, auto count) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
+        v8bf bg[N], bu[N], bx[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int k = (s + j) * 32 + lk;
+            bg[j] = __builtin_bit_cast(v8bf, loose_chunk(pg + k));
+            bu[j] = __builtin_bit_cast(v8bf, loose_chunk(pu + k));
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) bx[j] = __builtin_bit_cast(v8bf, loose_chunk(px + (s + j) * 32 + lk));
+        __builtin_amdgcn_sched_barrier(0);  // all of them are on their way before the first is waited for
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            ag = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bg[j], bx[j], ag, 0, 0, 0);
+            au = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bu[j], bx[j], au, 0, 0, 0);
+        }
+    };
+    int s = s0;
+    for (; s + 8 <= whole; s += 8) some(s, std::integral_constant<int, 8>{});
+    for (; s < whole; ++s) some(s, std::integral_constant<int, 1>{});
+    if (s < s1) {
+        auto chunk = [&](src_t row) { return __builtin_bit_cast(v8bf, ragged_chunk(row, s * 32 + lk, d.k)); };
+        const v8bf bg = chunk(pg), bu = chunk(pu);
+        const v8bf bx = chunk(px);
+        ag = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bg, bx, ag, 0, 0, 0);
+        au = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bu, bx, au, 0, 0, 0);
+    }
+    // register e of lane l: feature 4 (l / 16) + e, row l % 16
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        sums[wave][0][(lane >> 4) * 4 + e][lr] = ag[e];
+        sums[wave][1][(lane >> 4) * 4 + e][lr] = au[e];
+    }
+    __syncthreads();
+    if (threadIdx.x < FEW_F * FEW_ROWS) {
+        const int f = threadIdx.x % FEW_F, r = threadIdx.x / FEW_F;
+        if (r >= d.m || f0 + f >= d.f) return;
+        float sg = 0.0f, su = 0.0f;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) sg += sums[w][0][f][r], su += sums[w][1][f][r];
+        h[r * d.h_row + f0 + f] = (__bf16)(act_value<ACT>(sg) * su);
+        if (g) {
+            g[r * d.gu_row + f0 + f] = (__bf16)sg;
+            u[r * d.gu_row + f0 + f] = (__bf16)su;
+        }
+    }
+}
+
+// Four neighbours of the splits' sums, in their order
+__device__ __forceinline__ float4 joined(const float* __restrict__ part, int64_t at, int64_t plane, int splits) {
+    float4 s = *reinterpret_cast<const float4*>(part + at);
+    for (int k = 1; k < splits; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(part + k * plane + at);
+        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    return s;
+}
+__device__ __forceinline__ void leave_four(__bf16* to, const float (&v)[4], int n) {
+    struct __attribute__((packed, aligned(2))) Four {
+        u32x2 v;
+    };
+    if (n >= 4) {
+        u32x2 w;
+        w.x = bf16_pair(v[0], v[1]), w.y = bf16_pair(v[2], v[3]);
+        reinterpret_cast<Four*>(to)->v = w;
+    } else {
+        to[0] = (__bf16)v[0];
+        if (n > 1) to[1] = (__bf16)v[1];
+        if (n > 2) to[2] = (__bf16)v[2];
+    }
+}
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, int splits, int rows, int cols, __bf16* __restrict__ out,
                                                    int64_t row) {
-    const int64_t total = (int64_t)rows * cols;
+    const int fours = (cols + 3) >> 2;
+    const int64_t total = (int64_t)rows * fours;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        float s = 0.0f;
-        for (int k = 0; k < splits; ++k) s += part[k * total + i];
-        out[i / cols * row + i % cols] = (__bf16)s;
+        const int64_t r = i / fours;
+        const int c = (int)(i - r * fours) * 4;
+        const float4 s = joined(part, 4 * i, 4 * total, splits);
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        leave_four(out + r * row + c, v, cols - c);
+    }
+}
+// H, G and U of the splits' sums
+template <int ACT>
+__global__ __launch_bounds__(256) void join_gated_kernel(const float* __restrict__ part, int splits, int rows, int cols, __bf16* __restrict__ h,
+                                                         int64_t h_row, __bf16* __restrict__ g, __bf16* __restrict__ u, int64_t gu_row) {
+    const int fours = (cols + 3) >> 2;
+    const int64_t total = (int64_t)rows * fours;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / fours;
+        const int c = (int)(i - r * fours) * 4;
+        const float4 sg = joined(part, 4 * i, 8 * total, splits), su = joined(part + 4 * total, 4 * i, 8 * total, splits);
+        const float vg[4] = {sg.x, sg.y, sg.z, sg.w}, vu[4] = {su.x, su.y, su.z, su.w};
+        float vh[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vh[e] = act_value<ACT>(vg[e]) * vu[e];
+        leave_four(h + r * h_row + c, vh, cols - c);
+        if (g) {
+            leave_four(g + r * gu_row + c, vg, cols - c);
+            leave_four(u + r * gu_row + c, vu, cols - c);
+        }
+    }
+}
+
+// Copies of up to three operands of rows of `len`, padded with zeros to whole chunks; a thread a chunk
+struct PadJob {
+    Source from[3];
+    __bf16* to[3];
+    int64_t first[4];  // chunk that each begins with; the end
+    int n, len;
+};
+__global__ __launch_bounds__(256) void pad_kernel(PadJob j) {
+    const int per = (j.len + 7) / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < j.first[j.n]; i += (int64_t)gridDim.x * 256) {
+        const int w = i < j.first[1] || j.n == 1 ? 0 : i < j.first[2] || j.n == 2 ? 1 : 2;
+        const Source from = w == 0 ? j.from[0] : w == 1 ? j.from[1] : j.from[2];
+        __bf16* to = w == 0 ? j.to[0] : w == 1 ? j.to[1] : j.to[2];
+        const int64_t at = i - (w == 0 ? 0 : w == 1 ? j.first[1] : j.first[2]), r = at / per;
+        *reinterpret_cast<u32x4*>(to + at * 8) = ragged_chunk(from.p + r * from.row, (int)(at - r * per) * 8, j.len);
     }
 }
 
@@ -386,87 +538,203 @@ void with_act(int act, F&& f) {
 
 int tiles(int n, int of) { return (n + of - 1) / of; }
 
-bool chunked(const void* p, int64_t row, int len) {  // rows of whole, aligned 16-byte chunks
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && row % 8 == 0 && len % 8 == 0;
-}
+bool chunked(const void* p, int64_t row) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && row % 8 == 0; }  // rows begin at whole chunks
 
-template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, bool RAGGED>
+template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
 hipError_t launch_tiles(Product& a, hipStream_t s) {
     constexpr int BM = MT * 32 * WM, BN = NT * 32 * WN / (KIND == GATED ? 2 : 1);
     a.tiles_m = tiles(a.rows, BM) * (KIND == HALVES ? 2 : 1);
     a.tiles_n = tiles(a.cols, BN);
-    hipLaunchKernelGGL((tile_kernel<KIND, ACT, PT, QT, MT, NT, WM, WN, RAGGED>), dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.splits),
+    hipLaunchKernelGGL((tile_kernel<KIND, ACT, PT, QT, MT, NT, WM, WN, STAGES>), dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.splits),
                        dim3(WM * WN * 64), 0, s, a);
     return hipGetLastError();
 }
-template <int KIND, int ACT, bool PT, bool QT>
-hipError_t launch_product(Product& a, bool ragged, hipStream_t s) {
-    if (ragged) return launch_tiles<KIND, ACT, PT, QT, 2, 2, 2, 2, true>(a, s);
-    const int64_t big = (int64_t)tiles(a.rows, 256) * tiles(a.cols, KIND == GATED ? 128 : 256) * (KIND == HALVES ? 2 : 1);
-    if (big >= OP_CUS) return launch_tiles<KIND, ACT, PT, QT, 4, 2, 2, 4, false>(a, s);
-    return launch_tiles<KIND, ACT, PT, QT, 2, 2, 2, 2, false>(a, s);
+// Tile shapes (gated: the columns are both projections').  A step of 64 of the summed axis takes, with `count` workgroups,
+// about first * rounds + second * count / 256 us, a round being as many workgroups as run at once (measured: 4096 -> 4096 and 4096 -> 9216
+// features, 64 to 16384 rows); the shape and the number of parts of the summed axis with the least of it are taken.
+struct Shape {
+    int bm, bn, at_once;
+    float first, second;
+};
+enum Which : int { BIG = 0, WIDE = 1, WIDE_PAIR = 2, SMALL = 3 };
+constexpr Shape SHAPES[] = {
+    {256, 256, 256, 1.4f, 0.6f}, {128, 128, 256, 0.6f, 0.1f}, {128, 128, 512, 0.85f, 0.2f}, {64, 128, 512, 0.45f, 0.2f},
+};
+struct Plan {
+    int shape, splits;
+};
+// kind, rows, cols, len, pairs as in Product; `planes`: float32 results a split leaves of each element (0: no splits)
+Plan plan_product(int kind, int rows, int cols, int len, int pairs, int planes) {
+    Plan best{SMALL, 1};
+    float least = 1e30f;
+    const int steps = tiles(len, STEP) * pairs;
+    // no product is done before its operands have come from memory, at some 4 TB/s
+    const float floor_us = 2.0f * len * pairs * ((float)rows + (float)cols * (kind == GATED ? 2 : 1)) / 4e6f;
+    for (int w = BIG; w <= SMALL; ++w) {
+        const Shape& h = SHAPES[w];
+        const int64_t t = (int64_t)tiles(rows, h.bm) * tiles(cols, kind == GATED ? h.bn / 2 : h.bn) * (kind == HALVES ? 2 : 1);
+        for (int splits = 1; splits <= (planes ? 16 : 1); splits *= 2) {
+            if (splits > 1 && steps / splits < 4) break;
+            const int64_t count = t * splits, rounds = (count + h.at_once - 1) / h.at_once;
+            float us = tiles(steps, splits) * ((float)rounds * h.first + (float)count / OP_CUS * h.second);
+            if (us < floor_us) us = floor_us;
+            // the sums' way through memory and the launch that joins them
+            if (splits > 1) us += 5.0f + (float)splits * planes * rows * (float)cols * 8.0f / 6e6f;
+            if (us < least) least = us, best = Plan{w, splits};
+        }
+    }
+    return best;
 }
 
-size_t grads_bytes(const rrm_ff_desc& d) { return round256((size_t)d.m * ((d.f + 7) / 8 * 8) * 2); }
+template <int KIND, int ACT, bool PT, bool QT>
+hipError_t launch_product(Product& a, int shape, hipStream_t s) {
+    switch (shape) {
+        case BIG: return launch_tiles<KIND, ACT, PT, QT, 4, 2, 2, 4, 2>(a, s);
+        case WIDE: return launch_tiles<KIND, ACT, PT, QT, 2, 2, 2, 2, 4>(a, s);
+        case WIDE_PAIR: return launch_tiles<KIND, ACT, PT, QT, 2, 2, 2, 2, 2>(a, s);
+        default: return launch_tiles<KIND, ACT, PT, QT, 1, 2, 2, 2, 3>(a, s);
+    }
+}
+Plan forward_plan(const rrm_ff_desc& d) { return plan_product(GATED, d.m, d.f, d.k, 1, 2); }
+Plan dx_plan(const rrm_ff_desc& d) { return plan_product(PLAIN, d.m, d.k, d.f, 2, 1); }
+
+// Up to so many rows the weights go from memory into the fragments (few_rows_kernel): 4096 -> 4096, 1 / 16 / 32 / 64 rows
+// 14.6 / 16.9 / 18.5 / 26.7 us so, 19 by tiles; 4096 -> 9216 36 / 44 / 53 / 77 us and 40.
+bool few_rows(const rrm_ff_desc& d) { return d.m <= FEW_ROWS; }
+
+// The tile kernel copies whole, aligned 16-byte chunks: rows that are not made of them are copied to the workspace first, padded with zeros.
+int round8(int n) { return (n + 7) & ~7; }
+bool loose_rows(const rrm_ff_desc& d, int64_t row) { return d.unaligned || d.k % 8 != 0 || row % 8 != 0; }
+struct Padded {
+    size_t x, wg, wu, all;  // places in the workspace, and the bytes of all
+};
+Padded padded_places(const rrm_ff_desc& d, bool x, bool w) {
+    Padded p{};
+    const size_t row = (size_t)round8(d.k) * 2;
+    auto take = [&](int rows, int64_t stride, bool used) {
+        const size_t at = p.all;
+        if (used && loose_rows(d, stride)) p.all += round256(row * rows);
+        return at;
+    };
+    p.x = take(d.m, d.x_row, x);
+    p.wg = take(d.f, d.wg_row, w);
+    p.wu = take(d.f, d.wu_row, w);
+    return p;
+}
+// Sources for the products of up to three operands of rows of k: themselves, or their padded copies (one launch makes them)
+hipError_t sources(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, unsigned char* ws, Source& sx, Source& sg, Source& su,
+                   hipStream_t s) {
+    const Padded at = padded_places(d, x != nullptr, wg != nullptr);
+    PadJob job{};
+    job.len = d.k;
+    auto one = [&](const void* p, int64_t row, int rows, size_t place) {
+        if (!p || !loose_rows(d, row)) return Source{(src_t)p, row};
+        __bf16* to = (__bf16*)(ws + place);
+        const int64_t chunks = (int64_t)rows * (round8(d.k) / 8);
+        job.from[job.n] = Source{(src_t)p, row};
+        job.to[job.n] = to;
+        job.first[job.n + 1] = job.first[job.n] + chunks;
+        ++job.n;
+        return Source{to, round8(d.k)};
+    };
+    sx = one(x, d.x_row, d.m, at.x);
+    sg = one(wg, d.wg_row, d.f, at.wg);
+    su = one(wu, d.wu_row, d.f, at.wu);
+    if (job.n == 0) return hipSuccess;
+    const int64_t groups = (job.first[job.n] + 255) / 256;
+    hipLaunchKernelGGL(pad_kernel, dim3((unsigned)(groups < OP_CUS * 64 ? groups : OP_CUS * 64)), dim3(256), 0, s, job);
+    return hipGetLastError();
+}
+
+size_t grads_bytes(const rrm_ff_desc& d) { return round256((size_t)d.m * round8(d.f) * 2); }
+size_t split_bytes(const rrm_ff_desc& d, bool backward) {
+    const int splits = (backward ? dx_plan(d) : forward_plan(d)).splits;
+    return splits > 1 ? round256((size_t)splits * d.m * tiles(backward ? d.k : d.f, 4) * 16) * (backward ? 1 : 2) : 0;
+}
 
 }  // namespace
 
-size_t ff_scratch(const rrm_ff_desc& d, bool backward) { return backward ? 2 * grads_bytes(d) : 0; }
+// forward: [padded operands][splits' sums]; backward: [dG][dU][padded operands][splits' sums]
+size_t ff_scratch(const rrm_ff_desc& d, bool backward) {
+    if (d.m == 0 || (!backward && few_rows(d))) return 0;
+    return (backward ? 2 * grads_bytes(d) : 0) + padded_places(d, true, true).all + split_bytes(d, backward);
+}
 
-hipError_t launch_gated_ff(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void*,
+hipError_t launch_gated_ff(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* ws,
                            hipStream_t s) {
+    hipError_t e = hipSuccess;
+    if (few_rows(d)) {
+        with_act(d.act, [&](auto act) {
+            hipLaunchKernelGGL((few_rows_kernel<decltype(act)::value>), dim3((unsigned)tiles(d.f, FEW_F)), dim3(FEW_WAVES * 64), 0, s, d,
+                               (src_t)x, (src_t)wg, (src_t)wu, (__bf16*)h, (__bf16*)g, (__bf16*)u);
+        });
+        return hipGetLastError();
+    }
     Product a{};
-    a.p[0] = {(src_t)x, d.x_row};
-    a.q[0] = {(src_t)wg, d.wg_row};
-    a.q[1] = {(src_t)wu, d.wu_row};
-    a.pairs = 1, a.splits = 1;
+    e = sources(d, x, wg, wu, (unsigned char*)ws, a.p[0], a.q[0], a.q[1], s);
+    if (e != hipSuccess) return e;
+    const Plan plan = forward_plan(d);
+    a.pairs = 1, a.splits = plan.splits;
+    a.part = (float*)((unsigned char*)ws + padded_places(d, true, true).all);
     a.rows = d.m, a.cols = d.f, a.len = d.k;
     a.out = (__bf16*)h, a.out2 = (__bf16*)g, a.out3 = (__bf16*)u;
     a.out_row = d.h_row, a.out2_row = d.gu_row;
-    a.vec_out = chunked(h, d.h_row, 8) && (!g || (chunked(g, d.gu_row, 8) && chunked(u, d.gu_row, 8)));
-    const bool ragged = !chunked(x, d.x_row, d.k) || !chunked(wg, d.wg_row, d.k) || !chunked(wu, d.wu_row, d.k);
-    hipError_t e = hipSuccess;
-    with_act(d.act, [&](auto act) { e = launch_product<GATED, decltype(act)::value, false, false>(a, ragged, s); });
+    with_act(d.act, [&](auto act) {
+        e = launch_product<GATED, decltype(act)::value, false, false>(a, plan.shape, s);
+        if (e != hipSuccess || a.splits == 1) return;
+        const int64_t n = ((int64_t)d.m * tiles(d.f, 4) + 255) / 256;
+        hipLaunchKernelGGL((join_gated_kernel<decltype(act)::value>), dim3((unsigned)(n < OP_CUS * 16 ? n : OP_CUS * 16)), dim3(256), 0, s, a.part,
+                           a.splits, d.m, d.f, (__bf16*)h, d.h_row, (__bf16*)g, (__bf16*)u, d.gu_row);
+        e = hipGetLastError();
+    });
     return e;
 }
 
 hipError_t launch_gated_ff_backward(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, const void* g,
                                     const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* ws, hipStream_t s) {
-    __bf16* dg = (__bf16*)ws;
-    __bf16* du = (__bf16*)((char*)ws + grads_bytes(d));
-    const int pitch = (d.f + 7) / 8 * 8;
+    unsigned char* at = (unsigned char*)ws;
+    const int pitch = round8(d.f);
+    const Source dg{(src_t)at, pitch}, du{(src_t)(at + grads_bytes(d)), pitch};
+    Source sx{}, sg{}, su{};
+    hipError_t e = hipSuccess;
     if (d.m > 0) {
+        at += 2 * grads_bytes(d);
         const int64_t chunks = (int64_t)d.m * (pitch / 8), groups = (chunks + 255) / 256;
-        const int vec = chunked(g, d.gu_row, 8) && chunked(u, d.gu_row, 8) && chunked(dh, d.h_row, 8);
+        const int vec = chunked(g, d.gu_row) && chunked(u, d.gu_row) && chunked(dh, d.h_row);
         with_act(d.act, [&](auto act) {
             hipLaunchKernelGGL((slopes_kernel<decltype(act)::value>), dim3((unsigned)(groups < OP_CUS * 32 ? groups : OP_CUS * 32)), dim3(256),
-                               0, s, d, (src_t)g, (src_t)u, (src_t)dh, vec, pitch, dg, du);
+                               0, s, d, (src_t)g, (src_t)u, (src_t)dh, vec, pitch, (__bf16*)dg.p, (__bf16*)du.p);
         });
-        if (hipError_t e = hipGetLastError()) return e;
-        if (dx) {
-            Product a{};
-            a.p[0] = {dg, pitch}, a.p[1] = {du, pitch};
-            a.q[0] = {(src_t)wg, d.wg_row}, a.q[1] = {(src_t)wu, d.wu_row};
-            a.pairs = 2, a.splits = 1;
-            a.rows = d.m, a.cols = d.k, a.len = d.f;
-            a.out = (__bf16*)dx, a.out_row = d.dx_row;
-            a.vec_out = chunked(dx, d.dx_row, 8);
-            const bool ragged = !chunked(wg, d.wg_row, d.k) || !chunked(wu, d.wu_row, d.k);
-            if (hipError_t e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(a, ragged, s)) return e;
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = sources(d, dwg ? x : nullptr, dx ? wg : nullptr, dx ? wu : nullptr, at, sx, sg, su, s);
+        if (e != hipSuccess) return e;
+        at += padded_places(d, true, true).all;
+    }
+    if (d.m > 0 && dx) {
+        const Plan plan = dx_plan(d);
+        Product a{};
+        a.p[0] = dg, a.p[1] = du, a.q[0] = sg, a.q[1] = su;
+        a.pairs = 2, a.splits = plan.splits;
+        a.part = (float*)at;
+        a.rows = d.m, a.cols = d.k, a.len = d.f;
+        a.out = (__bf16*)dx, a.out_row = d.dx_row;
+        if ((e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(a, plan.shape, s)) != hipSuccess) return e;
+        if (a.splits > 1) {
+            const int64_t n = ((int64_t)d.m * tiles(d.k, 4) + 255) / 256;
+            hipLaunchKernelGGL(join_kernel, dim3((unsigned)(n < OP_CUS * 16 ? n : OP_CUS * 16)), dim3(256), 0, s, a.part, a.splits, d.m,
+                               d.k, (__bf16*)dx, d.dx_row);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }
-    if (dwg) {
+    if (dwg) {  // (no rows: sums of nothing, zeros)
         Product a{};
-        a.p[0] = {dg, pitch}, a.p[1] = {du, pitch};
-        a.q[0] = {(src_t)x, d.x_row};
+        a.p[0] = dg, a.p[1] = du, a.q[0] = sx;
         a.pairs = 1, a.splits = 1;
         a.rows = d.f, a.cols = d.k, a.len = d.m;
         a.out = (__bf16*)dwg, a.out_row = d.dwg_row, a.out2 = (__bf16*)dwu, a.out2_row = d.dwu_row;
-        a.vec_out = chunked(dwg, d.dwg_row, 8) && chunked(dwu, d.dwu_row, 8);
-        const bool ragged = !chunked(x, d.x_row, d.k);
-        if (hipError_t e = launch_product<HALVES, RRM_ACT_NONE, true, true>(a, ragged, s)) return e;
+        e = launch_product<HALVES, RRM_ACT_NONE, true, true>(a, plan_product(HALVES, d.f, d.k, d.m, 1, 0).shape, s);
     }
-    return hipSuccess;
+    return e;
 }
 
 }  // namespace rrm

@@ -184,8 +184,9 @@ rrm_status rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* wg, 
         return record_failure(RRM_ERR_SHAPE, "feed-forward: strides out of range");
     if (!apart(1, 0, d.m, d.h_row, d.f) || (g && !apart(1, 0, d.m, d.gu_row, d.f)))
         return record_failure(RRM_ERR_SHAPE, "feed-forward: two elements of an output lie at one place");
-    if (misaligned(x, 2) || misaligned(wg, 2) || misaligned(wu, 2) || misaligned(h, 2) || misaligned(g, 2) || misaligned(u, 2))
-        return record_failure(RRM_ERR_ALIGN, "feed-forward: a pointer is not aligned to its element");
+    const size_t e = d.unaligned ? 2 : 16;
+    if (misaligned(x, e) || misaligned(wg, e) || misaligned(wu, e) || misaligned(h, 2) || misaligned(g, 2) || misaligned(u, 2))
+        return record_failure(RRM_ERR_ALIGN, "feed-forward: a pointer is not aligned (to 16 bytes, to its element: see rrm_ff_desc)");
     if (rrm_status st = check_workspace(workspace, workspace_bytes, ff_scratch(d, false))) return st;
     return finish(launch_gated_ff(d, x, wg, wu, h, g, u, workspace, static_cast<hipStream_t>(hip_stream)));
 }
@@ -205,9 +206,10 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
         return record_failure(RRM_ERR_SHAPE, "feed-forward: strides out of range");
     if ((dx && !apart(1, 0, d.m, d.dx_row, d.k)) || (dwg && (!apart(1, 0, d.f, d.dwg_row, d.k) || !apart(1, 0, d.f, d.dwu_row, d.k))))
         return record_failure(RRM_ERR_SHAPE, "feed-forward: two elements of an output lie at one place");
-    if (misaligned(x, 2) || misaligned(wg, 2) || misaligned(wu, 2) || misaligned(g, 2) || misaligned(u, 2) || misaligned(dh, 2) ||
+    const size_t e = d.unaligned ? 2 : 16;
+    if (misaligned(x, e) || misaligned(wg, e) || misaligned(wu, e) || misaligned(g, 2) || misaligned(u, 2) || misaligned(dh, 2) ||
         misaligned(dx, 2) || misaligned(dwg, 2) || misaligned(dwu, 2))
-        return record_failure(RRM_ERR_ALIGN, "feed-forward: a pointer is not aligned to its element");
+        return record_failure(RRM_ERR_ALIGN, "feed-forward: a pointer is not aligned (to 16 bytes, to its element: see rrm_ff_desc)");
     if (rrm_status st = check_workspace(workspace, workspace_bytes, ff_scratch(d, true))) return st;
     return finish(launch_gated_ff_backward(d, x, wg, wu, g, u, dh, dx, dwg, dwu, workspace, static_cast<hipStream_t>(hip_stream)));
 }

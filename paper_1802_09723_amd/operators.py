@@ -31,7 +31,8 @@ class ScanDesc(ctypes.Structure):
 class FFDesc(ctypes.Structure):
     """``rrm_ff_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("m", "k", "f", "act")]
-                + [(k, ctypes.c_int64) for k in ("x_row", "wg_row", "wu_row", "h_row", "gu_row", "dx_row", "dwg_row", "dwu_row")])
+                + [(k, ctypes.c_int64) for k in ("x_row", "wg_row", "wu_row", "h_row", "gu_row", "dx_row", "dwg_row", "dwu_row")]
+                + [("unaligned", ctypes.c_int)])
 
 
 # Descriptors by their values, each with the bytes of workspace its call takes: a live frame's call fills in no structure.
@@ -285,7 +286,7 @@ def gated_ff(x, wg, wu, act: str = "silu", out=None, save=None, stream=None):
         if _row(save[1], "save[1]") != row:
             raise ValueError("save: both tensors need the same strides")
     d, ref, need = _desc(FFDesc, "rrm_gated_ff_workspace", 0, m, k, f, _act(act), _row(x, "x"), _row(wg, "wg"), _row(wu, "wu"),
-                         _row(out, "out"), row, 0, 0, 0)
+                         _row(out, "out"), row, 0, 0, 0, int((px | pg | pu) & 15 != 0))
     ws, pw = _workspace(need, x.device)
     _check(lib().rrm_gated_ff(ref, px, pg, pu, po, sg, su, pw, need, _stream_ptr(stream)))
     _used_on(stream, ws, out if made else None)
@@ -312,7 +313,8 @@ def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None,
     if _row(u, "u") != row:
         raise ValueError("g, u: both tensors need the same strides")
     d, ref, need = _desc(FFDesc, "rrm_gated_ff_workspace", 1, m, k, f, _act(act), _row(x, "x"), _row(wg, "wg"), _row(wu, "wu"),
-                         _row(dh, "dh"), row, _row(dx, "dx"), _row(dwg, "dwg"), _row(dwu, "dwu"))
+                         _row(dh, "dh"), row, _row(dx, "dx"), _row(dwg, "dwg"), _row(dwu, "dwu"),
+                         int((px | pg | pu) & 15 != 0))
     ws, pw = _workspace(need, x.device)
     _check(lib().rrm_gated_ff_backward(ref, px, pg, pu, sg, su, pdh, qx, qg, qu, pw, need, _stream_ptr(stream)))
     _used_on(stream, ws, *(t for t, was in zip((dx, dwg, dwu), made) if was))
