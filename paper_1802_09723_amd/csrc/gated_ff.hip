@@ -526,16 +526,6 @@ __global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src
     }
 }
 
-template <typename F>
-void with_act(int act, F&& f) {
-    switch (act) {
-        case RRM_ACT_RELU: f(std::integral_constant<int, RRM_ACT_RELU>{}); break;
-        case RRM_ACT_SILU: f(std::integral_constant<int, RRM_ACT_SILU>{}); break;
-        case RRM_ACT_GELU: f(std::integral_constant<int, RRM_ACT_GELU>{}); break;
-        default: f(std::integral_constant<int, RRM_ACT_NONE>{}); break;
-    }
-}
-
 int tiles(int n, int of) { return (n + of - 1) / of; }
 
 bool chunked(const void* p, int64_t row) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && row % 8 == 0; }  // rows begin at whole chunks

@@ -5,135 +5,648 @@ namespace rrm {
 
 namespace {
 
-constexpr int GN_THREADS = 256;
+constexpr int HELD_GROUPS = 64;  // groups of a workgroup at most
 
-// sum over the workgroup, to every thread
-__device__ float wg_sum(float v, float* lds) {
+// ---- samples that registers hold ---------------------------------------------------------------------------------------
+//
+// A workgroup has the `cb` channels of whole groups of one sample, all positions; a thread keeps up to P vectors of VEC neighbouring
+// channels (always the same channels) of positions R apart in registers.  So x (backward: and dy) is read once, the variance is summed about the
+// mean, and the result leaves without another look at memory.
+struct HeldGeom {
+    int cb, blocks;  // channels of a workgroup; workgroups of a sample
+    int lanes;       // threads of a position, a power of two
+    float r_cg;      // 1 / channels of a group
+};
+
+template <typename T, int VEC>
+struct Held {  // VEC elements as they lie in memory, at the alignment of one
+    static constexpr int WORDS = (VEC * (int)sizeof(T) + 3) / 4;
+    unsigned int w[WORDS];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (VEC * sizeof(T) == 2) w[0] = *reinterpret_cast<const unsigned short*>(p);
+        else load_words<WORDS>(p, w);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+    }
+};
+
+// A workgroup's place: id -> sample, block; a sample's blocks, whose runs share cache lines, are on one XCD (ids go to the eight in turn)
+__device__ __forceinline__ bool held_place(int id, int n, int blocks, int& sample, int& block) {
+    const int k = id >> 3;
+    block = k % blocks;
+    sample = (k / blocks) * 8 + (id & 7);
+    return sample < n;
+}
+
+// A thread's vector of channels: from `at` on, of which those before `first` are another thread's (the last vector of a workgroup whose channels are
+// no whole vectors begins early, which is never before the row: a workgroup has VEC channels at least, or others before it) and not to be summed or stored.  A thread without channels has first = VEC.
+template <int VEC>
+struct Span {
+    int at, first;
+    __device__ __forceinline__ Span(int slot, int c0, int cb) {
+        const int c = c0 + slot * VEC, end = c0 + cb - VEC;
+        const bool none = slot * VEC >= cb;
+        at = none || c > end ? (end > 0 ? end : 0) : c;
+        first = none ? VEC : c - at;
+    }
+};
+
+// part[row of the workgroup][channel] -> sums over the rows of a wavefront's threads of equal channels are in `v` of its first lanes; here they
+// go to LDS, one row a wavefront (or a set of wavefronts that span the channels)
+template <int VEC, int NS>
+__device__ __forceinline__ void rows_to_lds(float (&v)[NS][VEC], int lanes, int cb, float* part, int stride, int at, int first) {
+    for (int m = lanes; m < OP_WAVE; m <<= 1)
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[k][i] += __shfl_xor(v[k][i], m);
+    const int row = (int)threadIdx.x / (lanes > OP_WAVE ? lanes : OP_WAVE);
+    if (((int)threadIdx.x & (OP_WAVE - 1)) < lanes)
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i >= first) part[k * stride + row * cb + at + i] = v[k][i];
+}
+
+// sums over the rows of part and a group's channels, by as many lanes a group as it has channels (up to 64): f(group, sum) once for each
+template <int THREADS, typename F>
+__device__ __forceinline__ void groups_of_rows(const float* part, int rows, int cb, int cg, F&& f) {
+    int per = 1;
+    while (per < cg && per < OP_WAVE) per <<= 1;
+    const int ng = cb / cg, at = (int)threadIdx.x & (per - 1);
+    for (int g = (int)threadIdx.x / per; g < ng; g += THREADS / per) {
+        float s = 0.0f;
+        for (int r = 0; r < rows; ++r)
+            for (int c = at; c < cg; c += per) s += part[r * cb + g * cg + c];
+        for (int m = 1; m < per; m <<= 1) s += __shfl_xor(s, m);
+        if (at == 0) f(g, s);
+    }
+}
+
+template <typename TX, typename TY, int VEC, int P, int THREADS>
+__global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom h, const TX* __restrict__ x, const float* __restrict__ gamma,
+                                                       const float* __restrict__ beta, TY* __restrict__ y, float* __restrict__ stats) {
+    __shared__ float part[THREADS * VEC];
+    __shared__ float gs[2][HELD_GROUPS];
+    int sample, block;
+    if (!held_place((int)blockIdx.x, d.n, h.blocks, sample, block)) return;
+    const int cg = d.c / d.groups, c0 = block * h.cb, cb = d.c - c0 < h.cb ? d.c - c0 : h.cb;
+    const int slot = (int)threadIdx.x & (h.lanes - 1), row = (int)threadIdx.x / h.lanes, R = THREADS / h.lanes;
+    const int rows = THREADS / (h.lanes > OP_WAVE ? h.lanes : OP_WAVE);  // of part
+    const Span<VEC> me(slot, c0, cb);
+    const int c = me.at;
+    const TX* xs = x + sample * d.x_sample + c;
+    Held<TX, VEC> v[P];
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const int pos = row + j * R < d.positions ? row + j * R : d.positions - 1;  // (not under a condition: all loads are on their way at once)
+        v[j].load(xs + pos * d.x_position);
+    }
+    float ga[VEC], be[VEC], mean[VEC], s[1][VEC];
+    int gi[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        ga[i] = gamma ? gamma[c + i] : 1.0f;
+        be[i] = beta ? beta[c + i] : 0.0f;
+        gi[i] = i < me.first ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
+        s[0][i] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+        if (row + j * R < d.positions)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[0][i] += v[j].get(i);
+    rows_to_lds<VEC, 1>(s, h.lanes, cb, part, 0, c - c0, me.first);
+    __syncthreads();
+    const float inv = 1.0f / ((float)d.positions * (float)cg);
+    float* st = stats ? stats + 2 * ((int64_t)sample * d.groups + c0 / cg) : nullptr;
+    groups_of_rows<THREADS>(part, rows, cb, cg, [&](int g, float sum) {
+        gs[0][g] = sum * inv;
+        if (st) st[2 * g] = sum * inv;
+    });
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) mean[i] = gs[0][gi[i]], s[0][i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        if (row + j * R < d.positions)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float t = v[j].get(i) - mean[i];
+                s[0][i] += t * t;
+            }
+    }
+    rows_to_lds<VEC, 1>(s, h.lanes, cb, part, 0, c - c0, me.first);
+    __syncthreads();
+    groups_of_rows<THREADS>(part, rows, cb, cg, [&](int g, float sum) {
+        const float r = 1.0f / sqrtf(sum * inv + d.eps);
+        gs[1][g] = r;
+        if (st) st[2 * g + 1] = r;
+    });
+    __syncthreads();
+    if (me.first == VEC) return;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) ga[i] *= gs[1][gi[i]];
+    TY* ys = y + sample * d.y_sample + c;
+    with_act(d.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const int pos = row + j * R;
+            if (pos >= d.positions) continue;
+            float o[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) o[i] = act_value<decltype(act)::value>((v[j].get(i) - mean[i]) * ga[i] + be[i]);
+            store_some<VEC>(ys + pos * d.y_position, o, me.first);
+        }
+    });
+}
+
+// part2: [2][n][c], the samples' sums of dz and of dz * xh.  KEEP: dz stays in registers as well, else its slope is made twice
+template <typename TX, typename TY, int VEC, int P, int THREADS, bool KEEP>
+__global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, HeldGeom h, const TX* __restrict__ x, const float* __restrict__ stats,
+                                                            const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                            const TY* __restrict__ dy, TX* __restrict__ dx, float* __restrict__ part2) {
+    __shared__ float part[2 * THREADS * VEC];
+    __shared__ float gs[2][HELD_GROUPS];
+    int sample, block;
+    if (!held_place((int)blockIdx.x, d.n, h.blocks, sample, block)) return;
+    const int cg = d.c / d.groups, c0 = block * h.cb, cb = d.c - c0 < h.cb ? d.c - c0 : h.cb;
+    const int slot = (int)threadIdx.x & (h.lanes - 1), row = (int)threadIdx.x / h.lanes, R = THREADS / h.lanes;
+    const int rows = THREADS / (h.lanes > OP_WAVE ? h.lanes : OP_WAVE);
+    const Span<VEC> me(slot, c0, cb);
+    const int c = me.at;
+    const TX* xs = x + sample * d.x_sample + c;
+    const TY* dys = dy + sample * d.y_sample + c;
+    Held<TX, VEC> v[P];
+    Held<TY, VEC> w[P];
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const int pos = row + j * R < d.positions ? row + j * R : d.positions - 1;
+        v[j].load(xs + pos * d.x_position);
+        w[j].load(dys + pos * d.y_position);
+    }
+    const float* st = stats + 2 * ((int64_t)sample * d.groups + c0 / cg);
+    float ga[VEC], be[VEC], mean[VEC], r[VEC], s[2][VEC];
+    int gi[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        ga[i] = gamma ? gamma[c + i] : 1.0f;
+        be[i] = beta ? beta[c + i] : 0.0f;
+        gi[i] = i < me.first ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
+        mean[i] = st[2 * gi[i]];
+        r[i] = st[2 * gi[i] + 1];
+        s[0][i] = s[1][i] = 0.0f;
+    }
+    float kept[KEEP ? P : 1][VEC];
+    with_act(d.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            if (row + j * R >= d.positions) continue;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float xh = (v[j].get(i) - mean[i]) * r[i];
+                float value, slope;
+                act_pair<decltype(act)::value>(ga[i] * xh + be[i], value, slope);
+                const float dz = w[j].get(i) * slope;
+                if (KEEP) kept[KEEP ? j : 0][i] = dz;
+                s[0][i] += dz;
+                s[1][i] += dz * xh;
+            }
+        }
+    });
+    constexpr int STRIDE = THREADS * VEC;
+    rows_to_lds<VEC, 2>(s, h.lanes, cb, part, STRIDE, c - c0, me.first);
+    __syncthreads();
+    // the channels' sums leave for dgamma and dbeta, and, times gamma, become the first row
+    for (int ch = threadIdx.x; ch < cb; ch += THREADS) {
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int k = 0; k < rows; ++k) s1 += part[k * cb + ch], s2 += part[STRIDE + k * cb + ch];
+        part2[(int64_t)sample * d.c + c0 + ch] = s1;
+        part2[((int64_t)d.n + sample) * d.c + c0 + ch] = s2;
+        const float g = gamma ? gamma[c0 + ch] : 1.0f;
+        part[ch] = g * s1;
+        part[STRIDE + ch] = g * s2;
+    }
+    if (!dx) return;
+    __syncthreads();
+    const float inv = 1.0f / ((float)d.positions * (float)cg);
+    groups_of_rows<THREADS>(part, 1, cb, cg, [&](int g, float sum) { gs[0][g] = sum * inv; });
+    groups_of_rows<THREADS>(part + STRIDE, 1, cb, cg, [&](int g, float sum) { gs[1][g] = sum * inv; });
+    __syncthreads();
+    if (me.first == VEC) return;
+    TX* dxs = dx + sample * d.dx_sample + c;
+    float gp[VEC], gq[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) gp[i] = gs[0][gi[i]], gq[i] = gs[1][gi[i]];
+    auto leave = [&](int j, auto dz_of) __attribute__((always_inline)) {
+        const int pos = row + j * R;
+        if (pos >= d.positions) return;
+        float o[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float xh = (v[j].get(i) - mean[i]) * r[i];
+            o[i] = r[i] * (ga[i] * dz_of(i, xh) - gp[i] - xh * gq[i]);
+        }
+        store_some<VEC>(dxs + pos * d.dx_position, o, me.first);
+    };
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) leave(j, [&](int i, float) { return kept[KEEP ? j : 0][i]; });
+    } else {
+        with_act(d.act, [&](auto act) {
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                leave(j, [&](int i, float xh) {
+                    float value, slope;
+                    act_pair<decltype(act)::value>(ga[i] * xh + be[i], value, slope);
+                    return w[j].get(i) * slope;
+                });
+        });
+    }
+}
+
+// ---- samples that registers do not hold ----------------------------------------------------------------------------------
+//
+// Slices of a sample's positions: their channels' means and squares (backward: sums of dz and dz * xh), a joining of slices and channels for
+// each group, and a second pass over x (and dy).
+struct SliceGeom {
+    int slices, span;   // of a sample; positions of a slice
+    int blocks, lanes;  // sets of channels; threads of a position, a power of two
+    float r_cg;
+};
+constexpr int SLICE_THREADS = 256;
+
+// what a thread of a slice's workgroup has: its channels and rows
+template <int VEC>
+struct Slice {
+    int sample, slice, row, step, p0, p1;
+    Span<VEC> me;
+    __device__ __forceinline__ Slice(const rrm_norm_desc& d, const SliceGeom& g)
+        : sample((int)(blockIdx.x / (unsigned)(g.slices * g.blocks))),
+          slice((int)(blockIdx.x / (unsigned)g.blocks) % g.slices),
+          row((int)threadIdx.x / g.lanes),
+          step(SLICE_THREADS / g.lanes),
+          p0(slice * g.span),
+          p1(p0 + g.span < d.positions ? p0 + g.span : d.positions),
+          me((int)threadIdx.x & (g.lanes - 1), (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC,
+             min(d.c - (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC, g.lanes * VEC)) {}
+};
+
+// sums over the workgroup's rows, to the first row's threads (lanes <= 256, any number of rows)
+template <int VEC, int NS>
+__device__ __forceinline__ void sum_rows(float (&v)[NS][VEC], int lanes, float* lds) {
+    for (int half = SLICE_THREADS / 2; half >= lanes; half >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x >= half && (int)threadIdx.x < 2 * half)
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) lds[(k * VEC + i) * SLICE_THREADS / 2 + (int)threadIdx.x - half] = v[k][i];
+        __syncthreads();
+        if ((int)threadIdx.x < half)
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[k][i] += lds[(k * VEC + i) * SLICE_THREADS / 2 + (int)threadIdx.x];
+    }
+}
+
+// part: [n][slices][2][c], mean and sum of squares about it of each channel of a slice.  Values are taken less the slice's first: the sums lose
+// nothing to a mean far from zero.
+template <typename TX, int VEC>
+__global__ __launch_bounds__(SLICE_THREADS) void slice_stats_kernel(rrm_norm_desc d, SliceGeom g, const TX* __restrict__ x, float* __restrict__ part) {
+    __shared__ float lds[VEC * SLICE_THREADS / 2];
+    __shared__ float first_mean[SLICE_THREADS * VEC];
+    const Slice<VEC> t(d, g);
+    const TX* xs = x + t.sample * d.x_sample + t.me.at;
+    const int lane = (int)threadIdx.x & (g.lanes - 1);
+    float s[1][VEC], v[VEC], base[VEC];
+    load_vec<VEC>(xs + t.p0 * d.x_position, base);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s[0][i] = 0.0f;
+#pragma unroll 4
+    for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
+        load_vec<VEC>(xs + p * d.x_position, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[0][i] += v[i] - base[i];
+    }
+    sum_rows<VEC, 1>(s, g.lanes, lds);
+    const float inv = 1.0f / (float)(t.p1 - t.p0);
+    if (t.row == 0)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) first_mean[lane * VEC + i] = base[i] + s[0][i] * inv;
+    __syncthreads();
+    float mean[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) mean[i] = first_mean[lane * VEC + i], s[0][i] = 0.0f;
+    // (the slice again, out of the caches: some tens of kilobytes)
+#pragma unroll 4
+    for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
+        load_vec<VEC>(xs + p * d.x_position, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[0][i] += (v[i] - mean[i]) * (v[i] - mean[i]);
+    }
+    sum_rows<VEC, 1>(s, g.lanes, lds);
+    if (t.row != 0) return;
+    float* to = part + ((int64_t)t.sample * g.slices + t.slice) * 2 * d.c + t.me.at;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+        if (i >= t.me.first) to[i] = mean[i], to[d.c + i] = s[0][i];
+}
+
+__device__ __forceinline__ float sum_256(float v, float* lds) {
 #pragma unroll
     for (int m = 1; m < OP_WAVE; m <<= 1) v += __shfl_xor(v, m);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    float s = 0.0f;
-    for (int i = 0; i < GN_THREADS / OP_WAVE; ++i) s += lds[i];
-    return s;
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// One workgroup per (sample, group): mean, variance and result in three passes over the group.
-template <typename TX, typename TY, int ACT>
-__global__ __launch_bounds__(GN_THREADS) void norm_kernel(rrm_norm_desc d, const TX* __restrict__ x, const float* __restrict__ gamma,
-                                                          const float* __restrict__ beta, TY* __restrict__ y, float* __restrict__ stats) {
-    __shared__ float lds[GN_THREADS / OP_WAVE];
-    const int cg = d.c / d.groups, i = (int)blockIdx.x / d.groups, g = (int)blockIdx.x % d.groups;
-    const TX* xs = x + i * d.x_sample + g * cg;
-    TY* ys = y + i * d.y_sample + g * cg;
-    const long long m = (long long)d.positions * cg;
-    float s = 0.0f;
-    for (long long k = threadIdx.x; k < m; k += GN_THREADS) s += load_elem(xs + (k / cg) * d.x_position + k % cg);
-    const float mean = wg_sum(s, lds) / (float)m;
-    s = 0.0f;
-    for (long long k = threadIdx.x; k < m; k += GN_THREADS) {
-        const float v = load_elem(xs + (k / cg) * d.x_position + k % cg) - mean;
-        s += v * v;
+// One workgroup a group of a sample: the slices' and channels' means and squares become the group's
+__global__ __launch_bounds__(256) void join_stats_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, float* __restrict__ stats) {
+    __shared__ float lds[4];
+    const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
+    const float* from = part + (int64_t)sample * g.slices * 2 * d.c + group * cg;
+    const int64_t all = (int64_t)g.slices * cg;
+    const float per = 1.0f / ((float)d.positions * (float)cg);
+    float m = 0.0f;
+    for (int64_t k = threadIdx.x; k < all; k += 256) {
+        const int slice = (int)(k / cg), p0 = slice * g.span;
+        m += from[(int64_t)slice * 2 * d.c + k % cg] * (float)(min(p0 + g.span, d.positions) - p0);
     }
-    const float r = 1.0f / sqrtf(wg_sum(s, lds) / (float)m + d.eps);
-    if (stats && threadIdx.x == 0) stats[2 * blockIdx.x] = mean, stats[2 * blockIdx.x + 1] = r;
-    for (long long k = threadIdx.x; k < m; k += GN_THREADS) {
-        const int c = (int)(k % cg);
-        const float xh = (load_elem(xs + (k / cg) * d.x_position + c) - mean) * r;
-        const float z = (gamma ? gamma[g * cg + c] : 1.0f) * xh + (beta ? beta[g * cg + c] : 0.0f);
-        store_elem(ys + (k / cg) * d.y_position + c, act_value<ACT>(z));
+    const float mean = sum_256(m, lds) * per;
+    float q = 0.0f;
+    for (int64_t k = threadIdx.x; k < all; k += 256) {
+        const int slice = (int)(k / cg), p0 = slice * g.span;
+        const float* e = from + (int64_t)slice * 2 * d.c + k % cg;
+        const float off = e[0] - mean;
+        q += e[d.c] + off * off * (float)(min(p0 + g.span, d.positions) - p0);
     }
+    const float r = 1.0f / sqrtf(sum_256(q, lds) * per + d.eps);
+    if (threadIdx.x == 0) stats[2 * (int64_t)blockIdx.x] = mean, stats[2 * (int64_t)blockIdx.x + 1] = r;
 }
 
-// One workgroup per (sample, group): the sums of dz and dz * xh of each channel, left in part[2][n][c], then dx.
-template <typename TX, typename TY, int ACT>
-__global__ __launch_bounds__(GN_THREADS) void norm_back_kernel(rrm_norm_desc d, const TX* __restrict__ x, const float* __restrict__ stats,
-                                                               const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                               const TY* __restrict__ dy, TX* __restrict__ dx, float* __restrict__ part) {
-    __shared__ float lds[GN_THREADS / OP_WAVE];
-    const int cg = d.c / d.groups, i = (int)blockIdx.x / d.groups, g = (int)blockIdx.x % d.groups;
-    const TX* xs = x + i * d.x_sample + g * cg;
-    const TY* dys = dy + i * d.y_sample + g * cg;
-    const float mean = stats[2 * blockIdx.x], r = stats[2 * blockIdx.x + 1];
+template <typename TX, typename TY, int VEC>
+__global__ __launch_bounds__(SLICE_THREADS) void slice_apply_kernel(rrm_norm_desc d, SliceGeom g, const TX* __restrict__ x, const float* __restrict__ gamma,
+                                                                    const float* __restrict__ beta, const float* __restrict__ stats, TY* __restrict__ y) {
+    const Slice<VEC> t(d, g);
+    if (t.me.first == VEC) return;
+    const TX* xs = x + t.sample * d.x_sample + t.me.at;
+    TY* ys = y + t.sample * d.y_sample + t.me.at;
+    const float* st = stats + 2 * (int64_t)t.sample * d.groups;
+    float ga[VEC], be[VEC], mean[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
+        mean[i] = st[2 * gi];
+        ga[i] = (gamma ? gamma[c] : 1.0f) * st[2 * gi + 1];
+        be[i] = beta ? beta[c] : 0.0f;
+    }
+    with_act(d.act, [&](auto act) {
+#pragma unroll 4
+        for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
+            float v[VEC];
+            load_vec<VEC>(xs + p * d.x_position, v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = act_value<decltype(act)::value>((v[i] - mean[i]) * ga[i] + be[i]);
+            store_some<VEC>(ys + p * d.y_position, v, t.me.first);
+        }
+    });
+}
+
+// part: [2][n * slices][c], the slices' sums of dz and dz * xh (the layout that norm_params_kernel sums)
+template <typename TX, typename TY, int VEC>
+__global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc d, SliceGeom g, const TX* __restrict__ x, const float* __restrict__ stats,
+                                                                   const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                                   const TY* __restrict__ dy, float* __restrict__ part) {
+    __shared__ float lds[2 * VEC * SLICE_THREADS / 2];
+    const Slice<VEC> t(d, g);
+    const TX* xs = x + t.sample * d.x_sample + t.me.at;
+    const TY* dys = dy + t.sample * d.y_sample + t.me.at;
+    const float* st = stats + 2 * (int64_t)t.sample * d.groups;
+    float ga[VEC], be[VEC], mean[VEC], r[VEC], s[2][VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
+        mean[i] = st[2 * gi];
+        r[i] = st[2 * gi + 1];
+        ga[i] = gamma ? gamma[c] : 1.0f;
+        be[i] = beta ? beta[c] : 0.0f;
+        s[0][i] = s[1][i] = 0.0f;
+    }
+    with_act(d.act, [&](auto act) {
+#pragma unroll 2
+        for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
+            float v[VEC], w[VEC];
+            load_vec<VEC>(xs + p * d.x_position, v);
+            load_vec<VEC>(dys + p * d.y_position, w);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float xh = (v[i] - mean[i]) * r[i];
+                float value, slope;
+                act_pair<decltype(act)::value>(ga[i] * xh + be[i], value, slope);
+                s[0][i] += w[i] * slope;
+                s[1][i] += w[i] * slope * xh;
+            }
+        }
+    });
+    sum_rows<VEC, 2>(s, g.lanes, lds);
+    if (t.row != 0) return;
+    const int64_t k = (int64_t)t.sample * g.slices + t.slice, rows = (int64_t)d.n * g.slices;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+        if (i >= t.me.first) part[k * d.c + t.me.at + i] = s[0][i], part[(rows + k) * d.c + t.me.at + i] = s[1][i];
+}
+
+// One workgroup a group of a sample: means of gamma dz and of gamma dz xh, [n][groups][2]
+__global__ __launch_bounds__(256) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, const float* __restrict__ gamma,
+                                                        float* __restrict__ means) {
+    __shared__ float lds[4];
+    const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
+    const int64_t rows = (int64_t)d.n * g.slices, all = (int64_t)g.slices * cg;
     float p = 0.0f, q = 0.0f;
-    for (int c = 0; c < cg; ++c) {
-        const float ga = gamma ? gamma[g * cg + c] : 1.0f, be = beta ? beta[g * cg + c] : 0.0f;
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int k = threadIdx.x; k < d.positions; k += GN_THREADS) {
-            const float xh = (load_elem(xs + k * d.x_position + c) - mean) * r;
-            float v, slope;
-            act_pair<ACT>(ga * xh + be, v, slope);
-            const float dz = load_elem(dys + k * d.y_position + c) * slope;
-            s1 += dz;
-            s2 += dz * xh;
-        }
-        s1 = wg_sum(s1, lds);
-        s2 = wg_sum(s2, lds);
-        if (threadIdx.x == 0) {
-            part[(size_t)i * d.c + g * cg + c] = s1;
-            part[(size_t)d.n * d.c + (size_t)i * d.c + g * cg + c] = s2;
-        }
-        p += ga * s1;
-        q += ga * s2;
+    for (int64_t k = threadIdx.x; k < all; k += 256) {
+        const int c = group * cg + (int)(k % cg);
+        const int64_t row = (int64_t)sample * g.slices + k / cg;
+        const float ga = gamma ? gamma[c] : 1.0f;
+        p += ga * part[row * d.c + c];
+        q += ga * part[(rows + row) * d.c + c];
     }
-    if (!dx) return;
-    TX* dxs = dx + i * d.dx_sample + g * cg;
-    const long long m = (long long)d.positions * cg;
-    p /= (float)m;
-    q /= (float)m;
-    for (long long k = threadIdx.x; k < m; k += GN_THREADS) {
-        const int c = (int)(k % cg);
-        const float ga = gamma ? gamma[g * cg + c] : 1.0f, be = beta ? beta[g * cg + c] : 0.0f;
-        const float xh = (load_elem(xs + (k / cg) * d.x_position + c) - mean) * r;
-        float v, slope;
-        act_pair<ACT>(ga * xh + be, v, slope);
-        const float dz = load_elem(dys + (k / cg) * d.y_position + c) * slope;
-        store_elem(dxs + (k / cg) * d.dx_position + c, r * (ga * dz - p - xh * q));
-    }
+    const float per = 1.0f / ((float)d.positions * (float)cg);
+    p = sum_256(p, lds) * per;
+    q = sum_256(q, lds) * per;
+    if (threadIdx.x == 0) means[2 * (int64_t)blockIdx.x] = p, means[2 * (int64_t)blockIdx.x + 1] = q;
 }
 
-// dbeta and dgamma: the samples' sums in their order (no samples: zeros)
-__global__ void norm_params_kernel(const float* __restrict__ part, int n, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    const int ch = (int)(blockIdx.x * blockDim.x + threadIdx.x);
-    if (ch >= c) return;
+template <typename TX, typename TY, int VEC>
+__global__ __launch_bounds__(SLICE_THREADS) void slice_dx_kernel(rrm_norm_desc d, SliceGeom g, const TX* __restrict__ x, const float* __restrict__ stats,
+                                                                 const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                                 const TY* __restrict__ dy, const float* __restrict__ means, TX* __restrict__ dx) {
+    const Slice<VEC> t(d, g);
+    if (t.me.first == VEC) return;
+    const TX* xs = x + t.sample * d.x_sample + t.me.at;
+    const TY* dys = dy + t.sample * d.y_sample + t.me.at;
+    TX* dxs = dx + t.sample * d.dx_sample + t.me.at;
+    const float *st = stats + 2 * (int64_t)t.sample * d.groups, *me = means + 2 * (int64_t)t.sample * d.groups;
+    float ga[VEC], be[VEC], mean[VEC], r[VEC], gp[VEC], gq[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
+        mean[i] = st[2 * gi];
+        r[i] = st[2 * gi + 1];
+        gp[i] = me[2 * gi];
+        gq[i] = me[2 * gi + 1];
+        ga[i] = gamma ? gamma[c] : 1.0f;
+        be[i] = beta ? beta[c] : 0.0f;
+    }
+    with_act(d.act, [&](auto act) {
+#pragma unroll 2
+        for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
+            float v[VEC], w[VEC];
+            load_vec<VEC>(xs + p * d.x_position, v);
+            load_vec<VEC>(dys + p * d.y_position, w);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float xh = (v[i] - mean[i]) * r[i];
+                float value, slope;
+                act_pair<decltype(act)::value>(ga[i] * xh + be[i], value, slope);
+                v[i] = r[i] * (ga[i] * (w[i] * slope) - gp[i] - xh * gq[i]);
+            }
+            store_some<VEC>(dxs + p * d.dx_position, v, t.me.first);
+        }
+    });
+}
+
+// dbeta and dgamma: the samples' sums in their order (no samples: zeros).  32 channels a workgroup, eight threads a channel.
+__global__ __launch_bounds__(256) void norm_params_kernel(const float* __restrict__ part, int n, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ float lds[2][8][32];
+    const int ch = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), k = (int)threadIdx.x >> 5;
     float s1 = 0.0f, s2 = 0.0f;
-    for (int i = 0; i < n; ++i) {
-        s1 += part[(size_t)i * c + ch];
-        s2 += part[(size_t)(n + i) * c + ch];
-    }
-    if (dbeta) dbeta[ch] = s1;
-    if (dgamma) dgamma[ch] = s2;
+    if (ch < c)
+        for (int i = k; i < n; i += 8) {
+            s1 += part[(int64_t)i * c + ch];
+            s2 += part[((int64_t)n + i) * c + ch];
+        }
+    lds[0][k][threadIdx.x & 31] = s1;
+    lds[1][k][threadIdx.x & 31] = s2;
+    __syncthreads();
+    if (k > 1 || ch >= c) return;
+    float s = 0.0f;
+    for (int i = 0; i < 8; ++i) s += lds[k][i][threadIdx.x & 31];
+    if (k == 0 && dbeta) dbeta[ch] = s;
+    if (k == 1 && dgamma) dgamma[ch] = s;
 }
 
-// calls f(TX, TY, act) with the descriptor's types
+// calls f(TX, TY) with the descriptor's types
 template <typename F>
 void with_types(const rrm_norm_desc& d, F&& f) {
-    auto act = [&](auto tx, auto ty) {
-        switch (d.act) {
-            case RRM_ACT_RELU: f(tx, ty, std::integral_constant<int, RRM_ACT_RELU>{}); break;
-            case RRM_ACT_SILU: f(tx, ty, std::integral_constant<int, RRM_ACT_SILU>{}); break;
-            case RRM_ACT_GELU: f(tx, ty, std::integral_constant<int, RRM_ACT_GELU>{}); break;
-            default: f(tx, ty, std::integral_constant<int, RRM_ACT_NONE>{}); break;
-        }
-    };
-    auto out = [&](auto tx) { d.y_elem == RRM_F32 ? act(tx, float{}) : act(tx, __bf16{}); };
+    auto out = [&](auto tx) { d.y_elem == RRM_F32 ? f(tx, float{}) : f(tx, __bf16{}); };
     d.x_elem == RRM_F32 ? out(float{}) : out(__bf16{});
 }
 
+struct HeldPlan {
+    HeldGeom g;
+    int vec, which;  // which of the shapes; -1: registers do not hold it
+};
+struct HeldShape {
+    int threads, p;
+};
+constexpr HeldShape FORWARD[] = {{256, 1}, {256, 4}, {512, 8}, {1024, 16}};
+constexpr HeldShape BACKWARD[] = {{256, 1}, {256, 4}, {512, 8}, {1024, 8}};
+
+// The held form's shape: the smallest that holds the sample's positions.  Runs of a position are 64 bytes at least (what memory hands out)
+// where that fits, and more where there are workgroups enough.  It goes by sizes alone: strides and alignment do not change a result's bits.
+HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[4]) {
+    const int cg = d.c / d.groups, esize = d.x_elem == RRM_F32 ? 4 : 2;
+    HeldPlan p{{}, d.c >= wide ? wide : 1, -1};
+    auto fits = [&](int channels) {
+        p.which = -1;
+        int lanes = 1;
+        while (lanes * p.vec < channels) lanes <<= 1;
+        if (channels / cg > HELD_GROUPS) return false;
+        for (int w = 0; w < 4; ++w) {
+            if (lanes > shapes[w].threads || (int64_t)shapes[w].threads / lanes * shapes[w].p < d.positions) continue;
+            p.which = w;
+            p.g = HeldGeom{channels, (d.c + channels - 1) / channels, lanes, 1.0f / (float)cg};
+            return true;
+        }
+        return false;
+    };
+    int cb = cg;
+    while (cb < d.c && (cb * esize < 64 || cb % p.vec) && cb < HELD_GROUPS * cg) cb += cg;
+    // (few samples: narrower runs on more compute units, down to single groups; a vector at least: see Span)
+    while (cb - cg >= p.vec && (!fits(cb) || (int64_t)d.n * p.g.blocks < OP_CUS / 2)) cb -= cg;
+    if (!fits(cb)) return p;
+    while (cb < d.c && (int64_t)d.n * ((d.c + 2 * cb - 1) / (2 * cb)) >= 4 * OP_CUS) {
+        const HeldPlan before = p;
+        if (!fits(2 * cb) || p.which > before.which) return before;
+        cb *= 2;
+    }
+    return p;
+}
+SliceGeom plan_slices(const rrm_norm_desc& d, int vec) {
+    SliceGeom g{};
+    g.lanes = 1;
+    while (g.lanes < SLICE_THREADS && g.lanes * vec < d.c) g.lanes <<= 1;
+    g.blocks = (d.c + g.lanes * vec - 1) / (g.lanes * vec);
+    const int rows = SLICE_THREADS / g.lanes;
+    // some four workgroups a compute unit, of four rows of positions at least
+    int64_t want = 4 * OP_CUS / ((int64_t)d.n * g.blocks) + 1, most = (d.positions + 4 * rows - 1) / (4 * rows);
+    if (want > most) want = most;
+    g.span = (int)((d.positions + want - 1) / want);
+    g.slices = (d.positions + g.span - 1) / g.span;
+    g.r_cg = 1.0f / (float)(d.c / d.groups);
+    return g;
+}
+int wide_of(const rrm_norm_desc& d) { return d.x_elem == RRM_F32 ? 4 : 8; }
+int slice_vec(const rrm_norm_desc& d) { return d.c >= wide_of(d) ? wide_of(d) : 1; }
+bool held(const rrm_norm_desc& d, bool backward) { return plan_held(d, wide_of(d), backward ? BACKWARD : FORWARD).which >= 0; }
+size_t group_bytes(const rrm_norm_desc& d) { return round256((size_t)d.n * d.groups * 8); }
+
+unsigned held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (unsigned)(((d.n + 7) / 8) * 8 * p.g.blocks); }
+
 }  // namespace
 
+// backward, held: [2][n][c]; else the slices' sums and the groups' two values
 size_t norm_scratch(const rrm_norm_desc& d, bool backward) {
-    return backward ? round256((size_t)2 * d.n * d.c * 4) : 0;
+    if (held(d, backward)) return backward ? round256((size_t)2 * d.n * d.c * 4) : 0;
+    return round256((size_t)2 * d.n * plan_slices(d, slice_vec(d)).slices * d.c * 4) + group_bytes(d);
 }
 
 hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float* gamma, const float* beta, void* y, float* stats,
-                             void*, hipStream_t s) {
-    with_types(d, [&](auto tx, auto ty, auto act) {
+                             void* ws, hipStream_t s) {
+    with_types(d, [&](auto tx, auto ty) {
         using TX = decltype(tx);
         using TY = decltype(ty);
-        hipLaunchKernelGGL((norm_kernel<TX, TY, decltype(act)::value>), dim3((unsigned)(d.n * d.groups)), dim3(GN_THREADS), 0, s, d,
-                           (const TX*)x, gamma, beta, (TY*)y, stats);
+        constexpr int WIDE = 16 / sizeof(TX);
+        const HeldPlan p = plan_held(d, WIDE, FORWARD);
+        auto go = [&](auto vec, auto which) {
+            constexpr HeldShape h = FORWARD[decltype(which)::value];
+            hipLaunchKernelGGL((held_kernel<TX, TY, decltype(vec)::value, h.p, h.threads>), dim3(held_grid(d, p)), dim3(h.threads), 0, s, d, p.g,
+                               (const TX*)x, gamma, beta, (TY*)y, stats);
+        };
+        auto by_vec = [&](auto vec) {
+            constexpr int VEC = decltype(vec)::value;
+            switch (p.which) {
+                case 0: go(vec, std::integral_constant<int, 0>{}); break;
+                case 1: go(vec, std::integral_constant<int, 1>{}); break;
+                case 2: go(vec, std::integral_constant<int, 2>{}); break;
+                case 3: go(vec, std::integral_constant<int, 3>{}); break;
+                default: {
+                    const SliceGeom g = plan_slices(d, VEC);
+                    const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
+                    float* st = stats ? stats : (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
+                    hipLaunchKernelGGL((slice_stats_kernel<TX, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, (float*)ws);
+                    hipLaunchKernelGGL(join_stats_kernel, dim3((unsigned)(d.n * d.groups)), dim3(256), 0, s, d, g, (const float*)ws, st);
+                    hipLaunchKernelGGL((slice_apply_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, gamma, beta, st, (TY*)y);
+                }
+            }
+        };
+        p.vec == 1 ? by_vec(std::integral_constant<int, 1>{}) : by_vec(std::integral_constant<int, WIDE>{});
     });
     return hipGetLastError();
 }
@@ -141,19 +654,47 @@ hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float*
 hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, const float* stats, const float* gamma,
                                       const float* beta, const void* dy, void* dx, float* dgamma, float* dbeta, void* ws,
                                       hipStream_t s) {
-    const bool some = d.n > 0 && d.positions > 0;
-    if (some) {
-        with_types(d, [&](auto tx, auto ty, auto act) {
+    int rows = 0;  // of the sums in ws
+    if (d.n > 0 && d.positions > 0)
+        with_types(d, [&](auto tx, auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
-            hipLaunchKernelGGL((norm_back_kernel<TX, TY, decltype(act)::value>), dim3((unsigned)(d.n * d.groups)), dim3(GN_THREADS), 0, s,
-                               d, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, (float*)ws);
+            constexpr int WIDE = 16 / sizeof(TX);
+            const HeldPlan p = plan_held(d, WIDE, BACKWARD);
+            rows = d.n;
+            auto go = [&](auto vec, auto which) {
+                constexpr HeldShape h = BACKWARD[decltype(which)::value];
+                // (bfloat16, 1024 threads: there are no registers for dz in 32 bits)
+                constexpr bool KEEP = sizeof(TX) == 4 || h.threads < 1024;
+                hipLaunchKernelGGL((held_back_kernel<TX, TY, decltype(vec)::value, h.p, h.threads, KEEP>), dim3(held_grid(d, p)), dim3(h.threads),
+                                   0, s, d, p.g, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, (float*)ws);
+            };
+            auto by_vec = [&](auto vec) {
+                constexpr int VEC = decltype(vec)::value;
+                switch (p.which) {
+                    case 0: go(vec, std::integral_constant<int, 0>{}); break;
+                    case 1: go(vec, std::integral_constant<int, 1>{}); break;
+                    case 2: go(vec, std::integral_constant<int, 2>{}); break;
+                    case 3: go(vec, std::integral_constant<int, 3>{}); break;
+                    default: {
+                        const SliceGeom g = plan_slices(d, VEC);
+                        const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
+                        rows = d.n * g.slices;
+                        float* means = (float*)((char*)ws + round256((size_t)2 * rows * d.c * 4));
+                        hipLaunchKernelGGL((slice_sums_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
+                                           (const TY*)dy, (float*)ws);
+                        if (!dx) break;
+                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(256), 0, s, d, g, (const float*)ws, gamma, means);
+                        hipLaunchKernelGGL((slice_dx_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
+                                           (const TY*)dy, means, (TX*)dx);
+                    }
+                }
+            };
+            p.vec == 1 ? by_vec(std::integral_constant<int, 1>{}) : by_vec(std::integral_constant<int, WIDE>{});
         });
-        if (hipError_t e = hipGetLastError()) return e;
-    }
+    if (hipError_t e = hipGetLastError()) return e;
     if (dgamma || dbeta)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 255) / 256)), dim3(256), 0, s, (const float*)ws, some ? d.n : 0,
-                           d.c, dgamma, dbeta);
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(256), 0, s, (const float*)ws, rows, d.c, dgamma, dbeta);
     return hipGetLastError();
 }
 

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "rrm.h"
 
 namespace rrm {
@@ -35,70 +37,77 @@ __device__ __forceinline__ float load_elem(const __bf16* p) { return (float)*p; 
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(__bf16* p, float v) { *p = (__bf16)v; }
 
-// VEC neighbouring elements as float; p lies at a multiple of their size (see the callers' choice of VEC)
-template <int VEC>
-__device__ __forceinline__ void load_vec(const float* p, float (&v)[VEC]) {
-    if constexpr (VEC == 1) {
-        v[0] = *p;
-    } else if constexpr (VEC == 2) {
-        const float2 a = *reinterpret_cast<const float2*>(p);
-        v[0] = a.x, v[1] = a.y;
+// Words from and to memory at the alignment of an element: one instruction, whatever the address (the hardware takes any).
+template <int WORDS>
+struct __attribute__((packed, aligned(2))) LooseWords {
+    typedef unsigned int vec __attribute__((ext_vector_type(WORDS)));
+    vec v;
+};
+template <int WORDS>
+__device__ __forceinline__ void load_words(const void* p, unsigned int (&w)[WORDS]) {
+    if constexpr (WORDS == 1) {
+        struct __attribute__((packed, aligned(2))) One {
+            unsigned int v;
+        };
+        w[0] = reinterpret_cast<const One*>(p)->v;
+    } else if constexpr (WORDS <= 4) {
+        const auto v = reinterpret_cast<const LooseWords<WORDS>*>(p)->v;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = v[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-            const float4 a = *reinterpret_cast<const float4*>(p + i);
-            v[i] = a.x, v[i + 1] = a.y, v[i + 2] = a.z, v[i + 3] = a.w;
+        for (int k = 0; k < WORDS; k += 4) {
+            const auto v = reinterpret_cast<const LooseWords<4>*>(static_cast<const unsigned int*>(p) + k)->v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[k + i] = v[i];
         }
     }
 }
-template <int VEC>
-__device__ __forceinline__ void load_vec(const __bf16* p, float (&v)[VEC]) {
-    if constexpr (VEC == 1) {
-        v[0] = (float)*p;
-    } else if constexpr (VEC == 2) {
-        const unsigned int a = *reinterpret_cast<const unsigned int*>(p);
-        v[0] = bf16_lo(a), v[1] = bf16_hi(a);
-    } else if constexpr (VEC == 4) {
-        const u32x2 a = *reinterpret_cast<const u32x2*>(p);
-        v[0] = bf16_lo(a.x), v[1] = bf16_hi(a.x), v[2] = bf16_lo(a.y), v[3] = bf16_hi(a.y);
-    } else {
+template <int WORDS>
+__device__ __forceinline__ void store_words(void* p, const unsigned int (&w)[WORDS]) {
+    static_assert(WORDS == 2 || WORDS == 4 || WORDS == 8);
+    constexpr int RUN = WORDS < 4 ? WORDS : 4;
 #pragma unroll
-        for (int i = 0; i < VEC; i += 8) {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(p + i);
+    for (int k = 0; k < WORDS; k += RUN) {
+        typename LooseWords<RUN>::vec v;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[i + 2 * k] = bf16_lo(a[k]), v[i + 2 * k + 1] = bf16_hi(a[k]);
-        }
+        for (int i = 0; i < RUN; ++i) v[i] = w[k + i];
+        reinterpret_cast<LooseWords<RUN>*>(static_cast<unsigned int*>(p) + k)->v = v;
     }
 }
-template <int VEC>
-__device__ __forceinline__ void store_vec(float* p, const float (&v)[VEC]) {
+// VEC neighbouring elements as float, and back
+template <int VEC, typename T>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[VEC]) {
     if constexpr (VEC == 1) {
-        *p = v[0];
-    } else if constexpr (VEC == 2) {
-        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+        v[0] = load_elem(p);
     } else {
+        unsigned int w[VEC * sizeof(T) / 4];
+        load_words(p, w);
 #pragma unroll
-        for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        for (int i = 0; i < VEC; ++i)
+            v[i] = sizeof(T) == 4 ? __uint_as_float(w[sizeof(T) == 4 ? i : 0]) : i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
     }
 }
-template <int VEC>
-__device__ __forceinline__ void store_vec(__bf16* p, const float (&v)[VEC]) {
+template <int VEC, typename T>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[VEC]) {
     if constexpr (VEC == 1) {
-        *p = (__bf16)v[0];
-    } else if constexpr (VEC == 2) {
-        *reinterpret_cast<unsigned int*>(p) = bf16_pair(v[0], v[1]);
-    } else if constexpr (VEC == 4) {
-        u32x2 a;
-        a.x = bf16_pair(v[0], v[1]), a.y = bf16_pair(v[2], v[3]);
-        *reinterpret_cast<u32x2*>(p) = a;
+        store_elem(p, v[0]);
+    } else {
+        unsigned int w[VEC * sizeof(T) / 4];
+#pragma unroll
+        for (int i = 0; i < (int)(VEC * sizeof(T) / 4); ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : bf16_pair(v[(2 * i) % VEC], v[(2 * i + 1) % VEC]);
+        store_words(p, w);
+    }
+}
+// those from `first` on
+template <int VEC, typename T>
+__device__ __forceinline__ void store_some(T* p, const float (&v)[VEC], int first) {
+    if (first == 0) {
+        store_vec<VEC>(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 8) {
-            u32x4 a;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) a[k] = bf16_pair(v[i + 2 * k], v[i + 2 * k + 1]);
-            *reinterpret_cast<u32x4*>(p + i) = a;
-        }
+        for (int i = 0; i < VEC; ++i)
+            if (i >= first) store_elem(p + i, v[i]);
     }
 }
 
@@ -158,6 +167,17 @@ __device__ __forceinline__ void act_pair(float z, float& value, float& slope) {
     } else {
         value = z;
         slope = 1.0f;
+    }
+}
+
+// calls f(std::integral_constant<int, act>)
+template <typename F>
+__host__ __device__ __forceinline__ void with_act(int act, F&& f) {
+    switch (act) {
+        case RRM_ACT_RELU: f(std::integral_constant<int, RRM_ACT_RELU>{}); break;
+        case RRM_ACT_SILU: f(std::integral_constant<int, RRM_ACT_SILU>{}); break;
+        case RRM_ACT_GELU: f(std::integral_constant<int, RRM_ACT_GELU>{}); break;
+        default: f(std::integral_constant<int, RRM_ACT_NONE>{}); break;
     }
 }
 
