@@ -18,20 +18,6 @@ struct HeldGeom {
     float r_cg;      // 1 / channels of a group
 };
 
-template <typename T, int VEC>
-struct Held {  // VEC elements as they lie in memory, at the alignment of one
-    static constexpr int WORDS = (VEC * (int)sizeof(T) + 3) / 4;
-    unsigned int w[WORDS];
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (VEC * sizeof(T) == 2) w[0] = *reinterpret_cast<const unsigned short*>(p);
-        else load_words<WORDS>(p, w);
-    }
-    __device__ __forceinline__ float get(int i) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-    }
-};
-
 // A workgroup's place: id -> sample, block; a sample's blocks, whose runs share cache lines, are on one XCD (ids go to the eight in turn)
 __device__ __forceinline__ bool held_place(int id, int n, int blocks, int& sample, int& block) {
     const int k = id >> 3;
@@ -39,19 +25,6 @@ __device__ __forceinline__ bool held_place(int id, int n, int blocks, int& sampl
     sample = (k / blocks) * 8 + (id & 7);
     return sample < n;
 }
-
-// A thread's vector of channels: from `at` on, of which those before `first` are another thread's (the last vector of a workgroup whose channels are
-// no whole vectors begins early, which is never before the row: a workgroup has VEC channels at least, or others before it) and not to be summed or stored.  A thread without channels has first = VEC.
-template <int VEC>
-struct Span {
-    int at, first;
-    __device__ __forceinline__ Span(int slot, int c0, int cb) {
-        const int c = c0 + slot * VEC, end = c0 + cb - VEC;
-        const bool none = slot * VEC >= cb;
-        at = none || c > end ? (end > 0 ? end : 0) : c;
-        first = none ? VEC : c - at;
-    }
-};
 
 // part[row of the workgroup][channel] -> sums over the rows of a wavefront's threads of equal channels are in `v` of its first lanes; here they
 // go to LDS, one row a wavefront (or a set of wavefronts that span the channels)

@@ -111,6 +111,33 @@ __device__ __forceinline__ void store_some(T* p, const float (&v)[VEC], int firs
     }
 }
 
+template <typename T, int VEC>
+struct Held {  // VEC elements as they lie in memory, at the alignment of one
+    static constexpr int WORDS = (VEC * (int)sizeof(T) + 3) / 4;
+    unsigned int w[WORDS];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (VEC * sizeof(T) == 2) w[0] = *reinterpret_cast<const unsigned short*>(p);
+        else load_words<WORDS>(p, w);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+    }
+};
+
+// A thread's vector of channels: from `at` on, of which those before `first` are another thread's (the last vector of a workgroup whose channels are
+// no whole vectors begins early, which is never before the row: a workgroup has VEC channels at least, or others before it) and not to be summed or stored.  A thread without channels has first = VEC.
+template <int VEC>
+struct Span {
+    int at, first;
+    __device__ __forceinline__ Span(int slot, int c0, int cb) {
+        const int c = c0 + slot * VEC, end = c0 + cb - VEC;
+        const bool none = slot * VEC >= cb;
+        at = none || c > end ? (end > 0 ? end : 0) : c;
+        first = none ? VEC : c - at;
+    }
+};
+
 // exp2 and 1/x of one instruction each (1 ulp): the gates' and activations' exponentials.  Arguments below -126 give 0.
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
 __device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
