@@ -14,9 +14,9 @@ namespace rrm {
 namespace {
 
 constexpr int GS_THREADS = 256;
-constexpr int GS_BLOCK = 128;  // frames of a block
+constexpr int GS_BLOCK = 128;  // frames of a block; the chunks of the time axis are whole blocks
 constexpr int MARK = RRM_SCAN_MARK_FRAMES;
-static_assert(GS_BLOCK % MARK == 0, "blocks begin at marks");
+static_assert(GS_BLOCK % MARK == 0, "chunks begin at marks");
 
 __device__ __forceinline__ int video_frames(const int32_t* lengths, int i, int t) {
     if (!lengths) return t;
@@ -26,10 +26,10 @@ __device__ __forceinline__ int video_frames(const int32_t* lengths, int i, int t
 // LDS accesses done, then the barrier; loads from memory stay on their way
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Shape of a tile: VEC features a thread, LANES threads of a frame, ROWS of SPAN frames
-template <int VEC>
+// Shape of a tile: VEC features a thread, eight threads of a frame (runs of 128 bytes), 32 rows of FRAMES / 32 frames
+template <int VEC, int FRAMES = GS_BLOCK>
 struct Tile {
-    static constexpr int LANES = VEC == 8 ? 8 : VEC == 4 ? 16 : 8, ROWS = GS_THREADS / LANES, SPAN = GS_BLOCK / ROWS, WIDTH = LANES * VEC;
+    static constexpr int LANES = 8, ROWS = GS_THREADS / LANES, SPAN = FRAMES / ROWS, WIDTH = LANES * VEC;
 };
 
 // where the time axis is cut: workgroups of a video's tile, each a number of blocks
@@ -38,8 +38,8 @@ struct Cut {
 };
 struct Place {
     int video, tile, chunk;
-    __device__ __forceinline__ explicit Place(const Cut& c) {
-        const unsigned id = blockIdx.x, per = (unsigned)(c.tiles * c.chunks);
+    __device__ __forceinline__ Place(const Cut& c, int chunks) {
+        const unsigned id = blockIdx.x, per = (unsigned)(c.tiles * chunks);
         video = (int)(id / per);
         const unsigned k = id - (unsigned)video * per;
         chunk = (int)(k / (unsigned)c.tiles);
@@ -67,7 +67,8 @@ __global__ __launch_bounds__(GS_THREADS) void chunk_maps_kernel(rrm_scan_desc d,
                                                                 const int32_t* __restrict__ lengths, float* __restrict__ maps) {
     using Z = Tile<VEC>;
     __shared__ float sa[Z::ROWS * Z::WIDTH], sb[Z::ROWS * Z::WIDTH];
-    const Place w(cut);
+    Place w(cut, cut.chunks - 1);  // (forward nobody asks for the last chunk's map, backward for the first's)
+    if (BACK) ++w.chunk;
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
     const int end = video_frames(lengths, w.video, d.t);
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
     using Z = Tile<VEC>;
     constexpr int S = Z::SPAN;
     __shared__ float sa[2][Z::ROWS * Z::WIDTH], sb[2][Z::ROWS * Z::WIDTH];
-    const Place w(cut);
+    const Place w(cut, cut.chunks);
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
     const int end = video_frames(lengths, w.video, d.t);
@@ -208,15 +209,17 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
     }
 }
 
+constexpr int BACK_BLOCK = 64;  // frames of a block of the backward pass: it holds four values a frame
+
 template <typename T, int VEC>
 __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, Cut cut, const T* __restrict__ x, const T* __restrict__ f,
                                                                const float* __restrict__ marks, const int32_t* __restrict__ lengths,
                                                                const T* __restrict__ dy, const float* dh_last, const float* __restrict__ maps,
                                                                T* __restrict__ dx, T* __restrict__ df, float* dh0) {
-    using Z = Tile<VEC>;
-    constexpr int S = Z::SPAN, MARKS = GS_BLOCK / MARK, MROWS = Z::ROWS / MARKS;
+    using Z = Tile<VEC, BACK_BLOCK>;
+    constexpr int S = Z::SPAN, MARKS = BACK_BLOCK / MARK, MROWS = Z::ROWS / MARKS;
     __shared__ float sa[Z::ROWS * Z::WIDTH], sb[Z::ROWS * Z::WIDTH], sg[Z::ROWS * Z::WIDTH];
-    const Place w(cut);
+    const Place w(cut, cut.chunks);
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
     const int end = video_frames(lengths, w.video, d.t);
@@ -227,12 +230,12 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
     T* dxp = dx + w.video * d.dx_video + me.at;
     T* dfp = df + w.video * d.df_video + me.at;
     const int nm = (d.t + MARK - 1) / MARK;
-    const int blocks = live > t0 ? (live - t0 + GS_BLOCK - 1) / GS_BLOCK : 0;
+    const int blocks = live > t0 ? (live - t0 + BACK_BLOCK - 1) / BACK_BLOCK : 0;
     if (me.first < VEC) {  // behind the video's end
         float zero[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) zero[i] = 0.0f;
-        for (int t = t0 + blocks * GS_BLOCK + row; t < t1; t += Z::ROWS) {
+        for (int t = t0 + blocks * BACK_BLOCK + row; t < t1; t += Z::ROWS) {
             store_some<VEC>(dxp + t * d.dx_frame, zero, me.first);
             store_some<VEC>(dfp + t * d.df_frame, zero, me.first);
         }
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
             ry[k].load(yp + t * d.y_frame);
         }
     };
-    if (blocks) fetch(t0 + (blocks - 1) * GS_BLOCK);
+    if (blocks) fetch(t0 + (blocks - 1) * BACK_BLOCK);
     float carry = 0.0f;  // thread j: the gradient of the state behind the block, of feature c0 + j
     if (j < width) {
         carry = dh_last ? dh_last[(int64_t)w.video * d.c + c0 + j] : 0.0f;
@@ -256,7 +259,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
         for (int q = cut.chunks - 1; q > w.chunk; --q) carry = m[(int64_t)q * 2 * d.c] * carry + m[((int64_t)q * 2 + 1) * d.c];
     }
     for (int blk = blocks - 1; blk >= 0; --blk) {
-        const int tb = t0 + blk * GS_BLOCK;
+        const int tb = t0 + blk * BACK_BLOCK;
         float a[S][VEC], o[S][VEC], v[S][VEC], g[S][VEC], A[VEC], B[VEC], G[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) A[i] = 1.0f, B[i] = 0.0f, G[i] = 0.0f;
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
                 B[i] = a[k][i] * B[i] + o[k][i] * v[k][i];
             }
         }
-        if (blk > 0) fetch(tb - GS_BLOCK);
+        if (blk > 0) fetch(tb - BACK_BLOCK);
         lds_barrier();  // (the rows have been handed their states of the block before)
         put<VEC, Z::WIDTH>(sa + row * Z::WIDTH, me.at - c0, me.first, A);
         put<VEC, Z::WIDTH>(sb + row * Z::WIDTH, me.at - c0, me.first, B);
@@ -424,7 +427,7 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
         const Cut c = cut_of(d);
         const dim3 grid((unsigned)((int64_t)d.n * c.tiles * c.chunks));
         if (c.chunks > 1)
-            hipLaunchKernelGGL((chunk_maps_kernel<T, VEC, false>), grid, dim3(GS_THREADS), 0, s, d, c, (const T*)x, (const T*)f, lengths, (float*)ws);
+            hipLaunchKernelGGL((chunk_maps_kernel<T, VEC, false>), dim3((unsigned)((int64_t)d.n * c.tiles * (c.chunks - 1))), dim3(GS_THREADS), 0, s, d, c, (const T*)x, (const T*)f, lengths, (float*)ws);
         hipLaunchKernelGGL((scan_kernel<T, VEC>), grid, dim3(GS_THREADS), 0, s, d, c, (const T*)x, (const T*)f, h0, lengths, (const float*)ws,
                            (T*)y, h_last, marks);
     });
@@ -445,7 +448,7 @@ hipError_t launch_gated_scan_backward(const rrm_scan_desc& d, const void* x, con
         const Cut c = cut_of(d);
         const dim3 grid((unsigned)((int64_t)d.n * c.tiles * c.chunks));
         if (c.chunks > 1)
-            hipLaunchKernelGGL((chunk_maps_kernel<T, VEC, true>), grid, dim3(GS_THREADS), 0, s, d, c, (const T*)dy, (const T*)f, lengths, (float*)ws);
+            hipLaunchKernelGGL((chunk_maps_kernel<T, VEC, true>), dim3((unsigned)((int64_t)d.n * c.tiles * (c.chunks - 1))), dim3(GS_THREADS), 0, s, d, c, (const T*)dy, (const T*)f, lengths, (float*)ws);
         hipLaunchKernelGGL((scan_back_kernel<T, VEC>), grid, dim3(GS_THREADS), 0, s, d, c, (const T*)x, (const T*)f, marks, lengths,
                            (const T*)dy, dh_last, (const float*)ws, (T*)dx, (T*)df, dh0);
     });
