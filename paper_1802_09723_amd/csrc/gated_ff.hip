@@ -78,7 +78,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
     constexpr int NP = PB / (THREADS * 16), NQ = QB / (THREADS * 16);          // 16-byte chunks a thread stages
     constexpr int OUT_COLS = KIND == GATED ? BN / 2 : BN;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[STAGES * (PB + QB)];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = wave % WM, wn = wave / WM;
 
     // tiles XCD by XCD (workgroups go to the eight in turn), and there in blocks of eight rows of tiles
@@ -161,26 +161,37 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
         }
     };
     const src_t zeros = reinterpret_cast<src_t>(&g_zeros);
-    auto stage = [&](int s, int buf) __attribute__((always_inline)) {  // starts the copies of step s
+    // The copies of a step are started in three parts, between products, so that these do not queue behind all of them
+    auto begin = [&](int s) __attribute__((always_inline)) {  // step s is next
         const int pair = KIND == PLAIN && s >= steps_of ? 1 : 0;
+        if (KIND == PLAIN && s == steps_of) point(s);
         const int rem = a.len - (s - pair * steps_of) * STEP;
-        unsigned char* dp = lds + buf * (PB + QB);
-        unsigned char* dq = dp + PB;
+        if (rem < STEP) {  // the summed axis ends in it
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
-            __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || pk[i] < rem ? pp[i] : zeros), (lptr_t)(dp + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+            for (int i = 0; i < NP; ++i) pp[i] = pk[i] < rem ? pp[i] : zeros;
 #pragma unroll
-        for (int i = 0; i < NQ; ++i)
-            __builtin_amdgcn_global_load_lds((gptr_t)(rem >= STEP || qk[i] < rem ? qp[i] : zeros), (lptr_t)(dq + (i * THREADS + wave * 64) * 16), 16, 0, 0);
-        if (KIND == PLAIN && s + 1 == steps_of && s + 1 < s1) {
-            point(s + 1);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NP; ++i) pp[i] += p_step;
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) qp[i] += q_step;
+            for (int i = 0; i < NQ; ++i) qp[i] = qk[i] < rem ? qp[i] : zeros;
         }
     };
+    auto part = [&](auto which, unsigned char* dp) __attribute__((always_inline)) {
+        constexpr int W = decltype(which)::value, PARTS = STAGES == 2 ? 2 : 3;
+        constexpr int FROM = (NP + NQ) * (W < PARTS ? W : PARTS) / PARTS, TO = (NP + NQ) * (W + 1 < PARTS ? W + 1 : PARTS) / PARTS;
+#pragma unroll
+        for (int i = FROM; i < TO; ++i)
+            if (i < NP)
+                __builtin_amdgcn_global_load_lds((gptr_t)pp[i < NP ? i : 0], (lptr_t)(dp + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+            else
+                __builtin_amdgcn_global_load_lds((gptr_t)qp[i < NP ? 0 : i - NP], (lptr_t)(dp + PB + ((i - NP) * THREADS + wave * 64) * 16), 16, 0, 0);
+    };
+    auto end = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) pp[i] += p_step;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) qp[i] += q_step;
+    };
+    const std::integral_constant<int, 0> one;
+    const std::integral_constant<int, 1> two;
+    const std::integral_constant<int, 2> three;
 
     v16f acc[MT][NT];
 #pragma unroll
@@ -218,8 +229,8 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
     // Fragments of 16 of the summed axis are read while those before are multiplied, across steps as well: the barrier that publishes
     // the next step stands before the last products of this one.
     v8bf fp[2][MT], fq[2][NT];
-    auto fragments = [&](int set, int place, int ks) __attribute__((always_inline)) {
-        const unsigned char* tp = lds + place * (PB + QB);
+    auto place = [&](int i) { return lds + i * (PB + QB); };
+    auto fragments = [&](int set, const unsigned char* tp, int ks) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) fq[set][j] = frag(tp + PB, (wn * NT + j) * 32, ks, q_turned, q_rows);
 #pragma unroll
@@ -237,43 +248,69 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);  // (reads of the next group would be waited for with those of this one)
     };
     if (s0 < s1) {
         point(s0);
 #pragma unroll
         for (int i = 0; i < STAGES; ++i)
-            if (s0 + i < s1) stage(s0 + i, i);
+            if (s0 + i < s1) {
+                begin(s0 + i);
+                part(one, place(i));
+                part(two, place(i));
+                part(three, place(i));
+                end();
+            }
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        fragments(0, 0, 0);
-    }
-    int buf = 0;  // place of the step at hand
-    auto first_three = [&]() __attribute__((always_inline)) {
-        fragments(1, buf, 1);
+        fragments(0, lds, 0);
+        fragments(1, lds, 1);
         products(0);
-        fragments(0, buf, 2);
+        fragments(0, lds, 2);
         products(1);
-        fragments(1, buf, 3);
+        fragments(1, lds, 3);
         products(0);
-    };
-    for (int s = s0; s + 1 < s1; ++s) {
-        const int after = buf + 1 == STAGES ? 0 : buf + 1;
-        first_three();
-        // this wavefront's copies of the next step have landed (those of later steps may still be on their way), and its reads
-        // of this one are done ..
-        if (STAGES > 2 && s + STAGES <= s1) {
+        // From here on a turn takes the last quarter of step s and three of the next one.  `from` and `to` never overlap, which the compiler
+        // has to know: it would wait for the copies to `to` before each transposing read of `from`.
+        auto turn = [&](const unsigned char* __restrict from, unsigned char* __restrict to) __attribute__((always_inline)) {
+            part(one, to);
+            fragments(0, from, 0);
+            products(1);
+            part(two, to);
+            fragments(1, from, 1);
+            products(0);
+            part(three, to);
+            fragments(0, from, 2);
+            products(1);
+            fragments(1, from, 3);
+            products(0);
+        };
+        int s = s0, buf = 0;  // place of step s
+        for (; s + STAGES < s1; ++s) {
+            const int after = buf + 1 == STAGES ? 0 : buf + 1;
+            // this wavefront's copies of the next step have landed (those of later steps may still be on their way), and its reads
+            // of this one are done ..
             wait_copies<(STAGES - 2) * (NP + NQ)>();
-        } else {
-            wait_copies<0>();
+            barrier();  // .. and so are everybody's
+            begin(s + STAGES);
+            turn(place(after), place(buf));
+            end();
+            buf = after;
         }
-        barrier();  // .. and so are everybody's
-        if (s + STAGES < s1) stage(s + STAGES, buf);
-        fragments(0, after, 0);
-        products(1);
-        buf = after;
-    }
-    if (s0 < s1) {
-        first_three();
+        for (; s + 1 < s1; ++s) {  // nothing left to be copied
+            const int after = buf + 1 == STAGES ? 0 : buf + 1;
+            wait_copies<0>();
+            barrier();
+            fragments(0, place(after), 0);
+            products(1);
+            fragments(1, place(after), 1);
+            products(0);
+            fragments(0, place(after), 2);
+            products(1);
+            fragments(1, place(after), 3);
+            products(0);
+            buf = after;
+        }
         products(1);
     }
 
