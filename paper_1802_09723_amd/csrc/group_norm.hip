@@ -330,36 +330,52 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_stats_kernel(rrm_norm_des
         if (i >= t.me.first) to[i] = mean[i], to[d.c + i] = s[0][i];
 }
 
-__device__ __forceinline__ float sum_256(float v, float* lds) {
+constexpr int JOIN_THREADS = 512;
+__device__ __forceinline__ float sum_all(float v, float* lds) {
 #pragma unroll
     for (int m = 1; m < OP_WAVE; m <<= 1) v += __shfl_xor(v, m);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < JOIN_THREADS / OP_WAVE; ++i) s += lds[i];
+    return s;
 }
+// a group's channels over a workgroup's threads: `lanes` of them (a power of two), rows of slices behind
+struct JoinShape {
+    int lane, row, lanes, rows;
+    __device__ __forceinline__ explicit JoinShape(int cg) {
+        lanes = 1;
+        while (lanes < cg && lanes < JOIN_THREADS) lanes <<= 1;
+        rows = JOIN_THREADS / lanes;
+        lane = (int)threadIdx.x & (lanes - 1);
+        row = (int)threadIdx.x / lanes;
+    }
+};
 
 // One workgroup a group of a sample: the slices' and channels' means and squares become the group's
-__global__ __launch_bounds__(256) void join_stats_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, float* __restrict__ stats) {
-    __shared__ float lds[4];
+__global__ __launch_bounds__(JOIN_THREADS) void join_stats_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, float* __restrict__ stats) {
+    __shared__ float lds[JOIN_THREADS / OP_WAVE];
     const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
     const float* from = part + (int64_t)sample * g.slices * 2 * d.c + group * cg;
-    const int64_t all = (int64_t)g.slices * cg;
+    const JoinShape j(cg);
     const float per = 1.0f / ((float)d.positions * (float)cg);
+    const float whole = (float)g.span, last = (float)(d.positions - (g.slices - 1) * g.span);
     float m = 0.0f;
-    for (int64_t k = threadIdx.x; k < all; k += 256) {
-        const int slice = (int)(k / cg), p0 = slice * g.span;
-        m += from[(int64_t)slice * 2 * d.c + k % cg] * (float)(min(p0 + g.span, d.positions) - p0);
-    }
-    const float mean = sum_256(m, lds) * per;
+    for (int c = j.lane; c < cg; c += j.lanes)
+#pragma unroll 4
+        for (int k = j.row; k < g.slices; k += j.rows) m += from[(int64_t)k * 2 * d.c + c] * (k + 1 < g.slices ? whole : last);
+    const float mean = sum_all(m, lds) * per;
     float q = 0.0f;
-    for (int64_t k = threadIdx.x; k < all; k += 256) {
-        const int slice = (int)(k / cg), p0 = slice * g.span;
-        const float* e = from + (int64_t)slice * 2 * d.c + k % cg;
-        const float off = e[0] - mean;
-        q += e[d.c] + off * off * (float)(min(p0 + g.span, d.positions) - p0);
-    }
-    const float r = 1.0f / sqrtf(sum_256(q, lds) * per + d.eps);
+    for (int c = j.lane; c < cg; c += j.lanes)
+#pragma unroll 4
+        for (int k = j.row; k < g.slices; k += j.rows) {
+            const float* e = from + (int64_t)k * 2 * d.c + c;
+            const float off = e[0] - mean;
+            q += e[d.c] + off * off * (k + 1 < g.slices ? whole : last);
+        }
+    const float r = 1.0f / sqrtf(sum_all(q, lds) * per + d.eps);
     if (threadIdx.x == 0) stats[2 * (int64_t)blockIdx.x] = mean, stats[2 * (int64_t)blockIdx.x + 1] = r;
 }
 
@@ -391,7 +407,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_apply_kernel(rrm_norm_des
     });
 }
 
-// part: [2][n * slices][c], the slices' sums of dz and dz * xh (the layout that norm_params_kernel sums)
+// part: [2][n * slices][c], the slices' sums of dz and dz * xh
 template <typename TX, typename TY, int VEC>
 __global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc d, SliceGeom g, const TX* __restrict__ x, const float* __restrict__ stats,
                                                                    const float* __restrict__ gamma, const float* __restrict__ beta,
@@ -435,23 +451,42 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc
         if (i >= t.me.first) part[k * d.c + t.me.at + i] = s[0][i], part[(rows + k) * d.c + t.me.at + i] = s[1][i];
 }
 
-// One workgroup a group of a sample: means of gamma dz and of gamma dz xh, [n][groups][2]
-__global__ __launch_bounds__(256) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, const float* __restrict__ gamma,
-                                                        float* __restrict__ means) {
-    __shared__ float lds[4];
+// One workgroup a group of a sample: the slices' sums of each channel, [2][n][c], and the group's means of gamma dz and of gamma dz xh, [n][groups][2]
+__global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, const float* __restrict__ gamma,
+                                                                 float* __restrict__ sums, float* __restrict__ means) {
+    __shared__ float lds[JOIN_THREADS / OP_WAVE], rows[2][JOIN_THREADS];
     const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
-    const int64_t rows = (int64_t)d.n * g.slices, all = (int64_t)g.slices * cg;
+    const JoinShape j(cg);
+    const int64_t all = (int64_t)d.n * g.slices;
     float p = 0.0f, q = 0.0f;
-    for (int64_t k = threadIdx.x; k < all; k += 256) {
-        const int c = group * cg + (int)(k % cg);
-        const int64_t row = (int64_t)sample * g.slices + k / cg;
-        const float ga = gamma ? gamma[c] : 1.0f;
-        p += ga * part[row * d.c + c];
-        q += ga * part[(rows + row) * d.c + c];
+    for (int c0 = 0; c0 < cg; c0 += j.lanes) {
+        const int c = group * cg + c0 + j.lane;
+        const bool in = c0 + j.lane < cg;
+        float s1 = 0.0f, s2 = 0.0f;
+        if (in)
+#pragma unroll 4
+            for (int k = j.row; k < g.slices; k += j.rows) {
+                const int64_t row = (int64_t)sample * g.slices + k;
+                s1 += part[row * d.c + c];
+                s2 += part[(all + row) * d.c + c];
+            }
+        __syncthreads();
+        rows[0][threadIdx.x] = s1;
+        rows[1][threadIdx.x] = s2;
+        __syncthreads();
+        if (j.row == 0 && in) {
+            s1 = s2 = 0.0f;
+            for (int k = 0; k < j.rows; ++k) s1 += rows[0][k * j.lanes + j.lane], s2 += rows[1][k * j.lanes + j.lane];
+            sums[(int64_t)sample * d.c + c] = s1;
+            sums[((int64_t)d.n + sample) * d.c + c] = s2;
+            const float ga = gamma ? gamma[c] : 1.0f;
+            p += ga * s1;
+            q += ga * s2;
+        }
     }
     const float per = 1.0f / ((float)d.positions * (float)cg);
-    p = sum_256(p, lds) * per;
-    q = sum_256(q, lds) * per;
+    p = sum_all(p, lds) * per;
+    q = sum_all(q, lds) * per;
     if (threadIdx.x == 0) means[2 * (int64_t)blockIdx.x] = p, means[2 * (int64_t)blockIdx.x + 1] = q;
 }
 
@@ -494,13 +529,14 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_dx_kernel(rrm_norm_desc d
     });
 }
 
-// dbeta and dgamma: the samples' sums in their order (no samples: zeros).  32 channels a workgroup, eight threads a channel.
-__global__ __launch_bounds__(256) void norm_params_kernel(const float* __restrict__ part, int n, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ float lds[2][8][32];
+// dbeta and dgamma: the samples' sums (no samples: zeros).  32 channels a workgroup, 32 threads a channel, joined in their order.
+__global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restrict__ part, int n, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ float lds[2][32][32];
     const int ch = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), k = (int)threadIdx.x >> 5;
     float s1 = 0.0f, s2 = 0.0f;
     if (ch < c)
-        for (int i = k; i < n; i += 8) {
+#pragma unroll 4
+        for (int i = k; i < n; i += 32) {
             s1 += part[(int64_t)i * c + ch];
             s2 += part[((int64_t)n + i) * c + ch];
         }
@@ -509,7 +545,8 @@ __global__ __launch_bounds__(256) void norm_params_kernel(const float* __restric
     __syncthreads();
     if (k > 1 || ch >= c) return;
     float s = 0.0f;
-    for (int i = 0; i < 8; ++i) s += lds[k][i][threadIdx.x & 31];
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) s += lds[k][i][threadIdx.x & 31];
     if (k == 0 && dbeta) dbeta[ch] = s;
     if (k == 1 && dgamma) dgamma[ch] = s;
 }
@@ -551,9 +588,20 @@ HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[4
     };
     int cb = cg;
     while (cb < d.c && (cb * esize < 64 || cb % p.vec) && cb < HELD_GROUPS * cg) cb += cg;
-    // (few samples: narrower runs on more compute units, down to single groups; a vector at least: see Span)
-    while (cb - cg >= p.vec && (!fits(cb) || (int64_t)d.n * p.g.blocks < OP_CUS / 2)) cb -= cg;
+    // (few samples: narrower runs on more compute units, by whole vectors as far as that goes, then down to single groups; a vector at
+    // least: see Span)
+    int whole = cg;
+    while (whole % p.vec) whole += cg;
+    for (int next = cb; next >= p.vec && next > 0; next = cb - (cb - whole >= whole ? whole : cg)) {
+        cb = next;
+        if (fits(cb) && (int64_t)d.n * p.g.blocks >= OP_CUS) break;
+    }
     if (!fits(cb)) return p;
+    // a few workgroups of the largest shape take longer than slices on all compute units (8 x 14 x 14 x 512 in one group, bf16: 33 and 16 us)
+    if (p.which == 3 && (int64_t)d.n * p.g.blocks < OP_CUS / 2) {
+        p.which = -1;
+        return p;
+    }
     while (cb < d.c && (int64_t)d.n * ((d.c + 2 * cb - 1) / (2 * cb)) >= 4 * OP_CUS) {
         const HeldPlan before = p;
         if (!fits(2 * cb) || p.which > before.which) return before;
@@ -584,10 +632,10 @@ unsigned held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (unsigned
 
 }  // namespace
 
-// backward, held: [2][n][c]; else the slices' sums and the groups' two values
+// backward, held: the samples' sums [2][n][c]; else the slices' sums, (backward) the samples' and the groups' two values
 size_t norm_scratch(const rrm_norm_desc& d, bool backward) {
     if (held(d, backward)) return backward ? round256((size_t)2 * d.n * d.c * 4) : 0;
-    return round256((size_t)2 * d.n * plan_slices(d, slice_vec(d)).slices * d.c * 4) + group_bytes(d);
+    return round256((size_t)2 * d.n * plan_slices(d, slice_vec(d)).slices * d.c * 4) + (backward ? round256((size_t)2 * d.n * d.c * 4) : 0) + group_bytes(d);
 }
 
 hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float* gamma, const float* beta, void* y, float* stats,
@@ -614,7 +662,7 @@ hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float*
                     const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
                     float* st = stats ? stats : (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
                     hipLaunchKernelGGL((slice_stats_kernel<TX, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, (float*)ws);
-                    hipLaunchKernelGGL(join_stats_kernel, dim3((unsigned)(d.n * d.groups)), dim3(256), 0, s, d, g, (const float*)ws, st);
+                    hipLaunchKernelGGL(join_stats_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, st);
                     hipLaunchKernelGGL((slice_apply_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, gamma, beta, st, (TY*)y);
                 }
             }
@@ -627,14 +675,14 @@ hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float*
 hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, const float* stats, const float* gamma,
                                       const float* beta, const void* dy, void* dx, float* dgamma, float* dbeta, void* ws,
                                       hipStream_t s) {
-    int rows = 0;  // of the sums in ws
-    if (d.n > 0 && d.positions > 0)
+    const bool some = d.n > 0 && d.positions > 0;
+    const float* sums = (const float*)ws;  // [2][n][c]
+    if (some)
         with_types(d, [&](auto tx, auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
             constexpr int WIDE = 16 / sizeof(TX);
             const HeldPlan p = plan_held(d, WIDE, BACKWARD);
-            rows = d.n;
             auto go = [&](auto vec, auto which) {
                 constexpr HeldShape h = BACKWARD[decltype(which)::value];
                 // (bfloat16, 1024 threads: there are no registers for dz in 32 bits)
@@ -652,12 +700,14 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                     default: {
                         const SliceGeom g = plan_slices(d, VEC);
                         const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
-                        rows = d.n * g.slices;
-                        float* means = (float*)((char*)ws + round256((size_t)2 * rows * d.c * 4));
+                        float* to = (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
+                        float* means = (float*)((char*)to + round256((size_t)2 * d.n * d.c * 4));
+                        sums = to;
                         hipLaunchKernelGGL((slice_sums_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, (float*)ws);
+                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, gamma, to,
+                                           means);
                         if (!dx) break;
-                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(256), 0, s, d, g, (const float*)ws, gamma, means);
                         hipLaunchKernelGGL((slice_dx_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, means, (TX*)dx);
                     }
@@ -667,7 +717,7 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
         });
     if (hipError_t e = hipGetLastError()) return e;
     if (dgamma || dbeta)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(256), 0, s, (const float*)ws, rows, d.c, dgamma, dbeta);
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, s, sums, some ? d.n : 0, d.c, dgamma, dbeta);
     return hipGetLastError();
 }
 
