@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
 )
 from .operators import (  # noqa: F401
     gated_ff, gated_ff_backward, gated_scan, gated_scan_backward, gated_scan_marks, group_norm_act, group_norm_act_backward,
+    group_norm_act_of,
 )

@@ -14,7 +14,7 @@ import ctypes
 
 import torch
 
-from .binding import _check, _stream_ptr, lib
+from .binding import BF16, CONV, _check, _stream_ptr, lib
 
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 MARK_FRAMES = 64  # RRM_SCAN_MARK_FRAMES
@@ -170,6 +170,32 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
                                    *_outer_inner(out, "out"), 0, 0), "rrm_group_norm_workspace", 0)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act(plan[1], x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
+                                    _stream_ptr(stream)))
+    if stream is not None:
+        _used_on(stream, ws, out if made else None)
+    return out
+
+
+def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "none", eps: float = 1e-5, out=None, stats=None, stream=None):
+    """group_norm_act of a bfloat16 convolution's stored projection (``rrm_snapshot``), read where it lies: after ``layer.step`` on the same
+    stream, the next layer's input, bfloat16 [n, h_out, w_out, c_out]."""
+    if layer.dtype != BF16 or layer.shape.kind != CONV:
+        raise ValueError("layer: expected a bfloat16 convolution")
+    n, h, w, c = layer.y_shape
+    made = out is None
+    if made:
+        out = torch.empty((n, h, w, c), dtype=torch.bfloat16, device="cuda")
+    key = ("norm of", groups, act, eps, n, h, w, c, made or _look(out), _look(gamma), _look(beta), _look(stats))
+    plan = _plans.get(key)
+    if plan is None:
+        _expect(out, "out", (n, h, w, c), torch.bfloat16)
+        _dense(gamma, "gamma", (c,), torch.float32)
+        _dense(beta, "beta", (c,), torch.float32)
+        _dense(stats, "stats", (n, groups, 2), torch.float32)
+        plan = _keep(key, NormDesc(n, h * w, c, int(groups), 0, 1, _act(act), float(eps), h * w * c, c, *_outer_inner(out, "out"), 0, 0),
+                     "rrm_group_norm_workspace", 0)
+    ws = _workspace(plan[2], out.device)
+    _check(lib().rrm_group_norm_act(plan[1], layer.snapshot_ptrs()[1], _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
                                     _stream_ptr(stream)))
     if stream is not None:
         _used_on(stream, ws, out if made else None)

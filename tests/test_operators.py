@@ -587,6 +587,98 @@ def test_operators_on_a_stream_of_their_own_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@gpu
+def test_the_example_runs_them_together():
+    """The live path against plain torch in 64 bits on the same parameters and frames; training brings the loss down."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "video_head.py")
+    spec = importlib.util.spec_from_file_location("video_head", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    losses, logits, labels = ex.main()
+    assert losses[-1] < 0.5 * losses[0] and torch.isfinite(logits).all()
+    net = ex.Net(seed=3)
+    frames = ex.synthetic_clip(net, 6, seed=4)
+    got = [net.serve(fr).cpu().double() for fr in frames]
+
+    def b(v):  # the roundings between the steps
+        return v.float().bfloat16().double()
+
+    def conv(x, w, stride):
+        return torch.nn.functional.conv2d(x.permute(0, 3, 1, 2), b(w).permute(0, 3, 1, 2), stride=stride, padding=1).permute(0, 2, 3, 1)
+
+    h = torch.zeros(net.n, 64, dtype=torch.float64)
+    for fr, lg in zip(frames, got):
+        a = b(norm64(conv(fr.cpu().double(), net.w1, 1), 8, torch.ones(32).double(), torch.zeros(32).double(), "silu")[0])
+        a = b(norm64(conv(a, net.w2, 2), 8, torch.ones(64).double(), torch.zeros(64).double(), "silu")[0])
+        feat = b(a.mean((1, 2)))
+        gate = torch.sigmoid(b(feat @ net.gate.cpu().double().t()))
+        h = gate * h + (1 - gate) * feat
+        y = b(h)
+        z = b(act64("silu", y @ net.wg.cpu().double().t()) * (y @ net.wu.cpu().double().t()))
+        want = z @ net.out.cpu().double().t()
+        # six roundings to bfloat16 stand between a frame and its logits, each off by 2^-8 of what it rounds at the most; a value
+        # that another precision's sum rounds the other way moves by twice that, and the sums behind average it
+        assert float((lg - want).abs().max()) <= 12 * V * float(want.abs().max()), float((lg - want).abs().max() / want.abs().max())
+
+
+@gpu
+def test_norm_of_a_layers_stored_projection():
+    """Read in place after a delta step; the same as of a copy; other layers are refused."""
+    import rrm_synth as S
+    w = S.f32_to_bf16_bits(np.random.default_rng(0).normal(size=(40, 3, 3, 16)).astype(np.float32) * 0.1)
+    layer = rrm.Layer(S.conv_shape(9, 11, 16, 40, 3, 1, 1, n=2), rrm.BF16, w)
+    x = torch.randn(2, 9, 11, 16, generator=gen(1)).bfloat16().cuda()
+    for k in range(2):
+        x[:, k:k + 3, 2:5] += 1
+        layer.step(x)
+        stats = torch.empty(2, 5, 2, device="cuda")
+        got = rrm.group_norm_act_of(layer, 5, act="relu", stats=stats)
+        want = rrm.group_norm_act(layer.y_snapshot(), 5, act="relu", out_dtype=torch.bfloat16)
+        assert torch.equal(got, want) and torch.isfinite(stats).all()
+    layer.destroy()
+    other = rrm.Layer(S.fc_shape(16, 8), rrm.BF16, S.f32_to_bf16_bits(np.ones((8, 16), np.float32)))
+    with pytest.raises(ValueError, match="convolution"):
+        rrm.group_norm_act_of(other, 2)
+    other.destroy()
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """Two videos, samples or rows more than 2^32 elements apart: the same results as of their copies."""
+    far = (1 << 32) + 24
+    big = torch.empty(far + 4096, dtype=torch.bfloat16, device="cuda")
+    small = torch.randn(2, 40, 24, generator=gen(2)).bfloat16().cuda()
+    x = big.as_strided((2, 40, 24), (far, 24, 1))
+    x.copy_(small)
+    f = torch.randn(2, 40, 24, generator=gen(3)).bfloat16().cuda()
+    out = torch.empty(far + 4096, dtype=torch.bfloat16, device="cuda").as_strided((2, 40, 24), (far, 24, 1))
+    y, last = rrm.gated_scan(x, f, out=out)
+    want, wlast = rrm.gated_scan(small, f)
+    assert torch.equal(y, want) and torch.equal(last, wlast)
+    marks = rrm.gated_scan_marks(small)
+    rrm.gated_scan(x, f, marks=marks)
+    got = rrm.gated_scan_backward(x, x, f, marks, dx=out)
+    for a, e in zip(got, rrm.gated_scan_backward(small, small, f, marks)):
+        assert torch.equal(a, e)
+    stats = torch.empty(2, 3, 2, device="cuda")
+    y = rrm.group_norm_act(x, 3, act="gelu", out=out, stats=stats)
+    assert torch.equal(y, rrm.group_norm_act(small, 3, act="gelu"))
+    for a, e in zip(rrm.group_norm_act_backward(x, x, stats, act="gelu", dx=out), rrm.group_norm_act_backward(small, small, stats, act="gelu")):
+        assert torch.equal(a, e)
+    for m in (2, 20):  # rows a gigabyte and more apart
+        step = far // (m - 1) // 8 * 8
+        rows = big.as_strided((m, 24), (step, 1))
+        rows.copy_(torch.randn(m, 24, generator=gen(m)).bfloat16())
+        x2, to = rows.contiguous(), torch.empty_strided((m, 24), (step, 1), dtype=torch.bfloat16, device="cuda")
+        wg, wu = torch.randn(24, 24, generator=gen(5)).bfloat16().cuda(), torch.randn(24, 24, generator=gen(6)).bfloat16().cuda()
+        g, u = torch.empty(m, 24, device="cuda", dtype=torch.bfloat16), torch.empty(m, 24, device="cuda", dtype=torch.bfloat16)
+        assert torch.equal(rrm.gated_ff(rows, wg, wu, out=to, save=(g, u)), rrm.gated_ff(x2, wg, wu))
+        for a, e in zip(rrm.gated_ff_backward(rows, rows, wg, wu, g, u, dx=to), rrm.gated_ff_backward(x2, x2, wg, wu, g, u)):
+            assert torch.equal(a, e)
+
+
 # -- refusals ------------------------------------------------------------------------------------------------------------------
 
 def _norm_desc(**kw):
