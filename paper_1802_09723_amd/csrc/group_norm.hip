@@ -6,6 +6,10 @@ namespace rrm {
 namespace {
 
 constexpr int HELD_GROUPS = 64;  // groups of a workgroup at most
+// A few workgroups (fewer than half the compute units) of more values than this take longer than slices on all compute units: us forward and backward,
+// 2 x 126 positions x 139 channels fp32 13.5 and 15.4, 14.3 and 18.3 in slices; 5 x 1050 x 28 bf16 15.8 and 25.3, 15.4 and 18.6; 8 x 196 x 512
+// bf16 33 and 21, 16 and 20.
+constexpr int64_t HELD_FEW = 20000;
 
 // ---- samples that registers hold ---------------------------------------------------------------------------------------
 //
@@ -565,12 +569,14 @@ struct HeldPlan {
 struct HeldShape {
     int threads, p;
 };
+// (64 x 28 x 28 x 128 bf16 in 1024 threads of four and two vectors instead of 512 of eight: 15.2 and 23 us, 13.7 and 18 so)
+constexpr int HELD_SHAPES = 4;
 constexpr HeldShape FORWARD[] = {{256, 1}, {256, 4}, {512, 8}, {1024, 16}};
 constexpr HeldShape BACKWARD[] = {{256, 1}, {256, 4}, {512, 8}, {1024, 8}};
 
 // The held form's shape: the smallest that holds the sample's positions.  Runs of a position are 64 bytes at least (what memory hands out)
 // where that fits, and more where there are workgroups enough.  It goes by sizes alone: strides and alignment do not change a result's bits.
-HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[4]) {
+HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[HELD_SHAPES]) {
     const int cg = d.c / d.groups, esize = d.x_elem == RRM_F32 ? 4 : 2;
     HeldPlan p{{}, d.c >= wide ? wide : 1, -1};
     auto fits = [&](int channels) {
@@ -578,7 +584,7 @@ HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[4
         int lanes = 1;
         while (lanes * p.vec < channels) lanes <<= 1;
         if (channels / cg > HELD_GROUPS) return false;
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < HELD_SHAPES; ++w) {
             if (lanes > shapes[w].threads || (int64_t)shapes[w].threads / lanes * shapes[w].p < d.positions) continue;
             p.which = w;
             p.g = HeldGeom{channels, (d.c + channels - 1) / channels, lanes, 1.0f / (float)cg};
@@ -597,8 +603,7 @@ HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[4
         if (fits(cb) && (int64_t)d.n * p.g.blocks >= OP_CUS) break;
     }
     if (!fits(cb)) return p;
-    // a few workgroups of the largest shape take longer than slices on all compute units (8 x 14 x 14 x 512 in one group, bf16: 33 and 16 us)
-    if (p.which == 3 && (int64_t)d.n * p.g.blocks < OP_CUS / 2) {
+    if ((int64_t)d.n * p.g.blocks < OP_CUS / 2 && (int64_t)cb * d.positions > HELD_FEW) {
         p.which = -1;
         return p;
     }
@@ -685,7 +690,7 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
             const HeldPlan p = plan_held(d, WIDE, BACKWARD);
             auto go = [&](auto vec, auto which) {
                 constexpr HeldShape h = BACKWARD[decltype(which)::value];
-                // (bfloat16, 1024 threads: there are no registers for dz in 32 bits)
+                // (bfloat16, the largest: there are no registers for dz in 32 bits)
                 constexpr bool KEEP = sizeof(TX) == 4 || h.threads < 1024;
                 hipLaunchKernelGGL((held_back_kernel<TX, TY, decltype(vec)::value, h.p, h.threads, KEEP>), dim3(held_grid(d, p)), dim3(h.threads),
                                    0, s, d, p.g, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, (float*)ws);
@@ -697,7 +702,7 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                     case 1: go(vec, std::integral_constant<int, 1>{}); break;
                     case 2: go(vec, std::integral_constant<int, 2>{}); break;
                     case 3: go(vec, std::integral_constant<int, 3>{}); break;
-                    default: {
+                        default: {
                         const SliceGeom g = plan_slices(d, VEC);
                         const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
                         float* to = (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));

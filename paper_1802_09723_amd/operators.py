@@ -153,7 +153,7 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
     ``stats``, float32 [n, groups, 2], what the backward pass needs."""
     made = out is None
     if made:
-        out = x.new_empty(x.shape, dtype=out_dtype or x.dtype)
+        out = torch.empty_like(x, dtype=out_dtype)
     key = ("norm", groups, act, eps, out_dtype, _look(x), made or _look(out), _look(gamma), _look(beta), _look(stats))
     plan = _plans.get(key)
     if plan is None:
@@ -208,7 +208,7 @@ def group_norm_act_backward(dy, x, stats, gamma=None, beta=None, act: str = "non
     c = x.shape[-1]
     made = [t is None for t in (dx, dgamma, dbeta)]
     if dx is None:
-        dx = x.new_empty(x.shape)
+        dx = torch.empty_like(x)
     if dgamma is None:
         dgamma = x.new_empty((c,), dtype=torch.float32)
     if dbeta is None:
@@ -256,7 +256,7 @@ def gated_scan(x, f, h0=None, lengths=None, out=None, h_last=None, marks=None, s
     n, t, c = shape = x.shape
     made = (out is None, h_last is None)
     if out is None:
-        out = x.new_empty(shape)
+        out = torch.empty_like(x)
     if h_last is None:
         h_last = x.new_empty((n, c), dtype=torch.float32)
     key = ("scan", _look(x), _look(f), _look(h0), _look(lengths), made[0] or _look(out), made[1] or _look(h_last), _look(marks))
@@ -287,9 +287,9 @@ def gated_scan_backward(dy, x, f, marks, lengths=None, dh_last=None, dx=None, df
     n, t, c = shape = x.shape
     made = [g is None for g in (dx, df, dh0)]
     if dx is None:
-        dx = x.new_empty(shape)
+        dx = torch.empty_like(x)
     if df is None:
-        df = x.new_empty(shape)
+        df = torch.empty_like(f)
     if dh0 is None:
         dh0 = x.new_empty((n, c), dtype=torch.float32)
     key = ("scan back", _look(dy), _look(x), _look(f), _look(marks), _look(lengths), _look(dh_last),
@@ -352,11 +352,11 @@ def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None,
     """``rrm_gated_ff_backward``: (dx, dwg, dwu) from ``dh`` and the projections ``g`` and ``u`` that the forward pass saved."""
     made = [t is None for t in (dx, dwg, dwu)]
     if dx is None:
-        dx = x.new_empty(x.shape)
+        dx = torch.empty_like(x)
     if dwg is None:
-        dwg = wg.new_empty(wg.shape)
+        dwg = torch.empty_like(wg)
     if dwu is None:
-        dwu = wu.new_empty(wu.shape)
+        dwu = torch.empty_like(wu)
     px, pg, pu = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     loose = (px | pg | pu) & 15 != 0
     key = ("ff back", act, loose, _look(dh), _look(x), _look(wg), _look(wu), _look(g), _look(u),
