@@ -71,20 +71,22 @@ __device__ __forceinline__ u32x4 ragged_chunk(src_t row, int k, int len) {
 }
 
 // Tile product on the matrix cores.  (comment to come)
+template <int MT, int NT, int WM, int WN, int STAGES>
+constexpr int TILE_LDS = STAGES * (MT * 32 * WM + NT * 32 * WN) * STEP * 2;
+
 template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_kernel(Product a) {
+__device__ __forceinline__ void tile_product(const Product& a, unsigned char* lds, int id, int split) {
     constexpr int THREADS = WM * WN * 64, BM = MT * 32 * WM, BN = NT * 32 * WN;
     constexpr int PB = BM * STEP * 2, QB = BN * STEP * 2;                       // bytes of a staged tile
     constexpr int NP = PB / (THREADS * 16), NQ = QB / (THREADS * 16);          // 16-byte chunks a thread stages
     constexpr int OUT_COLS = KIND == GATED ? BN / 2 : BN;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[STAGES * (PB + QB)];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = wave % WM, wn = wave / WM;
 
     // tiles XCD by XCD (workgroups go to the eight in turn), and there in blocks of eight rows of tiles
     int tm, tn;
     {
-        const int total = a.tiles_m * a.tiles_n, id = (int)blockIdx.x, xcd = id & 7, q = total >> 3, r = total & 7;
+        const int total = a.tiles_m * a.tiles_n, xcd = id & 7, q = total >> 3, r = total & 7;
         const int t = xcd * q + (xcd < r ? xcd : r) + (id >> 3);
         const int group = 8 * a.tiles_n, g = t / group, first = g * 8, n = a.tiles_m - first < 8 ? a.tiles_m - first : 8;
         tm = first + (t - g * group) % n;
@@ -99,7 +101,6 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
     const int m0 = tm * BM, n0 = tn * OUT_COLS;
     const int steps_of = (a.len + STEP - 1) / STEP;  // of one pair
     const int steps_all = steps_of * (KIND == PLAIN ? a.pairs : 1);
-    const int split = (int)blockIdx.y;
     const int s0 = (int)((int64_t)steps_all * split / a.splits), s1 = (int)((int64_t)steps_all * (split + 1) / a.splits);
 
     // Sources of this thread's chunks.  LDS holds [row][64 of the summed axis] with the eight chunks of a row turned by the row's
@@ -387,6 +388,25 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT * 16 > 128 ? 1 : 2) void tile_
     }
 }
 
+template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM* WN * 64, 2) void tile_kernel(Product a) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[TILE_LDS<MT, NT, WM, WN, STAGES>];
+    tile_product<KIND, ACT, PT, QT, MT, NT, WM, WN, STAGES>(a, lds, (int)blockIdx.x, (int)blockIdx.y);
+}
+// dX and both dW in one launch, so that the one's last workgroups run beside the other's: first `dx`, its splits one behind the other, `whole`
+// workgroups each (its tiles, to whole eights: ids go to the XCDs in turn), then `dw`
+template <int MT, int NT, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM* WN * 64, 2) void gradients_kernel(Product dx, Product dw, int whole) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[TILE_LDS<MT, NT, WM, WN, STAGES>];
+    const int first = whole * dx.splits, id = (int)blockIdx.x;
+    if (id < first) {
+        const int split = id / whole, k = id - split * whole;
+        if (k < dx.tiles_m * dx.tiles_n) tile_product<PLAIN, RRM_ACT_NONE, false, true, MT, NT, WM, WN, STAGES>(dx, lds, k, split);
+    } else {
+        tile_product<HALVES, RRM_ACT_NONE, true, true, MT, NT, WM, WN, STAGES>(dw, lds, id - first, 0);
+    }
+}
+
 // Few rows (up to 16): the weights are the traffic, and each is read once, from memory straight into the fragments of the
 // matrix cores.  A workgroup makes 16 hidden features; its eight wavefronts take eight parts of the summed axis and meet in LDS.
 constexpr int FEW_WAVES = 8, FEW_F = 16, FEW_ROWS = 16;
@@ -510,35 +530,40 @@ __global__ __launch_bounds__(256) void join_gated_kernel(const float* __restrict
     }
 }
 
-// Copies of up to three operands of rows of `len`, padded with zeros to whole chunks; a thread a chunk
+// Copies of up to three operands of rows of `len`, padded with zeros to whole chunks; chunk i of all of them
 struct PadJob {
     Source from[3];
     __bf16* to[3];
     int64_t first[4];  // chunk that each begins with; the end
     int n, len;
 };
-__global__ __launch_bounds__(256) void pad_kernel(PadJob j) {
+__device__ __forceinline__ void pad_chunk(const PadJob& j, int64_t i) {
     const int per = (j.len + 7) / 8;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < j.first[j.n]; i += (int64_t)gridDim.x * 256) {
-        const int w = i < j.first[1] || j.n == 1 ? 0 : i < j.first[2] || j.n == 2 ? 1 : 2;
-        const Source from = w == 0 ? j.from[0] : w == 1 ? j.from[1] : j.from[2];
-        __bf16* to = w == 0 ? j.to[0] : w == 1 ? j.to[1] : j.to[2];
-        const int64_t at = i - (w == 0 ? 0 : w == 1 ? j.first[1] : j.first[2]), r = at / per;
-        *reinterpret_cast<u32x4*>(to + at * 8) = ragged_chunk(from.p + r * from.row, (int)(at - r * per) * 8, j.len);
-    }
+    const int w = i < j.first[1] || j.n == 1 ? 0 : i < j.first[2] || j.n == 2 ? 1 : 2;
+    const Source from = w == 0 ? j.from[0] : w == 1 ? j.from[1] : j.from[2];
+    __bf16* to = w == 0 ? j.to[0] : w == 1 ? j.to[1] : j.to[2];
+    const int64_t at = i - (w == 0 ? 0 : w == 1 ? j.first[1] : j.first[2]), r = at / per;
+    *reinterpret_cast<u32x4*>(to + at * 8) = ragged_chunk(from.p + r * from.row, (int)(at - r * per) * 8, j.len);
+}
+__global__ __launch_bounds__(256) void pad_kernel(PadJob j) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < j.first[j.n]; i += (int64_t)gridDim.x * 256) pad_chunk(j, i);
 }
 
-// dG and dU from dH, G and U; rows of `pitch` elements, a multiple of eight, zeros behind column f (they are summed over).
-// Eight columns a thread.
+// dG and dU from dH, G and U; rows of `pitch` elements, a multiple of eight, zeros behind column f (they are summed over), eight columns a
+// thread; then the padded copies that the products need.
 template <int ACT>
-__global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src_t u, src_t dh, int vec, int pitch, __bf16* __restrict__ dg,
-                                                     __bf16* __restrict__ du) {
-    const int64_t chunks = pitch / 8, total = chunks * d.m;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src_t u, src_t dh, int pitch, __bf16* __restrict__ dg, __bf16* __restrict__ du,
+                                                     PadJob job) {
+    const int64_t chunks = pitch / 8, total = chunks * d.m, all = total + (job.n ? job.first[job.n] : 0);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        if (i >= total) {
+            pad_chunk(job, i - total);
+            continue;
+        }
         const int64_t r = i / chunks;
         const int f = (int)(i - r * chunks) * 8;
         float gv[8], uv[8], dv[8], og[8], ou[8];
-        if (vec && f + 8 <= d.f) {
+        if (f + 8 <= d.f) {
             load_vec<8>(g + r * d.gu_row + f, gv);
             load_vec<8>(u + r * d.gu_row + f, uv);
             load_vec<8>(dh + r * d.h_row + f, dv);
@@ -565,8 +590,6 @@ __global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src
 
 int tiles(int n, int of) { return (n + of - 1) / of; }
 
-bool chunked(const void* p, int64_t row) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && row % 8 == 0; }  // rows begin at whole chunks
-
 template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
 hipError_t launch_tiles(Product& a, hipStream_t s) {
     constexpr int BM = MT * 32 * WM, BN = NT * 32 * WN / (KIND == GATED ? 2 : 1);
@@ -589,25 +612,33 @@ constexpr Shape SHAPES[] = {
 };
 struct Plan {
     int shape, splits;
+    float us;
 };
-// kind, rows, cols, len, pairs as in Product; `planes`: float32 results a split leaves of each element (0: no splits)
-Plan plan_product(int kind, int rows, int cols, int len, int pairs, int planes) {
-    Plan best{SMALL, 1};
-    float least = 1e30f;
-    const int steps = tiles(len, STEP) * pairs;
-    // no product is done before its operands have come from memory, at some 4 TB/s
-    const float floor_us = 2.0f * len * pairs * ((float)rows + (float)cols * (kind == GATED ? 2 : 1)) / 4e6f;
+constexpr float LAUNCH_US = 6.0f;  // what a launch of tiles takes beside its steps: its start, its first copies, its results
+struct Work {  // of a launch: products of rows x cols (each of `ways` results) over `steps` steps
+    int rows, cols, steps, ways;
+};
+// The least estimate for a product, or two in one launch.  Of the first the summed axis may be split, which leaves `planes` float32 results of each
+// element (0: no splits); `bytes`: what comes from memory at the least, at some 4 TB/s.
+Plan plan_products(const Work& a, const Work& b, int planes, float bytes) {
+    Plan best{SMALL, 1, 1e30f};
     for (int w = BIG; w <= SMALL; ++w) {
         const Shape& h = SHAPES[w];
-        const int64_t t = (int64_t)tiles(rows, h.bm) * tiles(cols, kind == GATED ? h.bn / 2 : h.bn) * (kind == HALVES ? 2 : 1);
+        auto count = [&](const Work& p) { return (int64_t)tiles(p.rows, h.bm) * tiles(p.cols, h.bn) * p.ways; };
         for (int splits = 1; splits <= (planes ? 16 : 1); splits *= 2) {
-            if (splits > 1 && steps / splits < 4) break;
-            const int64_t count = t * splits, rounds = (count + h.at_once - 1) / h.at_once;
-            float us = tiles(steps, splits) * ((float)rounds * h.first + (float)count / OP_CUS * h.second);
-            if (us < floor_us) us = floor_us;
+            if (splits > 1 && a.steps / splits < 4) break;
+            const int each = tiles(a.steps, splits), longest = each > b.steps ? each : b.steps;
+            const int64_t groups = count(a) * splits + count(b), all = count(a) * splits * each + count(b) * b.steps;
+            // rounds of the longest workgroups' steps; two products share them by their steps
+            const int64_t rounds = (groups + h.at_once - 1) / h.at_once;
+            float steps = (float)rounds * longest;
+            if (b.steps && rounds > 1) steps = (float)all / h.at_once + 0.5f * longest;
+            float us = steps * h.first + (float)all / OP_CUS * h.second;
+            if (us < bytes / 4e6f) us = bytes / 4e6f;
             // the sums' way through memory and the launch that joins them
-            if (splits > 1) us += 5.0f + (float)splits * planes * rows * (float)cols * 8.0f / 6e6f;
-            if (us < least) least = us, best = Plan{w, splits};
+            if (splits > 1) us += 5.0f + (float)splits * planes * a.rows * (float)(a.cols / a.ways) * 8.0f / 6e6f;
+            us += LAUNCH_US;
+            if (us < best.us) best = Plan{w, splits, us};
         }
     }
     return best;
@@ -622,8 +653,42 @@ hipError_t launch_product(Product& a, int shape, hipStream_t s) {
         default: return launch_tiles<KIND, ACT, PT, QT, 1, 2, 2, 2, 3>(a, s);
     }
 }
-Plan forward_plan(const rrm_ff_desc& d) { return plan_product(GATED, d.m, d.f, d.k, 1, 2); }
-Plan dx_plan(const rrm_ff_desc& d) { return plan_product(PLAIN, d.m, d.k, d.f, 2, 1); }
+template <int MT, int NT, int WM, int WN, int STAGES>
+hipError_t launch_both(Product& x, Product& w, hipStream_t s) {
+    constexpr int BM = MT * 32 * WM, BN = NT * 32 * WN;
+    x.tiles_m = tiles(x.rows, BM), x.tiles_n = tiles(x.cols, BN);
+    w.tiles_m = 2 * tiles(w.rows, BM), w.tiles_n = tiles(w.cols, BN);
+    const int whole = (x.tiles_m * x.tiles_n + 7) / 8 * 8;
+    hipLaunchKernelGGL((gradients_kernel<MT, NT, WM, WN, STAGES>), dim3((unsigned)(whole * x.splits + w.tiles_m * w.tiles_n)), dim3(WM * WN * 64), 0, s,
+                       x, w, whole);
+    return hipGetLastError();
+}
+hipError_t launch_gradients(Product& x, Product& w, int shape, hipStream_t s) {
+    switch (shape) {
+        case BIG: return launch_both<4, 2, 2, 4, 2>(x, w, s);
+        case WIDE: return launch_both<2, 2, 2, 2, 4>(x, w, s);
+        case WIDE_PAIR: return launch_both<2, 2, 2, 2, 2>(x, w, s);
+        default: return launch_both<1, 2, 2, 2, 3>(x, w, s);
+    }
+}
+Plan forward_plan(const rrm_ff_desc& d) {
+    return plan_products({d.m, 2 * d.f, tiles(d.k, STEP), 1}, {0, 0, 0, 0}, 1, 2.0f * d.k * ((float)d.m + 2.0f * d.f));
+}
+// dX and dW, one launch of one shape or each by itself (512 x 4096 x 4096: dX wants few large parts, dW 256 x 256 tiles of eight steps; 106 us
+// together, 92 apart; 512 x 1024 x 2048: 27 and 34)
+struct GradientsPlan {
+    Plan x, w;
+    bool together;
+};
+GradientsPlan gradients_plan(const rrm_ff_desc& d, bool dx, bool dw) {
+    const Work x{d.m, d.k, 2 * tiles(d.f, STEP), 1}, w{d.f, d.k, tiles(d.m, STEP), 2}, none{0, 0, 0, 0};
+    const float of_x = 2.0f * ((float)d.m + d.k) * 2 * d.f, of_w = 2.0f * ((float)d.m * d.k + 2.0f * d.f * d.k);
+    GradientsPlan p{plan_products(x, none, 1, of_x), plan_products(w, none, 0, of_w), false};
+    if (!dx || !dw) return p;
+    const Plan both = plan_products(x, w, 1, of_x + of_w);
+    if (both.us < p.x.us + p.w.us) p.x = p.w = both, p.together = true;
+    return p;
+}
 
 // Up to so many rows the weights go from memory into the fragments (few_rows_kernel): 4096 -> 4096, 1 / 16 / 32 / 64 rows
 // 14.6 / 16.9 / 18.5 / 26.7 us so, 19 by tiles; 4096 -> 9216 36 / 44 / 53 / 77 us and 40.
@@ -648,35 +713,38 @@ Padded padded_places(const rrm_ff_desc& d, bool x, bool w) {
     p.wu = take(d.f, d.wu_row, w);
     return p;
 }
-// Sources for the products of up to three operands of rows of k: themselves, or their padded copies (one launch makes them)
-hipError_t sources(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, unsigned char* ws, Source& sx, Source& sg, Source& su,
-                   hipStream_t s) {
+// Sources for the products of up to three operands of rows of k: themselves, or padded copies, which `job` is to make
+PadJob sources(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, unsigned char* ws, Source& sx, Source& sg, Source& su) {
     const Padded at = padded_places(d, x != nullptr, wg != nullptr);
     PadJob job{};
     job.len = d.k;
     auto one = [&](const void* p, int64_t row, int rows, size_t place) {
         if (!p || !loose_rows(d, row)) return Source{(src_t)p, row};
         __bf16* to = (__bf16*)(ws + place);
-        const int64_t chunks = (int64_t)rows * (round8(d.k) / 8);
         job.from[job.n] = Source{(src_t)p, row};
         job.to[job.n] = to;
-        job.first[job.n + 1] = job.first[job.n] + chunks;
+        job.first[job.n + 1] = job.first[job.n] + (int64_t)rows * (round8(d.k) / 8);
         ++job.n;
         return Source{to, round8(d.k)};
     };
     sx = one(x, d.x_row, d.m, at.x);
     sg = one(wg, d.wg_row, d.f, at.wg);
     su = one(wu, d.wu_row, d.f, at.wu);
-    if (job.n == 0) return hipSuccess;
-    const int64_t groups = (job.first[job.n] + 255) / 256;
-    hipLaunchKernelGGL(pad_kernel, dim3((unsigned)(groups < OP_CUS * 64 ? groups : OP_CUS * 64)), dim3(256), 0, s, job);
-    return hipGetLastError();
+    return job;
+}
+unsigned some_groups(int64_t chunks) {
+    const int64_t groups = (chunks + 255) / 256;
+    return (unsigned)(groups < OP_CUS * 32 ? groups : OP_CUS * 32);
 }
 
 size_t grads_bytes(const rrm_ff_desc& d) { return round256((size_t)d.m * round8(d.f) * 2); }
-size_t split_bytes(const rrm_ff_desc& d, bool backward) {
-    const int splits = (backward ? dx_plan(d) : forward_plan(d)).splits;
-    return splits > 1 ? round256((size_t)splits * d.m * tiles(backward ? d.k : d.f, 4) * 16) * (backward ? 1 : 2) : 0;
+size_t split_bytes(const rrm_ff_desc& d, bool backward) {  // (backward: whichever gradients a call asks for)
+    auto bytes = [&](const Plan& p, int cols, int planes) {
+        return p.splits > 1 ? round256((size_t)p.splits * d.m * tiles(cols, 4) * 16 * planes) : 0;
+    };
+    if (!backward) return bytes(forward_plan(d), d.f, 2);
+    const size_t a = bytes(gradients_plan(d, true, true).x, d.k, 1), b = bytes(gradients_plan(d, true, false).x, d.k, 1);
+    return a > b ? a : b;
 }
 
 }  // namespace
@@ -698,8 +766,11 @@ hipError_t launch_gated_ff(const rrm_ff_desc& d, const void* x, const void* wg, 
         return hipGetLastError();
     }
     Product a{};
-    e = sources(d, x, wg, wu, (unsigned char*)ws, a.p[0], a.q[0], a.q[1], s);
-    if (e != hipSuccess) return e;
+    const PadJob job = sources(d, x, wg, wu, (unsigned char*)ws, a.p[0], a.q[0], a.q[1]);
+    if (job.n) {
+        hipLaunchKernelGGL(pad_kernel, dim3(some_groups(job.first[job.n])), dim3(256), 0, s, job);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const Plan plan = forward_plan(d);
     a.pairs = 1, a.splits = plan.splits;
     a.part = (float*)((unsigned char*)ws + padded_places(d, true, true).all);
@@ -726,42 +797,39 @@ hipError_t launch_gated_ff_backward(const rrm_ff_desc& d, const void* x, const v
     hipError_t e = hipSuccess;
     if (d.m > 0) {
         at += 2 * grads_bytes(d);
-        const int64_t chunks = (int64_t)d.m * (pitch / 8), groups = (chunks + 255) / 256;
-        const int vec = chunked(g, d.gu_row) && chunked(u, d.gu_row) && chunked(dh, d.h_row);
+        const PadJob job = sources(d, dwg ? x : nullptr, dx ? wg : nullptr, dx ? wu : nullptr, at, sx, sg, su);
+        at += padded_places(d, true, true).all;
+        const int64_t chunks = (int64_t)d.m * (pitch / 8) + (job.n ? job.first[job.n] : 0);
         with_act(d.act, [&](auto act) {
-            hipLaunchKernelGGL((slopes_kernel<decltype(act)::value>), dim3((unsigned)(groups < OP_CUS * 32 ? groups : OP_CUS * 32)), dim3(256),
-                               0, s, d, (src_t)g, (src_t)u, (src_t)dh, vec, pitch, (__bf16*)dg.p, (__bf16*)du.p);
+            hipLaunchKernelGGL((slopes_kernel<decltype(act)::value>), dim3(some_groups(chunks)), dim3(256), 0, s, d, (src_t)g, (src_t)u, (src_t)dh,
+                               pitch, (__bf16*)dg.p, (__bf16*)du.p, job);
         });
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        e = sources(d, dwg ? x : nullptr, dx ? wg : nullptr, dx ? wu : nullptr, at, sx, sg, su, s);
-        if (e != hipSuccess) return e;
-        at += padded_places(d, true, true).all;
     }
-    if (d.m > 0 && dx) {
-        const Plan plan = dx_plan(d);
-        Product a{};
-        a.p[0] = dg, a.p[1] = du, a.q[0] = sg, a.q[1] = su;
-        a.pairs = 2, a.splits = plan.splits;
-        a.part = (float*)at;
-        a.rows = d.m, a.cols = d.k, a.len = d.f;
-        a.out = (__bf16*)dx, a.out_row = d.dx_row;
-        if ((e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(a, plan.shape, s)) != hipSuccess) return e;
-        if (a.splits > 1) {
-            const int64_t n = ((int64_t)d.m * tiles(d.k, 4) + 255) / 256;
-            hipLaunchKernelGGL(join_kernel, dim3((unsigned)(n < OP_CUS * 16 ? n : OP_CUS * 16)), dim3(256), 0, s, a.part, a.splits, d.m,
-                               d.k, (__bf16*)dx, d.dx_row);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
+    Product px{}, pw{};
+    px.p[0] = dg, px.p[1] = du, px.q[0] = sg, px.q[1] = su;
+    px.pairs = 2, px.splits = 1;
+    px.part = (float*)at;
+    px.rows = d.m, px.cols = d.k, px.len = d.f;
+    px.out = (__bf16*)dx, px.out_row = d.dx_row;
+    pw.p[0] = dg, pw.p[1] = du, pw.q[0] = sx;  // (no rows: sums of nothing, zeros)
+    pw.pairs = 1, pw.splits = 1;
+    pw.rows = d.f, pw.cols = d.k, pw.len = d.m;
+    pw.out = (__bf16*)dwg, pw.out_row = d.dwg_row, pw.out2 = (__bf16*)dwu, pw.out2_row = d.dwu_row;
+    const bool want_x = d.m > 0 && dx;
+    const GradientsPlan plan = gradients_plan(d, want_x, dwg != nullptr);
+    px.splits = plan.x.splits;
+    if (plan.together) {
+        e = launch_gradients(px, pw, plan.x.shape, s);
+    } else {
+        if (want_x) e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(px, plan.x.shape, s);
+        if (dwg && e == hipSuccess) e = launch_product<HALVES, RRM_ACT_NONE, true, true>(pw, plan.w.shape, s);
     }
-    if (dwg) {  // (no rows: sums of nothing, zeros)
-        Product a{};
-        a.p[0] = dg, a.p[1] = du, a.q[0] = sx;
-        a.pairs = 1, a.splits = 1;
-        a.rows = d.f, a.cols = d.k, a.len = d.m;
-        a.out = (__bf16*)dwg, a.out_row = d.dwg_row, a.out2 = (__bf16*)dwu, a.out2_row = d.dwu_row;
-        e = launch_product<HALVES, RRM_ACT_NONE, true, true>(a, plan_product(HALVES, d.f, d.k, d.m, 1, 0).shape, s);
-    }
-    return e;
+    if (e != hipSuccess || !want_x || px.splits == 1) return e;
+    const int64_t n = ((int64_t)d.m * tiles(d.k, 4) + 255) / 256;
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(n < OP_CUS * 16 ? n : OP_CUS * 16)), dim3(256), 0, s, px.part, px.splits, d.m, d.k, (__bf16*)dx,
+                       d.dx_row);
+    return hipGetLastError();
 }
 
 }  // namespace rrm
