@@ -33,7 +33,7 @@ struct Product {
     int splits;             // parts of the summed axis, one workgroup each; more than one: sums to `part`
     __bf16 *out, *out2, *out3;  // gated: H, G, U (G and U may be nullptr); halves: out2 belongs to p[1]
     int64_t out_row, out2_row;
-    float* part;            // [splits][rows][cols, to whole fours] (gated: [splits][2][rows][..])
+    float* part;            // [splits][rows][cols, to whole fours] (gated, halves: [splits][2][rows][..])
 };
 
 enum Kind : int { GATED = 0, PLAIN = 1, HALVES = 2 };
@@ -317,8 +317,8 @@ __device__ __forceinline__ void tile_product(const Product& a, unsigned char* ld
 
     // acc[i][j][4 q + e] of lane l: row (wm MT + i) 32 + l % 32, column (wn NT + j) 32 + 8 q + 4 (l / 32) + e
     const int lr = lane & 31, lc = (lane >> 5) * 4;
-    if (KIND != HALVES && a.splits > 1) {
-        constexpr int WAYS = KIND == GATED ? 2 : 1;
+    if (a.splits > 1) {
+        constexpr int WAYS = KIND == GATED ? 2 : 1;  // results interleaved in a wavefront's blocks of 32 columns
         const int pitch = (a.cols + 3) & ~3;
         const int64_t plane = (int64_t)a.rows * pitch;
 #pragma unroll
@@ -327,7 +327,7 @@ __device__ __forceinline__ void tile_product(const Product& a, unsigned char* ld
             if (r >= a.rows) continue;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                float* to = a.part + (int64_t)(split * WAYS + j % WAYS) * plane + r * (int64_t)pitch;
+                float* to = a.part + (int64_t)(KIND == HALVES ? 2 * split + half : split * WAYS + j % WAYS) * plane + r * (int64_t)pitch;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = n0 + (wn * NT + j) / WAYS * 32 + 8 * q + lc;
@@ -393,17 +393,18 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void tile_kernel(Product a) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[TILE_LDS<MT, NT, WM, WN, STAGES>];
     tile_product<KIND, ACT, PT, QT, MT, NT, WM, WN, STAGES>(a, lds, (int)blockIdx.x, (int)blockIdx.y);
 }
-// dX and both dW in one launch, so that the one's last workgroups run beside the other's: first `dx`, its splits one behind the other, `whole`
-// workgroups each (its tiles, to whole eights: ids go to the XCDs in turn), then `dw`
+// dX and both dW in one launch, so that the one's last workgroups run beside the other's: first `dx`, its splits one behind the other, `whole_x`
+// workgroups each (its tiles, to whole eights: ids go to the XCDs in turn), then `dw` likewise
 template <int MT, int NT, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM* WN * 64, 2) void gradients_kernel(Product dx, Product dw, int whole) {
+__global__ __launch_bounds__(WM* WN * 64, 2) void gradients_kernel(Product dx, Product dw, int whole_x, int whole_w) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[TILE_LDS<MT, NT, WM, WN, STAGES>];
-    const int first = whole * dx.splits, id = (int)blockIdx.x;
+    const int first = whole_x * dx.splits, id = (int)blockIdx.x;
     if (id < first) {
-        const int split = id / whole, k = id - split * whole;
+        const int split = id / whole_x, k = id - split * whole_x;
         if (k < dx.tiles_m * dx.tiles_n) tile_product<PLAIN, RRM_ACT_NONE, false, true, MT, NT, WM, WN, STAGES>(dx, lds, k, split);
     } else {
-        tile_product<HALVES, RRM_ACT_NONE, true, true, MT, NT, WM, WN, STAGES>(dw, lds, id - first, 0);
+        const int split = (id - first) / whole_w, k = id - first - split * whole_w;
+        if (k < dw.tiles_m * dw.tiles_n) tile_product<HALVES, RRM_ACT_NONE, true, true, MT, NT, WM, WN, STAGES>(dw, lds, k, split);
     }
 }
 
@@ -496,16 +497,27 @@ __device__ __forceinline__ void leave_four(__bf16* to, const float (&v)[4], int 
         if (n > 2) to[2] = (__bf16)v[2];
     }
 }
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, int splits, int rows, int cols, __bf16* __restrict__ out,
-                                                   int64_t row) {
-    const int fours = (cols + 3) >> 2;
-    const int64_t total = (int64_t)rows * fours;
+// Up to three results (blockIdx.y) of split sums
+struct Join {
+    const float* part;
+    int64_t plane;  // from a split's sums to the next one's
+    __bf16* out;
+    int64_t row;
+    int splits, rows, cols;
+};
+struct Joins {
+    Join j[3];
+};
+__global__ __launch_bounds__(256) void join_kernel(Joins all) {
+    const Join& j = all.j[blockIdx.y];
+    const int fours = (j.cols + 3) >> 2;
+    const int64_t total = (int64_t)j.rows * fours;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / fours;
         const int c = (int)(i - r * fours) * 4;
-        const float4 s = joined(part, 4 * i, 4 * total, splits);
+        const float4 s = joined(j.part, 4 * i, j.plane, j.splits);
         const float v[4] = {s.x, s.y, s.z, s.w};
-        leave_four(out + r * row + c, v, cols - c);
+        leave_four(j.out + r * j.row + c, v, j.cols - c);
     }
 }
 // H, G and U of the splits' sums
@@ -589,6 +601,7 @@ __global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src
 }
 
 int tiles(int n, int of) { return (n + of - 1) / of; }
+int round8(int n) { return (n + 7) & ~7; }
 
 template <int KIND, int ACT, bool PT, bool QT, int MT, int NT, int WM, int WN, int STAGES>
 hipError_t launch_tiles(Product& a, hipStream_t s) {
@@ -611,35 +624,37 @@ constexpr Shape SHAPES[] = {
     {256, 256, 256, 1.4f, 0.6f}, {128, 128, 256, 0.6f, 0.1f}, {128, 128, 512, 0.85f, 0.2f}, {64, 128, 512, 0.45f, 0.2f},
 };
 struct Plan {
-    int shape, splits;
+    int shape, splits, splits2;  // parts of the summed axis (of the second product)
     float us;
 };
 constexpr float LAUNCH_US = 6.0f;  // what a launch of tiles takes beside its steps: its start, its first copies, its results
-struct Work {  // of a launch: products of rows x cols (each of `ways` results) over `steps` steps
+struct Work {  // a product of rows x cols, `ways` of them, over `steps` steps each
     int rows, cols, steps, ways;
 };
-// The least estimate for a product, or two in one launch.  Of the first the summed axis may be split, which leaves `planes` float32 results of each
-// element (0: no splits); `bytes`: what comes from memory at the least, at some 4 TB/s.
-Plan plan_products(const Work& a, const Work& b, int planes, float bytes) {
-    Plan best{SMALL, 1, 1e30f};
+// The least estimate for a product, or two in one launch (b.steps > 0); `bytes`: what comes from memory at the least, at some 4 TB/s.
+Plan plan_products(const Work& a, const Work& b, float bytes) {
+    Plan best{SMALL, 1, 1, 1e30f};
     for (int w = BIG; w <= SMALL; ++w) {
         const Shape& h = SHAPES[w];
-        auto count = [&](const Work& p) { return (int64_t)tiles(p.rows, h.bm) * tiles(p.cols, h.bn) * p.ways; };
-        for (int splits = 1; splits <= (planes ? 16 : 1); splits *= 2) {
-            if (splits > 1 && a.steps / splits < 4) break;
-            const int each = tiles(a.steps, splits), longest = each > b.steps ? each : b.steps;
-            const int64_t groups = count(a) * splits + count(b), all = count(a) * splits * each + count(b) * b.steps;
-            // rounds of the longest workgroups' steps; two products share them by their steps
-            const int64_t rounds = (groups + h.at_once - 1) / h.at_once;
-            float steps = (float)rounds * longest;
-            if (b.steps && rounds > 1) steps = (float)all / h.at_once + 0.5f * longest;
-            float us = steps * h.first + (float)all / OP_CUS * h.second;
-            if (us < bytes / 4e6f) us = bytes / 4e6f;
-            // the sums' way through memory and the launch that joins them
-            if (splits > 1) us += 5.0f + (float)splits * planes * a.rows * (float)(a.cols / a.ways) * 8.0f / 6e6f;
-            us += LAUNCH_US;
-            if (us < best.us) best = Plan{w, splits, us};
-        }
+        const int64_t ta = (int64_t)tiles(a.rows, h.bm) * tiles(a.cols, h.bn) * a.ways;
+        const int64_t tb = b.steps ? (int64_t)tiles(b.rows, h.bm) * tiles(b.cols, h.bn) * b.ways : 0;
+        for (int sa = 1; sa <= 16 && (sa == 1 || a.steps / sa >= 4); sa *= 2)
+            for (int sb = 1; sb <= 16 && (sb == 1 || b.steps / sb >= 4); sb *= 2) {
+                const int ea = tiles(a.steps, sa), eb = tiles(b.steps, sb), longest = ea > eb ? ea : eb;
+                const int64_t groups = ta * sa + tb * sb, all = ta * sa * ea + tb * sb * eb;
+                // rounds of the longest workgroups' steps; two products share them by their steps
+                const int64_t rounds = (groups + h.at_once - 1) / h.at_once;
+                float steps = (float)rounds * longest;
+                if (b.steps && rounds > 1) steps = (float)all / h.at_once + 0.5f * longest;
+                float us = steps * h.first + (float)all / OP_CUS * h.second;
+                if (us < bytes / 4e6f) us = bytes / 4e6f;
+                // the sums' way through memory and the launch that joins them
+                if (sa > 1 || sb > 1) us += 5.0f;
+                if (sa > 1) us += (float)sa * a.ways * a.rows * (float)a.cols * 8.0f / 6e6f;
+                if (sb > 1) us += (float)sb * b.ways * b.rows * (float)b.cols * 8.0f / 6e6f;
+                us += LAUNCH_US;
+                if (us < best.us) best = Plan{w, sa, sb, us};
+            }
     }
     return best;
 }
@@ -658,9 +673,9 @@ hipError_t launch_both(Product& x, Product& w, hipStream_t s) {
     constexpr int BM = MT * 32 * WM, BN = NT * 32 * WN;
     x.tiles_m = tiles(x.rows, BM), x.tiles_n = tiles(x.cols, BN);
     w.tiles_m = 2 * tiles(w.rows, BM), w.tiles_n = tiles(w.cols, BN);
-    const int whole = (x.tiles_m * x.tiles_n + 7) / 8 * 8;
-    hipLaunchKernelGGL((gradients_kernel<MT, NT, WM, WN, STAGES>), dim3((unsigned)(whole * x.splits + w.tiles_m * w.tiles_n)), dim3(WM * WN * 64), 0, s,
-                       x, w, whole);
+    const int whole_x = round8(x.tiles_m * x.tiles_n), whole_w = round8(w.tiles_m * w.tiles_n);
+    hipLaunchKernelGGL((gradients_kernel<MT, NT, WM, WN, STAGES>), dim3((unsigned)(whole_x * x.splits + whole_w * w.splits)), dim3(WM * WN * 64), 0, s,
+                       x, w, whole_x, whole_w);
     return hipGetLastError();
 }
 hipError_t launch_gradients(Product& x, Product& w, int shape, hipStream_t s) {
@@ -672,22 +687,23 @@ hipError_t launch_gradients(Product& x, Product& w, int shape, hipStream_t s) {
     }
 }
 Plan forward_plan(const rrm_ff_desc& d) {
-    return plan_products({d.m, 2 * d.f, tiles(d.k, STEP), 1}, {0, 0, 0, 0}, 1, 2.0f * d.k * ((float)d.m + 2.0f * d.f));
+    return plan_products({d.m, 2 * d.f, tiles(d.k, STEP), 1}, {0, 0, 0, 0}, 2.0f * d.k * ((float)d.m + 2.0f * d.f));
 }
 // dX and dW, one launch of one shape or each by itself (512 x 4096 x 4096: dX wants few large parts, dW 256 x 256 tiles of eight steps; 106 us
 // together, 92 apart; 512 x 1024 x 2048: 27 and 34)
 struct GradientsPlan {
-    Plan x, w;
+    int x_shape, w_shape, x_splits, w_splits;
     bool together;
 };
 GradientsPlan gradients_plan(const rrm_ff_desc& d, bool dx, bool dw) {
     const Work x{d.m, d.k, 2 * tiles(d.f, STEP), 1}, w{d.f, d.k, tiles(d.m, STEP), 2}, none{0, 0, 0, 0};
     const float of_x = 2.0f * ((float)d.m + d.k) * 2 * d.f, of_w = 2.0f * ((float)d.m * d.k + 2.0f * d.f * d.k);
-    GradientsPlan p{plan_products(x, none, 1, of_x), plan_products(w, none, 0, of_w), false};
-    if (!dx || !dw) return p;
-    const Plan both = plan_products(x, w, 1, of_x + of_w);
-    if (both.us < p.x.us + p.w.us) p.x = p.w = both, p.together = true;
-    return p;
+    const Plan px = plan_products(x, none, of_x), pw = plan_products(w, none, of_w);
+    if (dx && dw) {
+        const Plan both = plan_products(x, w, of_x + of_w);
+        if (both.us < px.us + pw.us) return {both.shape, both.shape, both.splits, both.splits2, true};
+    }
+    return {px.shape, pw.shape, px.splits, pw.splits, false};
 }
 
 // Up to so many rows the weights go from memory into the fragments (few_rows_kernel): 4096 -> 4096, 1 / 16 / 32 / 64 rows
@@ -695,7 +711,6 @@ GradientsPlan gradients_plan(const rrm_ff_desc& d, bool dx, bool dw) {
 bool few_rows(const rrm_ff_desc& d) { return d.m <= FEW_ROWS; }
 
 // The tile kernel copies whole, aligned 16-byte chunks: rows that are not made of them are copied to the workspace first, padded with zeros.
-int round8(int n) { return (n + 7) & ~7; }
 bool loose_rows(const rrm_ff_desc& d, int64_t row) { return d.unaligned || d.k % 8 != 0 || row % 8 != 0; }
 struct Padded {
     size_t x, wg, wu, all;  // places in the workspace, and the bytes of all
@@ -738,13 +753,16 @@ unsigned some_groups(int64_t chunks) {
 }
 
 size_t grads_bytes(const rrm_ff_desc& d) { return round256((size_t)d.m * round8(d.f) * 2); }
-size_t split_bytes(const rrm_ff_desc& d, bool backward) {  // (backward: whichever gradients a call asks for)
-    auto bytes = [&](const Plan& p, int cols, int planes) {
-        return p.splits > 1 ? round256((size_t)p.splits * d.m * tiles(cols, 4) * 16 * planes) : 0;
-    };
-    if (!backward) return bytes(forward_plan(d), d.f, 2);
-    const size_t a = bytes(gradients_plan(d, true, true).x, d.k, 1), b = bytes(gradients_plan(d, true, false).x, d.k, 1);
-    return a > b ? a : b;
+size_t sums_bytes(int splits, int rows, int cols, int ways) { return splits > 1 ? round256((size_t)splits * rows * tiles(cols, 4) * 16 * ways) : 0; }
+size_t split_bytes(const rrm_ff_desc& d, bool backward) {
+    if (!backward) return sums_bytes(forward_plan(d).splits, d.m, d.f, 2);
+    size_t most = 0;
+    for (int asked = 1; asked < 4; ++asked) {  // whichever gradients a call asks for
+        const GradientsPlan p = gradients_plan(d, asked & 1, asked & 2);
+        const size_t b = sums_bytes(p.x_splits, d.m, d.k, 1) + sums_bytes(p.w_splits, d.f, d.k, 2);
+        most = b > most ? b : most;
+    }
+    return most;
 }
 
 }  // namespace
@@ -817,18 +835,30 @@ hipError_t launch_gated_ff_backward(const rrm_ff_desc& d, const void* x, const v
     pw.rows = d.f, pw.cols = d.k, pw.len = d.m;
     pw.out = (__bf16*)dwg, pw.out_row = d.dwg_row, pw.out2 = (__bf16*)dwu, pw.out2_row = d.dwu_row;
     const bool want_x = d.m > 0 && dx;
+    if (d.m == 0) return dwg ? launch_product<HALVES, RRM_ACT_NONE, true, true>(pw, SMALL, s) : hipSuccess;
     const GradientsPlan plan = gradients_plan(d, want_x, dwg != nullptr);
-    px.splits = plan.x.splits;
+    px.splits = plan.x_splits, pw.splits = plan.w_splits;
+    pw.part = (float*)((unsigned char*)px.part + (want_x ? sums_bytes(px.splits, d.m, d.k, 1) : 0));
     if (plan.together) {
-        e = launch_gradients(px, pw, plan.x.shape, s);
+        e = launch_gradients(px, pw, plan.x_shape, s);
     } else {
-        if (want_x) e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(px, plan.x.shape, s);
-        if (dwg && e == hipSuccess) e = launch_product<HALVES, RRM_ACT_NONE, true, true>(pw, plan.w.shape, s);
+        if (want_x) e = launch_product<PLAIN, RRM_ACT_NONE, false, true>(px, plan.x_shape, s);
+        if (dwg && e == hipSuccess) e = launch_product<HALVES, RRM_ACT_NONE, true, true>(pw, plan.w_shape, s);
     }
-    if (e != hipSuccess || !want_x || px.splits == 1) return e;
-    const int64_t n = ((int64_t)d.m * tiles(d.k, 4) + 255) / 256;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(n < OP_CUS * 16 ? n : OP_CUS * 16)), dim3(256), 0, s, px.part, px.splits, d.m, d.k, (__bf16*)dx,
-                       d.dx_row);
+    if (e != hipSuccess) return e;
+    Joins joins{};
+    int n = 0;
+    int64_t fours = 0;
+    auto join = [&](const Product& p, int ways, int way, __bf16* out, int64_t row) {
+        const int64_t plane = (int64_t)p.rows * tiles(p.cols, 4) * 4;
+        joins.j[n++] = Join{p.part + way * plane, ways * plane, out, row, p.splits, p.rows, p.cols};
+        fours = plane / 4 > fours ? plane / 4 : fours;
+    };
+    if (want_x && px.splits > 1) join(px, 1, 0, px.out, px.out_row);
+    if (dwg && pw.splits > 1) join(pw, 2, 0, pw.out, pw.out_row), join(pw, 2, 1, pw.out2, pw.out2_row);
+    if (n == 0) return hipSuccess;
+    const int64_t groups = (fours + 255) / 256;
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(groups < OP_CUS * 8 ? groups : OP_CUS * 8), (unsigned)n), dim3(256), 0, s, joins);
     return hipGetLastError();
 }
 
