@@ -57,7 +57,7 @@ __device__ __forceinline__ void put(float* row, int at, int first, const float (
 template <int VEC, int WIDTH>
 __device__ __forceinline__ void take(const float* row, int at, int first, float (&v)[VEC]) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = row[at + i < 0 ? 0 : at + i];  // (those before `first`: whatever stands there, never stored)
+    for (int i = 0; i < VEC; ++i) v[i] = row[at + i < 0 ? 0 : at + i];  // (before the tile: whatever stands there, never stored)
 }
 
 // The map of a chunk, [n][chunks][2][c] (A, B): forward h -> A h + B, backward g -> A g + B from a chunk's end to its start.  Rows have runs of frames of
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
         take<VEC, Z::WIDTH>(ra, me.at - c0, me.first, h);
         if (me.first == VEC) continue;
         if (marks && (row * S) % MARK == 0 && tb + row * S < d.t)
-            store_some<VEC>(marks + ((int64_t)w.video * nm + (tb + row * S) / MARK) * d.c + me.at, h, me.first);
+            store_some<VEC>(marks + ((int64_t)w.video * nm + (tb + row * S) / MARK) * d.c + me.at, h, me.keep);
 #pragma unroll
         for (int k = 0; k < S; ++k) {
             const int t = tb + row * S + k;
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
                 h[i] = a[k][i] * h[i] + b[k][i];
                 o[i] = t < end ? h[i] : 0.0f;
             }
-            if (t < d.t) store_some<VEC>(yp + t * d.y_frame, o, me.first);
+            if (t < d.t) store_some<VEC>(yp + t * d.y_frame, o, me.keep);
         }
     }
     // behind the video's end: zeros, and the last state for the marks
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
         float zero[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) zero[i] = 0.0f;
-        for (int t = tb + row; t < t1; t += Z::ROWS) store_some<VEC>(yp + t * d.y_frame, zero, me.first);
+        for (int t = tb + row; t < t1; t += Z::ROWS) store_some<VEC>(yp + t * d.y_frame, zero, me.keep);
     }
     if (j < width) {
         if (marks)
@@ -236,8 +236,8 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
 #pragma unroll
         for (int i = 0; i < VEC; ++i) zero[i] = 0.0f;
         for (int t = t0 + blocks * BACK_BLOCK + row; t < t1; t += Z::ROWS) {
-            store_some<VEC>(dxp + t * d.dx_frame, zero, me.first);
-            store_some<VEC>(dfp + t * d.df_frame, zero, me.first);
+            store_some<VEC>(dxp + t * d.dx_frame, zero, me.keep);
+            store_some<VEC>(dfp + t * d.df_frame, zero, me.keep);
         }
     }
     Held<T, VEC> rx[S], rf[S], ry[S];
@@ -329,8 +329,8 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
                 h[i] = a[k][i] * h[i] + o[k][i] * v[k][i];
             }
             if (t < d.t) {
-                store_some<VEC>(dxp + t * d.dx_frame, ox, me.first);
-                store_some<VEC>(dfp + t * d.df_frame, of, me.first);
+                store_some<VEC>(dxp + t * d.dx_frame, ox, me.keep);
+                store_some<VEC>(dfp + t * d.df_frame, of, me.keep);
             }
         }
     }

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom
     for (int i = 0; i < VEC; ++i) {
         ga[i] = gamma ? gamma[c + i] : 1.0f;
         be[i] = beta ? beta[c + i] : 0.0f;
-        gi[i] = i < me.first ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
+        gi[i] = i < me.keep ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
         s[0][i] = 0.0f;
     }
 #pragma unroll
@@ -136,16 +136,17 @@ __global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom
             float o[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) o[i] = act_value<decltype(act)::value>((v[j].get(i) - mean[i]) * ga[i] + be[i]);
-            store_some<VEC>(ys + pos * d.y_position, o, me.first);
+            store_some<VEC>(ys + pos * d.y_position, o, me.keep);
         }
     });
 }
 
-// part2: [2][n][c], the samples' sums of dz and of dz * xh.  KEEP: dz stays in registers as well, else its slope is made twice
+// sum1, sum2: [n][c], the samples' sums of dz and of dz * xh.  KEEP: dz stays in registers as well, else its slope is made twice
 template <typename TX, typename TY, int VEC, int P, int THREADS, bool KEEP>
 __global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, HeldGeom h, const TX* __restrict__ x, const float* __restrict__ stats,
                                                             const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                            const TY* __restrict__ dy, TX* __restrict__ dx, float* __restrict__ part2) {
+                                                            const TY* __restrict__ dy, TX* __restrict__ dx, float* __restrict__ sum1,
+                                                            float* __restrict__ sum2) {
     __shared__ float part[2 * THREADS * VEC];
     __shared__ float gs[2][HELD_GROUPS];
     int sample, block;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, Hel
     for (int i = 0; i < VEC; ++i) {
         ga[i] = gamma ? gamma[c + i] : 1.0f;
         be[i] = beta ? beta[c + i] : 0.0f;
-        gi[i] = i < me.first ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
+        gi[i] = i < me.keep ? 0 : (int)(((float)(c - c0 + i) + 0.5f) * h.r_cg);
         mean[i] = st[2 * gi[i]];
         r[i] = st[2 * gi[i] + 1];
         s[0][i] = s[1][i] = 0.0f;
@@ -201,8 +202,8 @@ __global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, Hel
     for (int ch = threadIdx.x; ch < cb; ch += THREADS) {
         float s1 = 0.0f, s2 = 0.0f;
         for (int k = 0; k < rows; ++k) s1 += part[k * cb + ch], s2 += part[STRIDE + k * cb + ch];
-        part2[(int64_t)sample * d.c + c0 + ch] = s1;
-        part2[((int64_t)d.n + sample) * d.c + c0 + ch] = s2;
+        sum1[(int64_t)sample * d.c + c0 + ch] = s1;
+        sum2[(int64_t)sample * d.c + c0 + ch] = s2;
         const float g = gamma ? gamma[c0 + ch] : 1.0f;
         part[ch] = g * s1;
         part[STRIDE + ch] = g * s2;
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, Hel
             const float xh = (v[j].get(i) - mean[i]) * r[i];
             o[i] = r[i] * (ga[i] * dz_of(i, xh) - gp[i] - xh * gq[i]);
         }
-        store_some<VEC>(dxs + pos * d.dx_position, o, me.first);
+        store_some<VEC>(dxs + pos * d.dx_position, o, me.keep);
     };
     if constexpr (KEEP) {
 #pragma unroll
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_apply_kernel(rrm_norm_des
             load_vec<VEC>(xs + p * d.x_position, v);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) v[i] = act_value<decltype(act)::value>((v[i] - mean[i]) * ga[i] + be[i]);
-            store_some<VEC>(ys + p * d.y_position, v, t.me.first);
+            store_vec<VEC>(ys + p * d.y_position, v);  // (channels of the workgroup before too: the same bits)
         }
     });
 }
@@ -455,9 +456,9 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc
         if (i >= t.me.first) part[k * d.c + t.me.at + i] = s[0][i], part[(rows + k) * d.c + t.me.at + i] = s[1][i];
 }
 
-// One workgroup a group of a sample: the slices' sums of each channel, [2][n][c], and the group's means of gamma dz and of gamma dz xh, [n][groups][2]
+// One workgroup a group of a sample: the slices' sums of each channel, sum1 and sum2 [n][c], and the group's means of gamma dz and of gamma dz xh, [n][groups][2]
 __global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, const float* __restrict__ gamma,
-                                                                 float* __restrict__ sums, float* __restrict__ means) {
+                                                                 float* __restrict__ sum1, float* __restrict__ sum2, float* __restrict__ means) {
     __shared__ float lds[JOIN_THREADS / OP_WAVE], rows[2][JOIN_THREADS];
     const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
     const JoinShape j(cg);
@@ -481,8 +482,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d
         if (j.row == 0 && in) {
             s1 = s2 = 0.0f;
             for (int k = 0; k < j.rows; ++k) s1 += rows[0][k * j.lanes + j.lane], s2 += rows[1][k * j.lanes + j.lane];
-            sums[(int64_t)sample * d.c + c] = s1;
-            sums[((int64_t)d.n + sample) * d.c + c] = s2;
+            sum1[(int64_t)sample * d.c + c] = s1;
+            sum2[(int64_t)sample * d.c + c] = s2;
             const float ga = gamma ? gamma[c] : 1.0f;
             p += ga * s1;
             q += ga * s2;
@@ -528,21 +529,22 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_dx_kernel(rrm_norm_desc d
                 act_pair<decltype(act)::value>(ga[i] * xh + be[i], value, slope);
                 v[i] = r[i] * (ga[i] * (w[i] * slope) - gp[i] - xh * gq[i]);
             }
-            store_some<VEC>(dxs + p * d.dx_position, v, t.me.first);
+            store_vec<VEC>(dxs + p * d.dx_position, v);
         }
     });
 }
 
 // dbeta and dgamma: the samples' sums (no samples: zeros).  32 channels a workgroup, 32 threads a channel, joined in their order.
-__global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restrict__ part, int n, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+__global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restrict__ sum1, const float* __restrict__ sum2, int n, int c,
+                                                           float* __restrict__ dgamma, float* __restrict__ dbeta) {
     __shared__ float lds[2][32][32];
     const int ch = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), k = (int)threadIdx.x >> 5;
     float s1 = 0.0f, s2 = 0.0f;
     if (ch < c)
 #pragma unroll 4
         for (int i = k; i < n; i += 32) {
-            s1 += part[(int64_t)i * c + ch];
-            s2 += part[((int64_t)n + i) * c + ch];
+            s1 += sum1[(int64_t)i * c + ch];
+            s2 += sum2[(int64_t)i * c + ch];
         }
     lds[0][k][threadIdx.x & 31] = s1;
     lds[1][k][threadIdx.x & 31] = s2;
@@ -681,7 +683,13 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                                       const float* beta, const void* dy, void* dx, float* dgamma, float* dbeta, void* ws,
                                       hipStream_t s) {
     const bool some = d.n > 0 && d.positions > 0;
-    const float* sums = (const float*)ws;  // [2][n][c]
+    // [n][c] each; of one sample they are the parameters' gradients
+    const bool one = some && d.n == 1;
+    float *sum1 = (float*)ws, *sum2 = nullptr;
+    auto place_sums = [&](float* at) {
+        sum1 = one && dbeta ? dbeta : at;
+        sum2 = one && dgamma ? dgamma : at + (size_t)d.n * d.c;
+    };
     if (some)
         with_types(d, [&](auto tx, auto ty) {
             using TX = decltype(tx);
@@ -692,8 +700,9 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                 constexpr HeldShape h = BACKWARD[decltype(which)::value];
                 // (bfloat16, the largest: there are no registers for dz in 32 bits)
                 constexpr bool KEEP = sizeof(TX) == 4 || h.threads < 1024;
+                place_sums((float*)ws);
                 hipLaunchKernelGGL((held_back_kernel<TX, TY, decltype(vec)::value, h.p, h.threads, KEEP>), dim3(held_grid(d, p)), dim3(h.threads),
-                                   0, s, d, p.g, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, (float*)ws);
+                                   0, s, d, p.g, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, sum1, sum2);
             };
             auto by_vec = [&](auto vec) {
                 constexpr int VEC = decltype(vec)::value;
@@ -707,11 +716,11 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                         const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
                         float* to = (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
                         float* means = (float*)((char*)to + round256((size_t)2 * d.n * d.c * 4));
-                        sums = to;
+                        place_sums(to);
                         hipLaunchKernelGGL((slice_sums_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, (float*)ws);
-                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, gamma, to,
-                                           means);
+                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, gamma,
+                                           sum1, sum2, means);
                         if (!dx) break;
                         hipLaunchKernelGGL((slice_dx_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, means, (TX*)dx);
@@ -721,8 +730,8 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
             p.vec == 1 ? by_vec(std::integral_constant<int, 1>{}) : by_vec(std::integral_constant<int, WIDE>{});
         });
     if (hipError_t e = hipGetLastError()) return e;
-    if (dgamma || dbeta)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, s, sums, some ? d.n : 0, d.c, dgamma, dbeta);
+    if ((dgamma || dbeta) && !one)
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, s, sum1, sum2, some ? d.n : 0, d.c, dgamma, dbeta);
     return hipGetLastError();
 }
 

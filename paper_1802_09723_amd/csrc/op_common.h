@@ -125,16 +125,19 @@ struct Held {  // VEC elements as they lie in memory, at the alignment of one
     }
 };
 
-// A thread's vector of channels: from `at` on, of which those before `first` are another thread's (the last vector of a workgroup whose channels are
-// no whole vectors begins early, which is never before the row: a workgroup has VEC channels at least, or others before it) and not to be summed or stored.  A thread without channels has first = VEC.
+// A thread's vector of channels: from `at` on.  The last vector of a workgroup whose channels are no whole vectors begins early (never before the
+// row: a workgroup has VEC channels at least, or others before it): what it has before `first` is another thread's and not to be
+// summed.  It is to be stored from `keep` on: both threads make the same bits of a channel of their workgroup, and one whole store is
+// cheaper than its elements; not so where the vector reaches into the workgroup before.  A thread without channels has first = keep = VEC.
 template <int VEC>
 struct Span {
-    int at, first;
+    int at, first, keep;
     __device__ __forceinline__ Span(int slot, int c0, int cb) {
         const int c = c0 + slot * VEC, end = c0 + cb - VEC;
         const bool none = slot * VEC >= cb;
         at = none || c > end ? (end > 0 ? end : 0) : c;
         first = none ? VEC : c - at;
+        keep = none ? VEC : at >= c0 ? 0 : first;
     }
 };
 

@@ -210,9 +210,9 @@ def group_norm_act_backward(dy, x, stats, gamma=None, beta=None, act: str = "non
     if dx is None:
         dx = torch.empty_like(x)
     if dgamma is None:
-        dgamma = x.new_empty((c,), dtype=torch.float32)
+        dgamma = x.new_empty((c,), dtype=torch.float32) if gamma is None else torch.empty_like(gamma)
     if dbeta is None:
-        dbeta = x.new_empty((c,), dtype=torch.float32)
+        dbeta = torch.empty_like(dgamma)
     key = ("norm back", act, _look(dy), _look(x), _look(stats), _look(gamma), _look(beta),
            made[0] or _look(dx), made[1] or _look(dgamma), made[2] or _look(dbeta))
     plan = _plans.get(key)

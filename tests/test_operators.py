@@ -397,6 +397,7 @@ FF = [
     # m, k, f
     (1, 1, 1), (1, 64, 64), (1, 4096, 256), (2, 1001, 333), (5, 72, 40), (16, 512, 512), (17, 256, 130), (33, 1000, 96),
     (64, 384, 1024), (100, 65, 67), (128, 128, 128), (129, 136, 264), (200, 1030, 300), (300, 512, 257), (513, 64, 700), (1030, 320, 520),
+    (3000, 72, 104), (2100, 1001, 60), (40, 2500, 1100),  # few tiles over long sums
 ]
 
 
