@@ -47,17 +47,30 @@ struct Place {
     }
 };
 
-// A thread's features among LDS rows of WIDTH: those before `first` are another thread's
-template <int VEC, int WIDTH>
+// A thread's features among those of an LDS row, from `at` on (those before `first` are another thread's); whole vectors in 16-byte pieces
+template <int VEC>
 __device__ __forceinline__ void put(float* row, int at, int first, const float (&v)[VEC]) {
+    if (VEC >= 4 && first == 0) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i)
-        if (i >= first) row[at + i] = v[i];
+        for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4*>(row + at + i) = make_float4(v[i], v[(i + 1) % VEC], v[(i + 2) % VEC], v[(i + 3) % VEC]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i >= first) row[at + i] = v[i];
+    }
 }
-template <int VEC, int WIDTH>
+template <int VEC>
 __device__ __forceinline__ void take(const float* row, int at, int first, float (&v)[VEC]) {
+    if (VEC >= 4 && first == 0) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = row[at + i < 0 ? 0 : at + i];  // (before the tile: whatever stands there, never stored)
+        for (int i = 0; i < VEC; i += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(row + at + i);
+            v[i] = q.x, v[(i + 1) % VEC] = q.y, v[(i + 2) % VEC] = q.z, v[(i + 3) % VEC] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = row[at + i < 0 ? 0 : at + i];  // (before the tile: whatever stands there, never stored)
+    }
 }
 
 // The map of a chunk, [n][chunks][2][c] (A, B): forward h -> A h + B, backward g -> A g + B from a chunk's end to its start.  Rows have runs of frames of
@@ -66,7 +79,8 @@ template <typename T, int VEC, bool BACK>
 __global__ __launch_bounds__(GS_THREADS) void chunk_maps_kernel(rrm_scan_desc d, Cut cut, const T* __restrict__ in, const T* __restrict__ f,
                                                                 const int32_t* __restrict__ lengths, float* __restrict__ maps) {
     using Z = Tile<VEC>;
-    __shared__ float sa[Z::ROWS * Z::WIDTH], sb[Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sa[Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sb[Z::ROWS * Z::WIDTH];
     Place w(cut, cut.chunks - 1);  // (forward nobody asks for the last chunk's map, backward for the first's)
     if (BACK) ++w.chunk;
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES;
@@ -94,8 +108,8 @@ __global__ __launch_bounds__(GS_THREADS) void chunk_maps_kernel(rrm_scan_desc d,
                         : a * B[i] + o * v[i];
         }
     }
-    put<VEC, Z::WIDTH>(sa + row * Z::WIDTH, me.at - c0, me.first, A);
-    put<VEC, Z::WIDTH>(sb + row * Z::WIDTH, me.at - c0, me.first, B);
+    put<VEC>(sa + row * Z::WIDTH, me.at - c0, me.first, A);
+    put<VEC>(sb + row * Z::WIDTH, me.at - c0, me.first, B);
     __syncthreads();
     const int j = (int)threadIdx.x;
     if (j >= width) return;
@@ -111,13 +125,43 @@ __global__ __launch_bounds__(GS_THREADS) void chunk_maps_kernel(rrm_scan_desc d,
     to[d.c] = s;
 }
 
+// Thread j < width: `start` through the maps of `count` chunks, the first at `first`, the next `step` on (in floats).  The threads take a stretch of
+// chunks of a feature each, and the stretches' maps meet in LDS: some hundred maps one after the other would be as many trips to memory
+// (1 x 27594 x 80 fp32, forward and backward: 94 us so, 43 with stretches).
+template <int WIDTH>
+__device__ __forceinline__ float carried(const float* __restrict__ first, int64_t step, int count, int c, int width, float start, float* sa, float* sb) {
+    if (count == 0) return start;
+    constexpr int SEGS = GS_THREADS / WIDTH;
+    const int j = (int)threadIdx.x % WIDTH, seg = (int)threadIdx.x / WIDTH;
+    const int k0 = count * seg / SEGS, k1 = count * (seg + 1) / SEGS;
+    float A = 1.0f, B = 0.0f;
+    if (j < width) {
+#pragma unroll 8
+        for (int k = k0; k < k1; ++k) {
+            const float ma = first[k * step + j], mb = first[k * step + c + j];
+            A *= ma;
+            B = ma * B + mb;
+        }
+    }
+    sa[threadIdx.x] = A;
+    sb[threadIdx.x] = B;
+    lds_barrier();
+    if (seg == 0) {
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k) start = sa[k * WIDTH + j] * start + sb[k * WIDTH + j];
+    }
+    lds_barrier();
+    return start;
+}
+
 template <typename T, int VEC>
 __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut cut, const T* __restrict__ x, const T* __restrict__ f, const float* h0,
                                                           const int32_t* __restrict__ lengths, const float* __restrict__ maps, T* __restrict__ y,
                                                           float* h_last, float* __restrict__ marks) {
     using Z = Tile<VEC>;
     constexpr int S = Z::SPAN;
-    __shared__ float sa[2][Z::ROWS * Z::WIDTH], sb[2][Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sa[2][Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sb[2][Z::ROWS * Z::WIDTH];
     const Place w(cut, cut.chunks);
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
@@ -139,12 +183,8 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
     const int live = min(t1, end);  // frames from here on are zeros
     if (t0 < live) fetch(t0);
     float carry = 0.0f;  // thread j: the state of feature c0 + j before the block
-    if (j < width) {
-        carry = h0 ? h0[(int64_t)w.video * d.c + c0 + j] : 0.0f;
-        const float* m = maps + (int64_t)w.video * cut.chunks * 2 * d.c + c0 + j;
-#pragma unroll 8
-        for (int q = 0; q < w.chunk; ++q) carry = m[(int64_t)q * 2 * d.c] * carry + m[((int64_t)q * 2 + 1) * d.c];
-    }
+    if (j < width && h0) carry = h0[(int64_t)w.video * d.c + c0 + j];
+    carry = carried<Z::WIDTH>(maps + (int64_t)w.video * cut.chunks * 2 * d.c + c0, 2 * (int64_t)d.c, w.chunk, d.c, width, carry, sa[0], sb[0]);
     int buf = 0;
     int tb = t0;
     for (; tb < live; tb += GS_BLOCK, buf ^= 1) {
@@ -166,8 +206,8 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
         }
         if (tb + GS_BLOCK < live) fetch(tb + GS_BLOCK);
         float *ra = sa[buf] + row * Z::WIDTH, *rb = sb[buf] + row * Z::WIDTH;
-        put<VEC, Z::WIDTH>(ra, me.at - c0, me.first, A);
-        put<VEC, Z::WIDTH>(rb, me.at - c0, me.first, B);
+        put<VEC>(ra, me.at - c0, me.first, A);
+        put<VEC>(rb, me.at - c0, me.first, B);
         lds_barrier();
         if (j < width) {
 #pragma unroll 8
@@ -179,7 +219,7 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
         }
         lds_barrier();
         float h[VEC];
-        take<VEC, Z::WIDTH>(ra, me.at - c0, me.first, h);
+        take<VEC>(ra, me.at - c0, me.first, h);
         if (me.first == VEC) continue;
         if (marks && (row * S) % MARK == 0 && tb + row * S < d.t)
             store_some<VEC>(marks + ((int64_t)w.video * nm + (tb + row * S) / MARK) * d.c + me.at, h, me.keep);
@@ -212,13 +252,15 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, Cut c
 constexpr int BACK_BLOCK = 64;  // frames of a block of the backward pass: it holds four values a frame
 
 template <typename T, int VEC>
-__global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, Cut cut, const T* __restrict__ x, const T* __restrict__ f,
+__global__ __launch_bounds__(GS_THREADS, 3) void scan_back_kernel(rrm_scan_desc d, Cut cut, const T* __restrict__ x, const T* __restrict__ f,
                                                                const float* __restrict__ marks, const int32_t* __restrict__ lengths,
                                                                const T* __restrict__ dy, const float* dh_last, const float* __restrict__ maps,
                                                                T* __restrict__ dx, T* __restrict__ df, float* dh0) {
     using Z = Tile<VEC, BACK_BLOCK>;
     constexpr int S = Z::SPAN, MARKS = BACK_BLOCK / MARK, MROWS = Z::ROWS / MARKS;
-    __shared__ float sa[Z::ROWS * Z::WIDTH], sb[Z::ROWS * Z::WIDTH], sg[Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sa[Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sb[Z::ROWS * Z::WIDTH];
+    __shared__ __attribute__((aligned(16))) float sg[Z::ROWS * Z::WIDTH];
     const Place w(cut, cut.chunks);
     const int c0 = w.tile * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
@@ -252,12 +294,9 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
     };
     if (blocks) fetch(t0 + (blocks - 1) * BACK_BLOCK);
     float carry = 0.0f;  // thread j: the gradient of the state behind the block, of feature c0 + j
-    if (j < width) {
-        carry = dh_last ? dh_last[(int64_t)w.video * d.c + c0 + j] : 0.0f;
-        const float* m = maps + (int64_t)w.video * cut.chunks * 2 * d.c + c0 + j;
-#pragma unroll 8
-        for (int q = cut.chunks - 1; q > w.chunk; --q) carry = m[(int64_t)q * 2 * d.c] * carry + m[((int64_t)q * 2 + 1) * d.c];
-    }
+    if (j < width && dh_last) carry = dh_last[(int64_t)w.video * d.c + c0 + j];
+    carry = carried<Z::WIDTH>(maps + ((int64_t)(w.video + 1) * cut.chunks - 1) * 2 * d.c + c0, -2 * (int64_t)d.c, cut.chunks - 1 - w.chunk, d.c, width,
+                              carry, sa, sb);
     for (int blk = blocks - 1; blk >= 0; --blk) {
         const int tb = t0 + blk * BACK_BLOCK;
         float a[S][VEC], o[S][VEC], v[S][VEC], g[S][VEC], A[VEC], B[VEC], G[VEC];
@@ -280,9 +319,9 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
         }
         if (blk > 0) fetch(tb - BACK_BLOCK);
         lds_barrier();  // (the rows have been handed their states of the block before)
-        put<VEC, Z::WIDTH>(sa + row * Z::WIDTH, me.at - c0, me.first, A);
-        put<VEC, Z::WIDTH>(sb + row * Z::WIDTH, me.at - c0, me.first, B);
-        put<VEC, Z::WIDTH>(sg + row * Z::WIDTH, me.at - c0, me.first, G);
+        put<VEC>(sa + row * Z::WIDTH, me.at - c0, me.first, A);
+        put<VEC>(sb + row * Z::WIDTH, me.at - c0, me.first, B);
+        put<VEC>(sg + row * Z::WIDTH, me.at - c0, me.first, G);
         lds_barrier();
         // gradients by the first threads, states by those behind them, each from its mark
         if (j < width) {
@@ -308,8 +347,8 @@ __global__ __launch_bounds__(GS_THREADS) void scan_back_kernel(rrm_scan_desc d, 
         lds_barrier();
         if (me.first == VEC) continue;
         float h[VEC], gr[VEC];
-        take<VEC, Z::WIDTH>(sb + row * Z::WIDTH, me.at - c0, me.first, h);
-        take<VEC, Z::WIDTH>(sg + row * Z::WIDTH, me.at - c0, me.first, gr);
+        take<VEC>(sb + row * Z::WIDTH, me.at - c0, me.first, h);
+        take<VEC>(sg + row * Z::WIDTH, me.at - c0, me.first, gr);
         // g to the end of the row first, then states from its start
 #pragma unroll
         for (int k = S - 1; k >= 0; --k)
