@@ -331,7 +331,7 @@ rrm_status rrm_group_norm_act_backward(const rrm_norm_desc* desc, const void* x,
  * y, dx and df are 0 there, and h_last is the state after its last frame (h0 for a video of no frames).
  * One frame of live videos is t = 1, with h0 the state before and h_last the state after it; there h_last may be h0. */
 typedef struct {
-    int n, t, c; /* each may be 0 */
+    int n, t, c; /* each may be 0; t at most 2^31 - 256 */
     int elem;    /* rrm_elem of x, f, y and their gradients */
     int64_t x_video, x_frame, f_video, f_frame, y_video, y_frame; /* strides; dy lies by those of y */
     int64_t dx_video, dx_frame, df_video, df_frame;

@@ -55,6 +55,7 @@ rrm_status check(const rrm_scan_desc* d) {
     if (!d) return record_failure(RRM_ERR_NULL, "desc is NULL");
     if (d->elem < RRM_F32 || d->elem > RRM_BF16) return record_failure(RRM_ERR_DTYPE, "gated scan: elements are RRM_F32 or RRM_BF16");
     if (d->n < 0 || d->t < 0 || d->c < 0) return record_failure(RRM_ERR_SHAPE, "gated scan: n, t, c must not be negative");
+    if (d->t > 0x7fffff00) return record_failure(RRM_ERR_SHAPE, "gated scan: t is at most 2^31 - 256");
     if ((int64_t)d->n * d->c > 0x7fffffff) return record_failure(RRM_ERR_SHAPE, "gated scan: n * c must fit 31 bits");
     return RRM_OK;
 }

@@ -316,6 +316,46 @@ def test_scan_of_many_frames(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(4, 5000, 130), (3, 4224, 9), (1, 9001, 5)])
+def test_scan_of_one_video_by_many_workgroups(shape, dtype):
+    """The state is handed on between workgroups: the same bits in every call, and those of pieces of the video but for roundings; videos end at
+    the borders of what a workgroup takes, in it, at once."""
+    n, t, c = shape
+    x, f, h0, _ = scan_inputs(n, t, c, dtype, False)
+    ends = [t, 128 * 32, 0, 64 * 33][:n]
+    lengths = torch.tensor(ends, dtype=torch.int32).cuda()
+    xd, fd, hd = x.cuda(), f.cuda(), h0.cuda()
+    dy, dh = torch.randn(n, t, c, generator=gen(5)).to(DT[dtype]).cuda(), torch.randn(n, c, generator=gen(6)).cuda()
+    first = None
+    for _ in range(4):
+        marks = rrm.gated_scan_marks(xd)
+        y, last = rrm.gated_scan(xd, fd, hd, lengths=lengths, marks=marks)
+        got = (y, last, marks, *rrm.gated_scan_backward(dy, xd, fd, marks, lengths=lengths, dh_last=dh))
+        if first is None:
+            first = [v.clone() for v in got]
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    slack = 5 * (SUM + 2 * U * 64 + GATE) * 2
+    for i, end in enumerate(ends):
+        h = hd[i:i + 1]
+        assert not first[0][i, end:].any() and not first[3][i, end:].any() and not first[4][i, end:].any()
+        for k in range(0, end, 500):
+            e = min(end, k + 500)
+            piece, h = rrm.gated_scan(xd[i:i + 1, k:e], fd[i:i + 1, k:e], h)
+            check(first[0][i:i + 1, k:e], piece.double().cpu(), slack + (2 ** -8 * 5 if dtype == "bf16" else 0), "y")
+        check(first[1][i:i + 1], h.double().cpu(), slack, "h_last")
+        g = dh[i:i + 1]
+        for k in reversed(range(0, end, 320)):  # (whole marks)
+            e = min(end, k + 320)
+            part = [v[i:i + 1, k:e].contiguous() for v in (dy, xd, fd)]
+            dx, df, g = rrm.gated_scan_backward(*part, first[2][i:i + 1, k // 64:(e - 1) // 64 + 1].contiguous(), dh_last=g)
+            gs = slack * 20 + (2 ** -8 * 20 if dtype == "bf16" else 0)
+            check(first[3][i:i + 1, k:e], dx.double().cpu(), gs, "dx")
+            check(first[4][i:i + 1, k:e], df.double().cpu(), gs * 10, "df")
+        check(first[5][i:i + 1], g.double().cpu(), slack * 20, "dh0")
+
+
+@gpu
 def test_scan_gates_at_their_ends():
     """Gates of 0 and 1 from infinite and far logits: the state is x_t, or h_{t-1}, without an error; gradients stay finite."""
     x = torch.randn(1, 6, 8, generator=gen(1))
@@ -752,7 +792,7 @@ def test_refusals_come_back_as_status_codes():
 
     assert L.rrm_gated_scan(None, P, P, None, None, P, None, None, P, big, None) == -1
     assert scan(x=None) == -1 and scan(f=None) == -1 and scan(y=None) == -1
-    assert scan(t=-1) == -2 and scan(n=-1) == -2 and scan(c=-1) == -2 and scan(n=1 << 28, c=1 << 4) == -2
+    assert scan(t=-1) == -2 and scan(n=-1) == -2 and scan(c=-1) == -2 and scan(n=1 << 28, c=1 << 4) == -2 and scan(n=1, t=0x7fffffff, c=1) == -2
     assert scan(elem=2) == -3 and scan(y_frame=7) == -2 and scan(y_video=8) == -2
     assert scan(f=P + 2) == -9 and scan(lengths=P + 2) == -9
     assert scan(h0=P, last=P) == -6
