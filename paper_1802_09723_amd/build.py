@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -26,13 +28,22 @@ FLAGS = [
 
 
 def build_lib(verbose: bool = False) -> str:
+    """A source file a compiler, as many at once as MAX_JOBS (or the CPUs) allow, then one link."""
     os.makedirs(LIBDIR, exist_ok=True)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    jobs = max(1, min(len(SOURCES), int(os.environ.get("MAX_JOBS", "0") or 0) or len(os.sched_getaffinity(0))))
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory(prefix="rrm_build_") as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"] + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+        with ThreadPoolExecutor(jobs) as pool:
+            list(pool.map(lambda so: run([hipcc] + compile_flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]]), zip(SOURCES, objects)))
+        run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB])
     return LIB
 
 
