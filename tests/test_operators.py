@@ -629,6 +629,44 @@ def test_operators_on_a_stream_of_their_own_and_in_a_graph():
 
 
 @gpu
+def test_scans_that_hand_on_their_state_on_two_streams_and_in_a_graph():
+    """Long videos, whose blocks wait for one another: two calls at once on streams of their own, and a captured pass, both ways, replayed over
+    changing inputs with the same calls between the replays; strided inputs, not-a-numbers behind the ends."""
+    n, t, c = 3, 3000, 72
+    x, f, h0, _ = scan_inputs(n, t, 2 * c, "bf16", False)
+    ends = [t, 1000, 0]
+    for i, end in enumerate(ends):
+        x[i, end:], f[i, end:] = math.nan, math.inf
+    lengths = torch.tensor(ends, dtype=torch.int32).cuda()
+    xd, fd, hd = x.cuda()[:, :, c:], f.cuda()[:, :, :c], h0.cuda()[:, :c].contiguous()
+    dy = torch.randn(n, t, c, generator=gen(8)).bfloat16().cuda()
+
+    def both(stream=None):
+        marks = rrm.gated_scan_marks(xd)
+        y, last = rrm.gated_scan(xd, fd, hd, lengths=lengths, marks=marks, stream=stream)
+        return (y, last, marks, *rrm.gated_scan_backward(dy, xd, fd, marks, lengths=lengths, stream=stream))
+
+    want = [v.clone() for v in both()]
+    assert all(torch.isfinite(v).all() for v in want)
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [both(s) for _ in range(5) for s in sides]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for k in range(4):
+        xd.copy_(torch.randn(n, t, c, generator=gen(k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in held]
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
 def test_the_example_runs_them_together():
     """The live path against plain torch in 64 bits on the same parameters and frames; training brings the loss down."""
     import importlib.util
