@@ -21,6 +21,7 @@ namespace {
 
 constexpr int GS_THREADS = 256;
 constexpr int GS_BLOCK = 128;  // frames of a block
+constexpr int LONG_BLOCK = 256;  // of long fp32 videos: see forward_block
 constexpr int MARK = RRM_SCAN_MARK_FRAMES;
 static_assert(GS_BLOCK % MARK == 0, "blocks begin at marks");
 
@@ -275,12 +276,12 @@ __global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, int t
     }
 }
 
-// Many workgroups a chain: four a compute unit hide each other's waits (128 registers).
-template <typename T, int VEC>
-__global__ __launch_bounds__(GS_THREADS, 4) void chained_scan_kernel(rrm_scan_desc d, Chain ch, const T* __restrict__ x, const T* __restrict__ f,
+// Many workgroups a chain: four a compute unit hide each other's waits (128 registers; two with long blocks).
+template <typename T, int VEC, int FRAMES>
+__global__ __launch_bounds__(GS_THREADS, FRAMES == GS_BLOCK ? 4 : 2) void chained_scan_kernel(rrm_scan_desc d, Chain ch, const T* __restrict__ x, const T* __restrict__ f,
                                                                      const float* h0, const int32_t* __restrict__ lengths, T* __restrict__ y,
                                                                      float* h_last, float* __restrict__ marks) {
-    using Z = Tile<VEC>;
+    using Z = Tile<VEC, FRAMES>;
     constexpr int S = Z::SPAN, W = Z::WIDTH;
     __shared__ __attribute__((aligned(16))) float sa[Z::ROWS * W];
     __shared__ __attribute__((aligned(16))) float sb[Z::ROWS * W];
@@ -365,12 +366,12 @@ __global__ __launch_bounds__(GS_THREADS, 4) void chained_scan_kernel(rrm_scan_de
     __shared__ int sk;
     word_t* maps = ch.maps + (int64_t)chain * ch.blocks * W;
     word_t* states = ch.states + (int64_t)chain * ch.groups * W;
-    const int last = end > 0 ? (end - 1) / GS_BLOCK : 0;
+    const int last = end > 0 ? (end - 1) / FRAMES : 0;
     for (int k; (k = next_block(ch.counters + chain * 16, &sk)) < ch.blocks;) {
         asm volatile("" : "+v"(row));  // (what hangs on it is made in each block, not kept in registers over all)
-        const int tb = k * GS_BLOCK;
+        const int tb = k * FRAMES;
         if (k > last) {
-            zeros(tb, min(tb + GS_BLOCK, d.t));
+            zeros(tb, min(tb + FRAMES, d.t));
             continue;
         }
         fetch(tb);
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(GS_THREADS, 4) void chained_scan_kernel(rrm_scan_de
             const float after = am * state + bm;
             if (k < last && k % GROUP == GROUP - 1) put_word(states + (int64_t)(k / GROUP) * W + j, 0u, after);
             sh[j] = state;
-            if (k == last) leave(tb + GS_BLOCK, after);
+            if (k == last) leave(tb + FRAMES, after);
         }
         lds_barrier();
         float h[VEC], pa[VEC], pb[VEC];
@@ -784,6 +785,11 @@ struct Plan {
     }
 };
 
+// Frames of a block of the forward pass.  Long fp32 videos go in long blocks, half as many hands (us, blocks of 128 and 256 frames: fp32 1 x 65536 x
+// 512 105 and 96, x 256 46 and 42, x 32 24 and 17, 1 x 40000 x 1024 117 and 110; 1 x 8000 x 512 15.2 and 15.2, 8 x 4096 x 1024 98 and 100; bf16 1 x 65536
+// x 512 59 and 63, 1 x 40000 x 2048 134 and 139).
+int forward_block(const rrm_scan_desc& d) { return d.elem == RRM_F32 && d.t >= 16384 ? LONG_BLOCK : GS_BLOCK; }
+
 // f(element, VEC)
 template <typename F>
 void with_shape(const rrm_scan_desc& d, F&& f) {
@@ -797,7 +803,7 @@ void with_shape(const rrm_scan_desc& d, F&& f) {
 
 size_t scan_scratch(const rrm_scan_desc& d, bool backward) {
     if (d.n == 0 || d.t == 0 || d.c == 0 || (!backward && few_frames(d))) return 0;
-    return round256((size_t)Plan(d, backward ? BACK_BLOCK : GS_BLOCK, nullptr).words * sizeof(word_t));
+    return round256((size_t)Plan(d, backward ? BACK_BLOCK : forward_block(d), nullptr).words * sizeof(word_t));
 }
 
 hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* f, const float* h0, const int32_t* lengths,
@@ -815,11 +821,19 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
                                (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
             return;
         }
-        const Plan p(d, GS_BLOCK, ws);
+        const int frames = forward_block(d);
+        const Plan p(d, frames, ws);
         p.clear(s);
-        if (p.chained)
-            hipLaunchKernelGGL((chained_scan_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch, (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
-        else
+        auto chained = [&](auto block) {
+            hipLaunchKernelGGL((chained_scan_kernel<T, VEC, decltype(block)::value>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch, (const T*)x, (const T*)f, h0,
+                               lengths, (T*)y, h_last, marks);
+        };
+        if (p.chained) {
+            if constexpr (sizeof(T) == 4) {
+                if (frames == LONG_BLOCK) return chained(std::integral_constant<int, LONG_BLOCK>{});
+            }
+            chained(std::integral_constant<int, GS_BLOCK>{});
+        } else
             hipLaunchKernelGGL((scan_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch.tiles, (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
     });
     return hipGetLastError();
