@@ -83,15 +83,16 @@ __device__ __forceinline__ u32x4 ragged_chunk(src_t row, int k, int len) {
 //
 // A workgroup of WM x WN wavefronts makes (32 MT WM) x (32 NT WN) results.  Operands go from memory to LDS directly, 64 of the summed axis at
 // a time, STAGES steps ahead; a wavefront reads a fragment for each of its MT + NT rows of blocks and multiplies MT x NT pairs of them.  With 256 x 256
-// results (4 x 2 blocks of 2 x 4 wavefronts) that is 128 bytes from memory for 64 Ki multiplications a step, and 3/4 read from LDS for each product.
+// results (4 x 2 blocks of 2 x 4 wavefronts) that is a byte copied for 64 multiplications, and 3/4 of a fragment read from LDS for each product.
 // What feeds the matrix cores without a pause: fragments of the next 16 are read between the products of these; copies are started in
 // parts between products; one barrier a step, before its last quarter, so that the next step's first fragments are there when it ends; LDS
 // turned so that reads meet different banks (conflicts 6% of its busy cycles; half without).
 //
 // Measured, 16384 x 4096 rows x 4096 features of each projection: 955 us forward with G and U kept, 1.15 PFLOP/s; dX 910 us, 1.21; both dW 890
-// us, 1.24.  A library's plain products of these shapes, nothing fused, reach 1.40, 1.23 and 1.10 PFLOP/s.  Matrix cores busy 65% of the cycles, at
-// the 1.7 GHz that the card holds under them; what remains is the barrier and the first and last steps.  Four wavefronts of 128 x 128 results
-// took 932 us where eight took 900, and a raised wave priority and non-temporal results changed nothing.
+// us, 1.24.  A library's plain products of these shapes, nothing fused, reach 1.40, 1.23 and 1.10 PFLOP/s.  The matrix cores
+// are busy 69% of the cycles, at the 1.67 GHz that the card's power allows: on rows of equal values the same program runs at 2.0 GHz and takes 732 us,
+// and 4% fewer cycles, all operands being in the nearest caches.  Four wavefronts of 128 x 128 results took 932 us where eight took 900; a raised
+// wave priority, non-temporal results and copies spread one by one between the products changed nothing.
 template <int MT, int NT, int WM, int WN, int STAGES>
 constexpr int TILE_LDS = STAGES * (MT * 32 * WM + NT * 32 * WN) * STEP * 2;
 
@@ -583,8 +584,8 @@ __global__ __launch_bounds__(256) void pad_kernel(PadJob j) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < j.first[j.n]; i += (int64_t)gridDim.x * 256) pad_chunk(j, i);
 }
 
-// dG and dU from dH, G and U (16384 x 4096: 136 us, 4.9 TB/s); rows of `pitch` elements, a multiple of eight, zeros behind column f (they are summed over), eight columns a
-// thread; then the padded copies that the products need.
+// dG and dU from dH, G and U (16384 x 4096: 136 us, 4.9 TB/s); rows of `pitch` elements, a multiple of eight, zeros behind column f (they are
+// summed over), eight columns a thread; then the padded copies that the products need.
 template <int ACT>
 __global__ __launch_bounds__(256) void slopes_kernel(rrm_ff_desc d, src_t g, src_t u, src_t dh, int pitch, __bf16* __restrict__ dg, __bf16* __restrict__ du,
                                                      PadJob job) {

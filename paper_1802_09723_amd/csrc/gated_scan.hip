@@ -10,7 +10,7 @@
 //
 // States, maps and gradients of states are held in 32 bits; only results are rounded.  What bounds it is memory: x, f and y (backward x, f,
 // dy, dx and df) once, with a handful of operations an element.  Measured: 64 x 256 x 4096 bf16, a workgroup a chain, 88 us, 4.6 TB/s;
-// 1 x 65536 x 512 fp32, many workgroups a chain, 101 us, 4.0 TB/s (a card's copy: 5.1); backward, 4 x 4096 x 4096 bf16, 180 us, 3.7 TB/s.
+// 1 x 65536 x 512 fp32, many workgroups a chain, 93 us, 4.3 TB/s (a copy: 5.1); backward, 4 x 4096 x 4096 bf16, 170 us, 4.0 TB/s.
 #include <algorithm>
 
 #include "op_common.h"
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(GS_THREADS, FRAMES == GS_BLOCK ? 4 : 2) void chaine
     }
 }
 
-constexpr int BACK_BLOCK = 64;  // frames of a block of the backward pass: it holds four values a frame
+constexpr int BACK_BLOCK = 64;  // frames of a block where a workgroup has a chain: it holds four values a frame
 
 template <typename T, int VEC>
 __global__ __launch_bounds__(GS_THREADS, 3) void scan_back_kernel(rrm_scan_desc d, int tiles, const T* __restrict__ x, const T* __restrict__ f,
@@ -537,9 +537,9 @@ __global__ __launch_bounds__(GS_THREADS, 3) void chained_scan_back_kernel(rrm_sc
                                                                           const float* __restrict__ marks, const int32_t* __restrict__ lengths,
                                                                           const T* __restrict__ dy, const float* dh_last, T* __restrict__ dx,
                                                                           T* __restrict__ df, float* dh0) {
-    using Z = Tile<VEC, BACK_BLOCK>;
+    using Z = Tile<VEC, GS_BLOCK>;
     constexpr int S = Z::SPAN, W = Z::WIDTH;
-    static_assert(BACK_BLOCK == MARK, "a block has the state before it");
+    static_assert(GS_BLOCK % MARK == 0 && (GS_BLOCK / MARK + 1) * 8 * VEC <= GS_THREADS, "a thread for each state kept in a block");
     __shared__ __attribute__((aligned(16))) float sa[Z::ROWS * W];
     __shared__ __attribute__((aligned(16))) float sb[Z::ROWS * W];
     __shared__ __attribute__((aligned(16))) float sg[Z::ROWS * W];
@@ -601,13 +601,14 @@ __global__ __launch_bounds__(GS_THREADS, 3) void chained_scan_back_kernel(rrm_sc
         put<VEC>(sb + row * W, me.at - c0, me.first, B);
         put<VEC>(sg + row * W, me.at - c0, me.first, G);
     };
-    // a block's states from its mark, by the threads behind the first W
+    // a block's states from its marks, by the threads behind the first W
     auto states_of_rows = [&](int tb) __attribute__((always_inline)) {
-        const int c = j - W;
-        if (c >= 0 && c < width && tb < end) {
-            float h = mp[(int64_t)(tb / MARK) * d.c + c0 + c];
+        constexpr int EACH = Z::ROWS * MARK / GS_BLOCK;  // rows of a mark
+        const int m = j / W - 1, c = j % W;
+        if (m >= 0 && m < GS_BLOCK / MARK && c < width && tb + m * MARK < end) {
+            float h = mp[(int64_t)(tb / MARK + m) * d.c + c0 + c];
 #pragma unroll 8
-            for (int r = 0; r < Z::ROWS; ++r) {
+            for (int r = m * EACH; r < (m + 1) * EACH; ++r) {
                 const float ma = sa[r * W + c], mb = sb[r * W + c];
                 sb[r * W + c] = h;
                 h = ma * h + mb;
@@ -663,15 +664,15 @@ __global__ __launch_bounds__(GS_THREADS, 3) void chained_scan_back_kernel(rrm_sc
     __shared__ int sk;
     word_t* maps = ch.maps + (int64_t)chain * ch.blocks * W;
     word_t* states = ch.states + (int64_t)chain * ch.groups * W;
-    const int last = end > 0 ? (end - 1) / BACK_BLOCK : 0;
+    const int last = end > 0 ? (end - 1) / GS_BLOCK : 0;
     for (int k; (k = next_block(ch.counters + chain * 16, &sk)) < ch.blocks;) {
         asm volatile("" : "+v"(row));  // (what hangs on it is made in each block, not kept in registers over all)
         if (k > last) {  // blocks behind the end come after those with frames: nobody waits for them
-            const int tb = k * BACK_BLOCK;
-            zeros(tb, min(tb + BACK_BLOCK, d.t));
+            const int tb = k * GS_BLOCK;
+            zeros(tb, min(tb + GS_BLOCK, d.t));
             continue;
         }
-        const int tb = (last - k) * BACK_BLOCK;  // (the chain's k-th block is the k-th from the end)
+        const int tb = (last - k) * GS_BLOCK;  // (the chain's k-th block is the k-th from the end)
         fetch(tb);
         rows(tb);
         rows_to_lds();
@@ -753,21 +754,26 @@ __global__ __launch_bounds__(256) void zero_words_kernel(word_t* p, int64_t n) {
 int vec_of(const rrm_scan_desc& d) { return d.elem == RRM_F32 ? (d.c >= 4 ? 4 : 1) : (d.c >= 8 ? 8 : 1); }
 bool few_frames(const rrm_scan_desc& d) { return d.t <= 16; }
 
-// Chains of `frames` a block, and where their words lie in the workspace.  A chain has one workgroup where it has few blocks (us, one workgroup and
-// many, 2 x t x 512 bf16 forward: t = 384 12 and 15, 768 21 and 15; the words have to be cleared first) or where chains fill the card by
-// themselves (4096 frames of 4096 features bf16, forward, and forward and backward: 256 chains 127 and 344, many 100 and 282; 384 chains 151 and 425,
-// many 148 and 418; 448 chains 161 and 440, many 169 and 486).
+// Frames of a block of the forward pass.  Long fp32 videos go in long blocks, half as many hands (us, blocks of 128 and 256 frames: fp32 1 x 65536 x
+// 512 105 and 96, x 256 46 and 42, x 32 24 and 17, 1 x 40000 x 1024 117 and 110; 1 x 8000 x 512 15.2 and 15.2, 8 x 4096 x 1024 98 and 100; bf16 1 x 65536
+// x 512 59 and 63, 1 x 40000 x 2048 134 and 139).
+int forward_block(const rrm_scan_desc& d) { return d.elem == RRM_F32 && d.t >= 16384 ? LONG_BLOCK : GS_BLOCK; }
+
+// A call's chains, and where their words lie in the workspace.  A chain has one workgroup where it has few frames (us, one workgroup and many: forward
+// 2 x t x 512 bf16, t = 384 12 and 15, 768 21 and 15; backward 1 x t x 512 bf16, t = 200 16 and 16, 260 19 and 15, 520 30 and 15; the words have to be
+// cleared first) or where chains fill the card by themselves (n x 4096 x 4096 bf16, 64 chains each: forward n = 4 127 and 100, 6 151 and 148, 7 161 and
+// 169; backward n = 4 224 and 170, 6 279 and 248, 7 284 and 286).
 struct Plan {
     Chain ch;
     int64_t chains, words;  // of the workspace, the counters at its head included
     bool chained;
-    Plan(const rrm_scan_desc& d, int frames, void* ws) {
+    Plan(const rrm_scan_desc& d, bool backward, void* ws) {
         const int v = vec_of(d), width = v * Tile<1>::LANES;
         ch.tiles = (d.c + width - 1) / width;
-        ch.blocks = (d.t - 1) / frames + 1;
+        ch.blocks = (d.t - 1) / (backward ? GS_BLOCK : forward_block(d)) + 1;
         ch.groups = (ch.blocks - 1) / GROUP + 1;
         chains = (int64_t)d.n * ch.tiles;
-        chained = chains < 3 * OP_CUS / 2 && ch.blocks > 5;
+        chained = chains <= 3 * OP_CUS / 2 && d.t > (backward ? 2 : 5) * GS_BLOCK;
         ch.per = 1;
         if (chained) {
             const int64_t want = (8 * OP_CUS + chains - 1) / chains;
@@ -785,11 +791,6 @@ struct Plan {
     }
 };
 
-// Frames of a block of the forward pass.  Long fp32 videos go in long blocks, half as many hands (us, blocks of 128 and 256 frames: fp32 1 x 65536 x
-// 512 105 and 96, x 256 46 and 42, x 32 24 and 17, 1 x 40000 x 1024 117 and 110; 1 x 8000 x 512 15.2 and 15.2, 8 x 4096 x 1024 98 and 100; bf16 1 x 65536
-// x 512 59 and 63, 1 x 40000 x 2048 134 and 139).
-int forward_block(const rrm_scan_desc& d) { return d.elem == RRM_F32 && d.t >= 16384 ? LONG_BLOCK : GS_BLOCK; }
-
 // f(element, VEC)
 template <typename F>
 void with_shape(const rrm_scan_desc& d, F&& f) {
@@ -803,7 +804,7 @@ void with_shape(const rrm_scan_desc& d, F&& f) {
 
 size_t scan_scratch(const rrm_scan_desc& d, bool backward) {
     if (d.n == 0 || d.t == 0 || d.c == 0 || (!backward && few_frames(d))) return 0;
-    return round256((size_t)Plan(d, backward ? BACK_BLOCK : forward_block(d), nullptr).words * sizeof(word_t));
+    return round256((size_t)Plan(d, backward, nullptr).words * sizeof(word_t));
 }
 
 hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* f, const float* h0, const int32_t* lengths,
@@ -821,8 +822,7 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
                                (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
             return;
         }
-        const int frames = forward_block(d);
-        const Plan p(d, frames, ws);
+        const Plan p(d, false, ws);
         p.clear(s);
         auto chained = [&](auto block) {
             hipLaunchKernelGGL((chained_scan_kernel<T, VEC, decltype(block)::value>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch, (const T*)x, (const T*)f, h0,
@@ -830,7 +830,7 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
         };
         if (p.chained) {
             if constexpr (sizeof(T) == 4) {
-                if (frames == LONG_BLOCK) return chained(std::integral_constant<int, LONG_BLOCK>{});
+                if (forward_block(d) == LONG_BLOCK) return chained(std::integral_constant<int, LONG_BLOCK>{});
             }
             chained(std::integral_constant<int, GS_BLOCK>{});
         } else
@@ -850,7 +850,7 @@ hipError_t launch_gated_scan_backward(const rrm_scan_desc& d, const void* x, con
     with_shape(d, [&](auto t, auto vec) {
         using T = decltype(t);
         constexpr int VEC = decltype(vec)::value;
-        const Plan p(d, BACK_BLOCK, ws);
+        const Plan p(d, true, ws);
         p.clear(s);
         if (p.chained)
             hipLaunchKernelGGL((chained_scan_back_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch, (const T*)x, (const T*)f, marks, lengths, (const T*)dy, dh_last, (T*)dx, (T*)df, dh0);
