@@ -38,15 +38,51 @@ __device__ __forceinline__ bool held_place(int id, int n, int blocks, int& sampl
     return sample < n;
 }
 
+// Sums between lanes without a trip through LDS.  A lane's value plus that of another lane of its sixteen:
+template <int CTRL>
+__device__ __forceinline__ float plus_lane(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// .. plus that of the lane 16 or 32 on (one register's odd rows change places with the other's even ones)
+__device__ __forceinline__ float plus_16(float v) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float plus_32(float v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+// over the lanes that are `lanes` apart, for each of v; rotations within sixteen
+template <int N>
+__device__ __forceinline__ void sum_over_rows(float (&v)[N], int lanes) {
+    auto all = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = f(v[i]);
+    };
+    if (lanes <= 1) all([](float x) { return plus_lane<0x121>(x); });
+    if (lanes <= 2) all([](float x) { return plus_lane<0x122>(x); });
+    if (lanes <= 4) all([](float x) { return plus_lane<0x124>(x); });
+    if (lanes <= 8) all([](float x) { return plus_lane<0x128>(x); });
+    if (lanes <= 16) all(plus_16);
+    if (lanes <= 32) all(plus_32);
+}
+// over `lanes` neighbouring lanes, aligned; neighbours within four, then mirrored halves of eight and of sixteen
+__device__ __forceinline__ float sum_of_neighbours(float v, int lanes) {
+    if (lanes > 1) v = plus_lane<0xb1>(v);
+    if (lanes > 2) v = plus_lane<0x4e>(v);
+    if (lanes > 4) v = plus_lane<0x141>(v);
+    if (lanes > 8) v = plus_lane<0x140>(v);
+    if (lanes > 16) v = plus_16(v);
+    if (lanes > 32) v = plus_32(v);
+    return v;
+}
+
 // part[row of the workgroup][channel] -> sums over the rows of a wavefront's threads of equal channels are in `v` of its first lanes; here they
 // go to LDS, one row a wavefront (or a set of wavefronts that span the channels)
 template <int VEC, int NS>
 __device__ __forceinline__ void rows_to_lds(float (&v)[NS][VEC], int lanes, int cb, float* part, int stride, int at, int first) {
-    for (int m = lanes; m < OP_WAVE; m <<= 1)
 #pragma unroll
-        for (int k = 0; k < NS; ++k)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) v[k][i] += __shfl_xor(v[k][i], m);
+    for (int k = 0; k < NS; ++k) sum_over_rows<VEC>(v[k], lanes);
     const int row = (int)threadIdx.x / (lanes > OP_WAVE ? lanes : OP_WAVE);
     if (((int)threadIdx.x & (OP_WAVE - 1)) < lanes)
 #pragma unroll
@@ -66,7 +102,7 @@ __device__ __forceinline__ void groups_of_rows(const float* part, int rows, int 
         float s = 0.0f;
         for (int r = 0; r < rows; ++r)
             for (int c = at; c < cg; c += per) s += part[r * cb + g * cg + c];
-        for (int m = 1; m < per; m <<= 1) s += __shfl_xor(s, m);
+        s = sum_of_neighbours(s, per);  // (lanes without a group come in whole sets of `per`)
         if (at == 0) f(g, s);
     }
 }
@@ -345,8 +381,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_stats_kernel(rrm_norm_des
 
 constexpr int JOIN_THREADS = 512;
 __device__ __forceinline__ float sum_all(float v, float* lds) {
-#pragma unroll
-    for (int m = 1; m < OP_WAVE; m <<= 1) v += __shfl_xor(v, m);
+    v = sum_of_neighbours(v, OP_WAVE);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
