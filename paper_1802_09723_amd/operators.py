@@ -2,7 +2,8 @@
 
 Tensors are CUDA tensors whose last axis is adjacent; the axes before it may be strided as far as they collapse to the
 two (``gated_ff``: one) that the C calls take, and nothing is copied to make them so.  Results that the caller does not hand
-in, and the workspace, are allocated by torch on the current stream; with ``stream`` they are recorded on it as well.
+in, and the workspace, are allocated by torch.  With ``stream`` a call runs as if that stream were the current one, its allocations
+included; the caller orders it behind what its inputs wait for, and what uses its results behind it.
 
 What the checks of a call look at (shapes, strides, types) decides its descriptor and workspace too, so both are kept by it: a call with the
 shapes of an earlier one takes them from a table and goes on to the pointers.  (One frame of a live video, host time of a call:
@@ -135,13 +136,19 @@ def _workspace(nbytes: int, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def _used_on(stream, *tensors) -> None:
-    """A tensor made here on the current stream and used on another must not be handed out again before that one is through."""
+def _elsewhere(stream, call, *args):
+    """``call(*args)`` with ``stream`` (an object or a handle) current.  So its results and workspace come from memory of that stream's: a block of another stream's
+    may still be in use by what that one was given earlier, which ``stream`` does not wait for.  The results are recorded on the stream
+    that was current before, where the caller goes on: they must not be handed out again before that one is through with them."""
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
+    before = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        got = call(*args)
+    for t in got if isinstance(got, tuple) else (got,):
+        if all(t is not a for a in args):
+            t.record_stream(before)
+    return got
 
 
 # -- group norm with an activation -------------------------------------------------------------------------------------
@@ -151,6 +158,8 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
     """``rrm_group_norm_act``: ``x`` [n, .., c] float32 or bfloat16, channels last (2 axes: one position a sample); ``gamma``
     and ``beta`` float32 [c].  ``out`` or a new tensor of ``out_dtype`` (default: x's type) receives the result;
     ``stats``, float32 [n, groups, 2], what the backward pass needs."""
+    if stream is not None:
+        return _elsewhere(stream, group_norm_act, x, groups, gamma, beta, act, eps, out, out_dtype, stats)
     made = out is None
     if made:
         out = torch.empty_like(x, dtype=out_dtype)
@@ -170,15 +179,15 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
                                    *_outer_inner(out, "out"), 0, 0), "rrm_group_norm_workspace", 0)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act(plan[1], x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
-                                    _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, out if made else None)
+                                    _stream_ptr(None)))
     return out
 
 
 def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "none", eps: float = 1e-5, out=None, stats=None, stream=None):
     """group_norm_act of a bfloat16 convolution's stored projection (``rrm_snapshot``), read where it lies: after ``layer.step`` on the same
     stream, the next layer's input, bfloat16 [n, h_out, w_out, c_out]."""
+    if stream is not None:
+        return _elsewhere(stream, group_norm_act_of, layer, groups, gamma, beta, act, eps, out, stats)
     if layer.dtype != BF16 or layer.shape.kind != CONV:
         raise ValueError("layer: expected a bfloat16 convolution")
     n, h, w, c = layer.y_shape
@@ -196,15 +205,15 @@ def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "non
                      "rrm_group_norm_workspace", 0)
     ws = _workspace(plan[2], out.device)
     _check(lib().rrm_group_norm_act(plan[1], layer.snapshot_ptrs()[1], _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
-                                    _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, out if made else None)
+                                    _stream_ptr(None)))
     return out
 
 
 def group_norm_act_backward(dy, x, stats, gamma=None, beta=None, act: str = "none", dx=None, dgamma=None, dbeta=None, stream=None):
     """``rrm_group_norm_act_backward``: (dx, dgamma, dbeta) from ``dy`` (of the result's type and x's shape) and the ``stats`` that
     the forward pass left for the same ``x``, ``gamma``, ``beta`` and ``act``."""
+    if stream is not None:
+        return _elsewhere(stream, group_norm_act_backward, dy, x, stats, gamma, beta, act, dx, dgamma, dbeta)
     c = x.shape[-1]
     made = [t is None for t in (dx, dgamma, dbeta)]
     if dx is None:
@@ -233,16 +242,17 @@ def group_norm_act_backward(dy, x, stats, gamma=None, beta=None, act: str = "non
                                    *_outer_inner(dy, "dy"), *_outer_inner(dx, "dx")), "rrm_group_norm_workspace", 1)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act_backward(plan[1], x.data_ptr(), stats.data_ptr(), _ptr(gamma), _ptr(beta), dy.data_ptr(), dx.data_ptr(),
-                                             dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), plan[2], _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, *(t for t, was in zip((dx, dgamma, dbeta), made) if was))
+                                             dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None)))
     return dx, dgamma, dbeta
 
 
 # -- gated linear recurrence -------------------------------------------------------------------------------------------
 
-def gated_scan_marks(x):
-    """A tensor for the states that a forward pass of training keeps: float32 [n, ceil(t / 64), c] for x [n, t, c]."""
+def gated_scan_marks(x, stream=None):
+    """A tensor for the states that a forward pass of training keeps: float32 [n, ceil(t / 64), c] for x [n, t, c].  ``stream``: the one that
+    the passes run on, where it is not the current one."""
+    if stream is not None:
+        return _elsewhere(stream, gated_scan_marks, x)
     n, t, c = x.shape
     return x.new_empty((n, -(-t // MARK_FRAMES), c), dtype=torch.float32)
 
@@ -251,6 +261,8 @@ def gated_scan(x, f, h0=None, lengths=None, out=None, h_last=None, marks=None, s
     """``rrm_gated_scan``: (y, h_last) of the recurrence over ``x`` and the gates' logits ``f``, [n, t, c] float32 or bfloat16, from
     the state ``h0`` (float32 [n, c]; None: zeros).  ``lengths`` int32 [n]: frames of each video.  ``marks``: see gated_scan_marks;
     the backward pass needs them.  For one frame (t = 1) ``h_last`` may be ``h0``."""
+    if stream is not None:
+        return _elsewhere(stream, gated_scan, x, f, h0, lengths, out, h_last, marks)
     if x.dim() != 3:
         raise ValueError("x: expected [n, t, c]")
     n, t, c = shape = x.shape
@@ -273,15 +285,15 @@ def gated_scan(x, f, h0=None, lengths=None, out=None, h_last=None, marks=None, s
                      "rrm_gated_scan_workspace", 0)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_scan(plan[1], x.data_ptr(), f.data_ptr(), _ptr(h0), _ptr(lengths), out.data_ptr(), h_last.data_ptr(), _ptr(marks),
-                                _ptr(ws), plan[2], _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, out if made[0] else None, h_last if made[1] else None)
+                                _ptr(ws), plan[2], _stream_ptr(None)))
     return out, h_last
 
 
 def gated_scan_backward(dy, x, f, marks, lengths=None, dh_last=None, dx=None, df=None, dh0=None, stream=None):
     """``rrm_gated_scan_backward``: (dx, df, dh0) from ``dy``, the forward pass's inputs and ``marks``, and the gradient
     ``dh_last`` (float32 [n, c]; None: zeros) of the last state."""
+    if stream is not None:
+        return _elsewhere(stream, gated_scan_backward, dy, x, f, marks, lengths, dh_last, dx, df, dh0)
     if x.dim() != 3:
         raise ValueError("x: expected [n, t, c]")
     n, t, c = shape = x.shape
@@ -306,9 +318,7 @@ def gated_scan_backward(dy, x, f, marks, lengths=None, dh_last=None, dx=None, df
                                    *_frames(df, "df")), "rrm_gated_scan_workspace", 1)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_scan_backward(plan[1], x.data_ptr(), f.data_ptr(), marks.data_ptr(), _ptr(lengths), dy.data_ptr(), _ptr(dh_last),
-                                         dx.data_ptr(), df.data_ptr(), dh0.data_ptr(), _ptr(ws), plan[2], _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, *(g for g, was in zip((dx, df, dh0), made) if was))
+                                         dx.data_ptr(), df.data_ptr(), dh0.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None)))
     return dx, df, dh0
 
 
@@ -317,6 +327,8 @@ def gated_scan_backward(dy, x, f, marks, lengths=None, dh_last=None, dx=None, df
 def gated_ff(x, wg, wu, act: str = "silu", out=None, save=None, stream=None):
     """``rrm_gated_ff``: act(x wg^T) * (x wu^T), bfloat16: ``x`` [m, k], ``wg`` and ``wu`` [f, k], the result [m, f].
     ``save``: two tensors [m, f] that receive the two projections for the backward pass."""
+    if stream is not None:
+        return _elsewhere(stream, gated_ff, x, wg, wu, act, out, save)
     made = out is None
     if made:
         out = x.new_empty((x.shape[0], wg.shape[0]))
@@ -342,14 +354,14 @@ def gated_ff(x, wg, wu, act: str = "silu", out=None, save=None, stream=None):
                 raise ValueError("save: both tensors need the same strides")
         plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, saved, 0, 0, 0, int(loose)), "rrm_gated_ff_workspace", 0)
     ws = _workspace(plan[2], x.device)
-    _check(lib().rrm_gated_ff(plan[1], px, pg, pu, out.data_ptr(), _ptr(g), _ptr(u), _ptr(ws), plan[2], _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, out if made else None)
+    _check(lib().rrm_gated_ff(plan[1], px, pg, pu, out.data_ptr(), _ptr(g), _ptr(u), _ptr(ws), plan[2], _stream_ptr(None)))
     return out
 
 
 def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None, dwu=None, stream=None):
     """``rrm_gated_ff_backward``: (dx, dwg, dwu) from ``dh`` and the projections ``g`` and ``u`` that the forward pass saved."""
+    if stream is not None:
+        return _elsewhere(stream, gated_ff_backward, dh, x, wg, wu, g, u, act, dx, dwg, dwu)
     made = [t is None for t in (dx, dwg, dwu)]
     if dx is None:
         dx = torch.empty_like(x)
@@ -374,7 +386,5 @@ def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None,
         plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, int(loose)), "rrm_gated_ff_workspace", 1)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_ff_backward(plan[1], px, pg, pu, g.data_ptr(), u.data_ptr(), dh.data_ptr(), dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(),
-                                       _ptr(ws), plan[2], _stream_ptr(stream)))
-    if stream is not None:
-        _used_on(stream, ws, *(t for t, was in zip((dx, dwg, dwu), made) if was))
+                                       _ptr(ws), plan[2], _stream_ptr(None)))
     return dx, dwg, dwu

@@ -1,0 +1,100 @@
+"""The operators between and behind the linear layers where their surroundings are odd: other streams, sizes at the ends of the accepted range,
+tensors that do not belong, and the kernels' variants that small shapes do not reach.  Tolerances are those of test_operators where nothing else is said."""
+import contextlib
+
+import pytest
+import torch
+
+import paper_1802_09723_amd as rrm
+from paper_1802_09723_amd import operators as ops
+from test_operators import gen
+
+gpu = pytest.mark.gpu
+
+
+# -- streams -------------------------------------------------------------------------------------------------------------------
+
+BF = torch.bfloat16
+# a call of each operator on small tensors, and their shapes and type
+CALLS = {
+    "norm": (lambda t, **kw: rrm.group_norm_act(t[0], 2, **kw), torch.float32, [(2, 3, 8)]),
+    "norm_back": (lambda t, **kw: rrm.group_norm_act_backward(*t, **kw), torch.float32, [(2, 3, 8), (2, 3, 8), (2, 2, 2)]),
+    "scan": (lambda t, **kw: rrm.gated_scan(*t, **kw), torch.float32, [(2, 70, 8), (2, 70, 8)]),
+    "long_scan": (lambda t, **kw: rrm.gated_scan(*t, **kw), torch.float32, [(1, 900, 8), (1, 900, 8)]),
+    "scan_back": (lambda t, **kw: rrm.gated_scan_backward(*t, **kw), torch.float32, [(2, 70, 8), (2, 70, 8), (2, 70, 8), (2, 2, 8)]),
+    "ff": (lambda t, **kw: rrm.gated_ff(*t, **kw), BF, [(20, 9), (16, 9), (16, 9)]),
+    "ff_back": (lambda t, **kw: rrm.gated_ff_backward(*t, **kw), BF, [(20, 16), (20, 8), (16, 8), (16, 8), (20, 16), (20, 16)]),
+    "marks": (lambda t, **kw: rrm.gated_scan_marks(t[0], **kw), torch.float32, [(2, 70, 8)]),
+}
+
+
+def several(got):
+    return got if isinstance(got, tuple) else (got,)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_memory_of_a_call_on_another_stream_is_that_streams(name, monkeypatch):
+    """Results and workspace come from the pool of the stream that they are used on (a block of the current stream's may still be in use there), and
+    results are recorded on the one that was current.  Without a device: the library, the streams and what counts allocations are stand-ins."""
+    class Stream:
+        cuda_stream = 0x100
+        device = torch.device("cuda", 0)
+
+    here, side = Stream(), Stream()
+    now, taken, recorded = [here], [], []
+    call, dtype, shapes = CALLS[name]
+    inputs = [torch.zeros(shape, dtype=dtype) for shape in shapes]
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream)
+        yield
+        now.pop()
+
+    def counted(make):
+        def wrapped(*a, **kw):
+            kw.pop("device", None)
+            t = make(*a, **kw)
+            taken.append((now[-1], t))
+            return t
+        return wrapped
+
+    class Library:
+        def __getattr__(self, name):
+            return (lambda *a: 256) if name.endswith("_workspace") else (lambda *a: 0)
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: now[-1])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: recorded.append((s, t)))
+    monkeypatch.setattr(ops, "lib", Library)
+    monkeypatch.setattr(ops, "_expect", lambda *a: None)
+    monkeypatch.setattr(ops, "_plans", {})
+    monkeypatch.setattr(torch, "empty", counted(torch.empty))
+    monkeypatch.setattr(torch, "empty_like", counted(torch.empty_like))
+    monkeypatch.setattr(torch.Tensor, "new_empty", counted(torch.Tensor.new_empty))
+    got = several(call(inputs, stream=side))
+    assert taken and all(s is side for s, _ in taken)
+    for t in got:
+        assert any(r is t and s is here for s, r in recorded)
+
+
+@gpu
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "marks"])
+def test_a_call_on_another_stream_beside_one_that_uses_freed_memory(name):
+    """A block that was freed while the current stream still writes it is not handed to a call on another stream."""
+    call, dtype, shapes = CALLS[name]
+    inputs = [torch.randn(shape, generator=gen(i)).to(dtype).cuda() for i, shape in enumerate(shapes)]
+    want = [t.clone() for t in several(call(inputs))]
+    side = torch.cuda.Stream()
+    slow = torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):
+        slow.add_(1.0)
+    # blocks of the sizes that a call may ask for, written behind the slow work and freed before it is done
+    blocks = [torch.empty(256 << k, device="cuda", dtype=torch.uint8) for k in range(12) for _ in range(8)]
+    for b in blocks:
+        b.fill_(77)
+    del blocks, b
+    got = several(call(inputs, stream=side))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
