@@ -300,7 +300,6 @@ __global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, Hel
 struct SliceGeom {
     int slices, span;   // of a sample; positions of a slice
     int blocks, lanes;  // sets of channels; threads of a position, a power of two
-    float r_cg;
 };
 constexpr int SLICE_THREADS = 256;
 
@@ -319,6 +318,17 @@ struct Slice {
           me((int)threadIdx.x & (g.lanes - 1), (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC,
              min(d.c - (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC, g.lanes * VEC)) {}
 };
+
+// The groups of VEC neighbouring channels from c on, by integers: beyond some millions of channels a quotient in 32-bit floats is a group off.
+template <int VEC>
+__device__ __forceinline__ void groups_from(int c, int cg, int (&gi)[VEC]) {
+    int g = c / cg, left = (g + 1) * cg - c;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        gi[i] = g;
+        if (--left == 0) ++g, left = cg;
+    }
+}
 
 // sums over the workgroup's rows, to the first row's threads (lanes <= 256, any number of rows)
 template <int VEC, int NS>
@@ -439,11 +449,13 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_apply_kernel(rrm_norm_des
     TY* ys = y + t.sample * d.y_sample + t.me.at;
     const float* st = stats + 2 * (int64_t)t.sample * d.groups;
     float ga[VEC], be[VEC], mean[VEC];
+    int gi[VEC];
+    groups_from<VEC>(t.me.at, d.c / d.groups, gi);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
-        mean[i] = st[2 * gi];
-        ga[i] = (gamma ? gamma[c] : 1.0f) * st[2 * gi + 1];
+        const int c = t.me.at + i;
+        mean[i] = st[2 * gi[i]];
+        ga[i] = (gamma ? gamma[c] : 1.0f) * st[2 * gi[i] + 1];
         be[i] = beta ? beta[c] : 0.0f;
     }
     with_act(d.act, [&](auto act) {
@@ -469,11 +481,13 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc
     const TY* dys = dy + t.sample * d.y_sample + t.me.at;
     const float* st = stats + 2 * (int64_t)t.sample * d.groups;
     float ga[VEC], be[VEC], mean[VEC], r[VEC], s[2][VEC];
+    int gi[VEC];
+    groups_from<VEC>(t.me.at, d.c / d.groups, gi);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
-        mean[i] = st[2 * gi];
-        r[i] = st[2 * gi + 1];
+        const int c = t.me.at + i;
+        mean[i] = st[2 * gi[i]];
+        r[i] = st[2 * gi[i] + 1];
         ga[i] = gamma ? gamma[c] : 1.0f;
         be[i] = beta ? beta[c] : 0.0f;
         s[0][i] = s[1][i] = 0.0f;
@@ -552,13 +566,15 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_dx_kernel(rrm_norm_desc d
     TX* dxs = dx + t.sample * d.dx_sample + t.me.at;
     const float *st = stats + 2 * (int64_t)t.sample * d.groups, *me = means + 2 * (int64_t)t.sample * d.groups;
     float ga[VEC], be[VEC], mean[VEC], r[VEC], gp[VEC], gq[VEC];
+    int gi[VEC];
+    groups_from<VEC>(t.me.at, d.c / d.groups, gi);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int c = t.me.at + i, gi = (int)(((float)c + 0.5f) * g.r_cg);
-        mean[i] = st[2 * gi];
-        r[i] = st[2 * gi + 1];
-        gp[i] = me[2 * gi];
-        gq[i] = me[2 * gi + 1];
+        const int c = t.me.at + i;
+        mean[i] = st[2 * gi[i]];
+        r[i] = st[2 * gi[i] + 1];
+        gp[i] = me[2 * gi[i]];
+        gq[i] = me[2 * gi[i] + 1];
         ga[i] = gamma ? gamma[c] : 1.0f;
         be[i] = beta ? beta[c] : 0.0f;
     }
@@ -673,7 +689,6 @@ SliceGeom plan_slices(const rrm_norm_desc& d, int vec) {
     if (want > most) want = most;
     g.span = (int)((d.positions + want - 1) / want);
     g.slices = (d.positions + g.span - 1) / g.span;
-    g.r_cg = 1.0f / (float)(d.c / d.groups);
     return g;
 }
 int wide_of(const rrm_norm_desc& d) { return d.x_elem == RRM_F32 ? 4 : 8; }

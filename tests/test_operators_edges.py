@@ -1,13 +1,14 @@
 """The operators between and behind the linear layers where their surroundings are odd: other streams, sizes at the ends of the accepted range,
 tensors that do not belong, and the kernels' variants that small shapes do not reach.  Tolerances are those of test_operators where nothing else is said."""
 import contextlib
+import math
 
 import pytest
 import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_operators import gen
+from test_operators import GATE, U, gen
 
 gpu = pytest.mark.gpu
 
@@ -98,3 +99,51 @@ def test_a_call_on_another_stream_beside_one_that_uses_freed_memory(name):
     got = several(call(inputs, stream=side))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# -- sizes at the ends of the range ----------------------------------------------------------------------------------------------
+
+def norm_parts64(x, groups, eps=1e-5):
+    """(xh, mean, r) of a map [n, positions, c] in 64 bits, where it lies"""
+    n, p, c = x.shape
+    v = x.double().view(n, p, groups, c // groups)
+    mean = v.mean((1, 3), keepdim=True)
+    r = 1 / torch.sqrt(((v - mean) ** 2).mean((1, 3), keepdim=True) + eps)
+    return ((v - mean) * r).view(n, p, c), mean, r
+
+
+def close(got, want, slack, what):
+    err = (got.double() - want).abs() - slack
+    assert err.max() <= 0, f"{what}: {int((err > 0).sum())} off, by {float(err.max()):.3g} more than allowed"
+
+
+@gpu
+@pytest.mark.parametrize("n,c,groups", [(2, 1 << 24, 1), (1, 9000000, 1000), (1, 10000001, 1), (1, (1 << 23) + 3, 1)])
+def test_norm_of_very_many_channels(n, c, groups):
+    """Groups of which every one has a mean and a deviation of its own, so that another one's would show: a channel's group counts in
+    integers where 32-bit floats no longer tell neighbouring channels apart."""
+    cg = c // groups
+    g = torch.Generator(device="cuda").manual_seed(c)
+    own = torch.arange(n * groups, device="cuda").view(n, 1, groups, 1)
+    x = torch.empty(n, 1, c, device="cuda").normal_(generator=g)
+    x = (x.view(n, 1, groups, cg) * (1 + own % 3) + (own % 5)).view(n, 1, c)
+    xh, mean, r = norm_parts64(x, groups)
+    stats = torch.empty(n, groups, 2, device="cuda")
+    y = rrm.group_norm_act(x, groups, stats=stats)
+    # a thread sums its share of the group, some cg / 512 terms, one behind the other: their roundings at random signs, eight deviations
+    s = (8 * math.sqrt(cg / 512) + 32) * U
+    top = float(x.abs().max()) * float(r.max())
+    slack = s * (top + 1) + GATE
+    close(stats[..., 0], mean.view(n, groups), s * float(x.abs().max()), "mean")
+    close(stats[..., 1], r.view(n, groups), s * (1 + top) * r.view(n, groups), "r")
+    close(y, xh, slack, "y")
+    # with a mean and a part along xh, so that every term of the gradient counts
+    dy = (0.5 + 0.7 * xh + torch.empty(n, 1, c, device="cuda").normal_(generator=g)).float()
+    dx, dgamma, dbeta = rrm.group_norm_act_backward(dy, x, stats)
+    v, h = dy.double().view(n, 1, groups, cg), xh.view(n, 1, groups, cg)
+    p, q = v.mean((1, 3), keepdim=True), (v * h).mean((1, 3), keepdim=True)
+    want = (r * (v - p - h * q)).view(n, 1, c)
+    rr = r.expand(n, 1, groups, cg).reshape(n, 1, c)
+    close(dx, want, rr * 4 * (s + slack) * (dy.double().abs() + 1 + 2 * xh.abs() * (1 + xh.abs())), "dx")
+    close(dbeta, dy.double().sum((0, 1)), 4 * U * dy.double().abs().sum((0, 1)), "dbeta")
+    close(dgamma, (dy.double() * xh).sum((0, 1)), ((slack + 4 * U * (1 + xh.abs())) * dy.double().abs()).sum((0, 1)), "dgamma")
