@@ -305,7 +305,7 @@ typedef enum { RRM_ACT_NONE = 0, RRM_ACT_RELU = 1, RRM_ACT_SILU = 2, RRM_ACT_GEL
  *      y = act(gamma_c * (x - mean) * r + beta_c)
  * x may be a convolution's stored projection (rrm_snapshot), y the next layer's input. */
 typedef struct {
-    int n, positions, c, groups; /* groups divides c; n or positions may be 0 */
+    int n, positions, c, groups; /* groups divides c; n or positions may be 0; n * c and positions at most 2^31 - 4096 */
     int x_elem, y_elem, act;     /* rrm_elem of x and dx, of y and dy; rrm_act */
     float eps;                   /* > 0 */
     int64_t x_sample, x_position, y_sample, y_position, dx_sample, dx_position; /* strides; dy lies by those of y */

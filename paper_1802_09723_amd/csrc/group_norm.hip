@@ -314,7 +314,7 @@ struct Slice {
           row((int)threadIdx.x / g.lanes),
           step(SLICE_THREADS / g.lanes),
           p0(slice * g.span),
-          p1(p0 + g.span < d.positions ? p0 + g.span : d.positions),
+          p1(d.positions - p0 > g.span ? p0 + g.span : d.positions),
           me((int)threadIdx.x & (g.lanes - 1), (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC,
              min(d.c - (int)(blockIdx.x % (unsigned)g.blocks) * g.lanes * VEC, g.lanes * VEC)) {}
 };
@@ -626,6 +626,8 @@ void with_types(const rrm_norm_desc& d, F&& f) {
     d.x_elem == RRM_F32 ? out(float{}) : out(__bf16{});
 }
 
+int parts(int64_t n, int64_t of) { return (int)((n + of - 1) / of); }
+
 struct HeldPlan {
     HeldGeom g;
     int vec, which;  // which of the shapes; -1: registers do not hold it
@@ -643,6 +645,7 @@ constexpr HeldShape BACKWARD[] = {{256, 1}, {256, 4}, {512, 8}, {1024, 8}};
 HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[HELD_SHAPES]) {
     const int cg = d.c / d.groups, esize = d.x_elem == RRM_F32 ? 4 : 2;
     HeldPlan p{{}, d.c >= wide ? wide : 1, -1};
+    if (cg > shapes[HELD_SHAPES - 1].threads * p.vec) return p;  // (what is below counts in multiples of cg)
     auto fits = [&](int channels) {
         p.which = -1;
         int lanes = 1;
@@ -651,7 +654,7 @@ HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[H
         for (int w = 0; w < HELD_SHAPES; ++w) {
             if (lanes > shapes[w].threads || (int64_t)shapes[w].threads / lanes * shapes[w].p < d.positions) continue;
             p.which = w;
-            p.g = HeldGeom{channels, (d.c + channels - 1) / channels, lanes, 1.0f / (float)cg};
+            p.g = HeldGeom{channels, parts(d.c, channels), lanes, 1.0f / (float)cg};
             return true;
         }
         return false;
@@ -671,7 +674,7 @@ HeldPlan plan_held(const rrm_norm_desc& d, int wide, const HeldShape (&shapes)[H
         p.which = -1;
         return p;
     }
-    while (cb < d.c && (int64_t)d.n * ((d.c + 2 * cb - 1) / (2 * cb)) >= 4 * OP_CUS) {
+    while (cb < d.c && (int64_t)d.n * parts(d.c, 2 * cb) >= 4 * OP_CUS) {
         const HeldPlan before = p;
         if (!fits(2 * cb) || p.which > before.which) return before;
         cb *= 2;
@@ -682,13 +685,13 @@ SliceGeom plan_slices(const rrm_norm_desc& d, int vec) {
     SliceGeom g{};
     g.lanes = 1;
     while (g.lanes < SLICE_THREADS && g.lanes * vec < d.c) g.lanes <<= 1;
-    g.blocks = (d.c + g.lanes * vec - 1) / (g.lanes * vec);
+    g.blocks = parts(d.c, g.lanes * vec);
     const int rows = SLICE_THREADS / g.lanes;
     // some four workgroups a compute unit, of four rows of positions at least
-    int64_t want = 4 * OP_CUS / ((int64_t)d.n * g.blocks) + 1, most = (d.positions + 4 * rows - 1) / (4 * rows);
+    int64_t want = 4 * OP_CUS / ((int64_t)d.n * g.blocks) + 1, most = parts(d.positions, 4 * rows);
     if (want > most) want = most;
-    g.span = (int)((d.positions + want - 1) / want);
-    g.slices = (d.positions + g.span - 1) / g.span;
+    g.span = parts(d.positions, want);
+    g.slices = parts(d.positions, g.span);
     return g;
 }
 int wide_of(const rrm_norm_desc& d) { return d.x_elem == RRM_F32 ? 4 : 8; }
@@ -696,7 +699,7 @@ int slice_vec(const rrm_norm_desc& d) { return d.c >= wide_of(d) ? wide_of(d) : 
 bool held(const rrm_norm_desc& d, bool backward) { return plan_held(d, wide_of(d), backward ? BACKWARD : FORWARD).which >= 0; }
 size_t group_bytes(const rrm_norm_desc& d) { return round256((size_t)d.n * d.groups * 8); }
 
-unsigned held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (unsigned)(((d.n + 7) / 8) * 8 * p.g.blocks); }
+unsigned held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (unsigned)((int64_t)parts(d.n, 8) * 8 * p.g.blocks); }
 
 }  // namespace
 
@@ -792,7 +795,7 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
         });
     if (hipError_t e = hipGetLastError()) return e;
     if ((dgamma || dbeta) && !one)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, s, sum1, sum2, some ? d.n : 0, d.c, dgamma, dbeta);
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)parts(d.c, 32)), dim3(1024), 0, s, sum1, sum2, some ? d.n : 0, d.c, dgamma, dbeta);
     return hipGetLastError();
 }
 

@@ -45,8 +45,9 @@ rrm_status check(const rrm_norm_desc* d) {
         return record_failure(RRM_ERR_DTYPE, "group norm: elements are RRM_F32 or RRM_BF16");
     if (d->n < 0 || d->positions < 0 || d->c < 1 || d->groups < 1 || d->c % d->groups)
         return record_failure(RRM_ERR_SHAPE, "group norm: n and positions not negative, c positive, groups a divisor of c");
-    if ((int64_t)d->n * d->groups > 0x7fffffff || (int64_t)d->n * d->c > 0x7fffffff)
-        return record_failure(RRM_ERR_SHAPE, "group norm: n * c must fit 31 bits");
+    // (below 2^31 by more than any kernel's step over channels or positions)
+    if ((int64_t)d->n * d->c > 0x7ffff000 || d->positions > 0x7ffff000)
+        return record_failure(RRM_ERR_SHAPE, "group norm: n * c and positions are at most 2^31 - 4096");
     if (!(d->eps > 0.0f) || d->eps > 3.0e38f) return record_failure(RRM_ERR_OPTION, "group norm: eps must be positive and finite");
     return check_act(d->act);
 }

@@ -1,14 +1,18 @@
 """The operators between and behind the linear layers where their surroundings are odd: other streams, sizes at the ends of the accepted range,
 tensors that do not belong, and the kernels' variants that small shapes do not reach.  Tolerances are those of test_operators where nothing else is said."""
 import contextlib
+import ctypes
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_operators import GATE, U, gen
+from test_operators import GATE, U, V, _norm_desc, gen
 
 gpu = pytest.mark.gpu
 
@@ -147,3 +151,80 @@ def test_norm_of_very_many_channels(n, c, groups):
     close(dx, want, rr * 4 * (s + slack) * (dy.double().abs() + 1 + 2 * xh.abs() * (1 + xh.abs())), "dx")
     close(dbeta, dy.double().sum((0, 1)), 4 * U * dy.double().abs().sum((0, 1)), "dbeta")
     close(dgamma, (dy.double() * xh).sum((0, 1)), ((slack + 4 * U * (1 + xh.abs())) * dy.double().abs()).sum((0, 1)), "dgamma")
+
+
+# n, positions, c, groups at the ends of what a descriptor may say
+FAR_NORM = [
+    (1, 1, 0x7ffff000, 1), (1, 1, (1 << 30) + 8, 1), (1, 100, 1 << 30, 2), (1, 3, 1 << 30, 1 << 26), (1, 0x7ffff000, 1, 1), (1, 0x7ffff000, 64, 1),
+    (0x7ffff000, 1, 1, 1), (0x7ffff000, 40000, 1, 1), (3, 0x7fffe000, 8, 8), (2, 0x7fffe000, 24, 4), (1, 1, 0x7ffff000, 0x7ffff000),
+]
+
+
+def test_norm_plans_of_the_largest_sizes():
+    """The host's choice of a layout ends, and the bytes it asks for hold what the kernels keep there.  In a process of its own: it used not to end."""
+    code = """
+import ctypes, sys
+sys.path.insert(0, sys.argv[1])
+import paper_1802_09723_amd as rrm
+from paper_1802_09723_amd.operators import NormDesc
+for n, p, c, g in eval(sys.argv[2]):
+    for x in (0, 1):
+        for back in (0, 1):
+            d = NormDesc(n, p, c, g, x, 0, 0, 1e-5, 0, c, 0, c, 0, c)
+            print(rrm.lib().rrm_group_norm_workspace(ctypes.byref(d), back))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code, root, repr(FAR_NORM)], capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0, done.stderr
+    sizes = iter(int(v) for v in done.stdout.split())
+    for n, p, c, groups in FAR_NORM:
+        for x in (0, 1):
+            # a value a channel and sample where samples are held, two a channel of a slice beside the groups' where not: at most about
+            # 1024 slices and one for each sample and set of channels
+            forward, backward = next(sizes), next(sizes)
+            least, most = 8 * n * c, 8 * n * c + 8 * 1024 * 2048 * 8
+            assert forward == 0 or least <= forward <= 3 * most, (n, p, c, groups, x, forward)
+            assert least <= backward <= 4 * most, (n, p, c, groups, x, backward)
+
+
+def test_norm_refuses_sizes_beyond_the_range():
+    L = rrm.lib()
+    P = 1 << 20
+    for kw in (dict(n=1, positions=1, c=0x7ffff001, groups=1), dict(n=1, positions=0x7ffff001, c=1, groups=1), dict(n=0x7fffffff, positions=1, c=1, groups=1)):
+        d = _norm_desc(**kw)
+        assert L.rrm_group_norm_act(ctypes.byref(d), P, None, None, P, None, P, 1 << 40, None) == -2
+        assert L.rrm_group_norm_act_backward(ctypes.byref(d), P, P, None, None, P, P, P, P, P, 1 << 40, None) == -2
+
+
+@gpu
+@pytest.mark.parametrize("positions", [0x7ffff000, (1 << 30) + 77])
+def test_norm_of_very_many_positions(positions):
+    """One channel, as many positions as a call takes: the last slices end where the map does, both ways."""
+    x = torch.empty(1, positions, 1, device="cuda", dtype=BF).normal_(3.0, 2.0, generator=torch.Generator(device="cuda").manual_seed(5))
+    parts = [slice(k, min(k + (1 << 27), positions)) for k in range(0, positions, 1 << 27)]
+    flat = x.view(-1)
+    mean = sum(float(flat[p].double().sum()) for p in parts) / positions
+    r = (sum(float(((flat[p].double() - mean) ** 2).sum()) for p in parts) / positions + 1e-5) ** -0.5
+    stats = torch.empty(1, 1, 2, device="cuda")
+    y = rrm.group_norm_act(x, 1, stats=stats).view(-1)
+    # a thread sums some 8192 positions of a slice one behind the other
+    s = (8 * math.sqrt(positions / 1024 / 256) + 32) * U
+    top = float(x.abs().max())
+    assert abs(float(stats[0, 0, 0]) - mean) <= s * top and abs(float(stats[0, 0, 1]) - r) <= s * r * (1 + top * r)
+    slack = s * (top * r + 1)
+    for p in parts:
+        want = (flat[p].double() - mean) * r
+        close(y[p], want, slack + V * (want.abs() + slack), "y")
+    # dy = 0.5 y + 1: <dy> = 1 and <dy xh> = 0.5 but for roundings, so dx is r times what these leave
+    dy = y.mul_(0.5).add_(1).view(1, positions, 1)
+    dx, dgamma, dbeta = rrm.group_norm_act_backward(dy, x, stats)
+    d = dy.view(-1)
+    p1 = sum(float(d[p].double().sum()) for p in parts)
+    q1 = sum(float((d[p].double() * ((flat[p].double() - mean) * r)).sum()) for p in parts)
+    most = 1 + 0.5 * top * r
+    assert abs(float(dbeta) - p1) <= s * most * positions and abs(float(dgamma) - q1) <= (s * (1 + top * r) + slack) * most * positions
+    for p in parts:
+        xh = (flat[p].double() - mean) * r
+        want = r * (d[p].double() - p1 / positions - xh * q1 / positions)
+        off = r * 4 * (s + slack) * (1 + xh.abs()) ** 2 * most
+        close(dx.view(-1)[p], want, off + V * (want.abs() + off), "dx")
