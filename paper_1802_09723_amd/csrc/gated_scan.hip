@@ -185,15 +185,16 @@ __device__ __forceinline__ void take(const float* row, int at, int first, float 
 
 // A workgroup a chain.
 template <typename T, int VEC>
-__global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, int tiles, const T* __restrict__ x, const T* __restrict__ f, const float* h0,
+__global__ __launch_bounds__(GS_THREADS) void scan_kernel(rrm_scan_desc d, int tiles, unsigned from, const T* __restrict__ x, const T* __restrict__ f, const float* h0,
                                                           const int32_t* __restrict__ lengths, T* __restrict__ y,
                                                           float* h_last, float* __restrict__ marks) {
     using Z = Tile<VEC>;
     constexpr int S = Z::SPAN;
     __shared__ __attribute__((aligned(16))) float sa[2][Z::ROWS * Z::WIDTH];
     __shared__ __attribute__((aligned(16))) float sb[2][Z::ROWS * Z::WIDTH];
-    const int video = (int)(blockIdx.x / (unsigned)tiles);
-    const int c0 = (int)(blockIdx.x % (unsigned)tiles) * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
+    const unsigned id = from + blockIdx.x;
+    const int video = (int)(id / (unsigned)tiles);
+    const int c0 = (int)(id % (unsigned)tiles) * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
     const int end = video_frames(lengths, video, d.t);
     const T* xp = x + video * d.x_video + me.at;
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(GS_THREADS, FRAMES == GS_BLOCK ? 4 : 2) void chaine
 constexpr int BACK_BLOCK = 64;  // frames of a block where a workgroup has a chain: it holds four values a frame
 
 template <typename T, int VEC>
-__global__ __launch_bounds__(GS_THREADS, 3) void scan_back_kernel(rrm_scan_desc d, int tiles, const T* __restrict__ x, const T* __restrict__ f,
+__global__ __launch_bounds__(GS_THREADS, 3) void scan_back_kernel(rrm_scan_desc d, int tiles, unsigned from, const T* __restrict__ x, const T* __restrict__ f,
                                                                const float* __restrict__ marks, const int32_t* __restrict__ lengths,
                                                                const T* __restrict__ dy, const float* dh_last,
                                                                T* __restrict__ dx, T* __restrict__ df, float* dh0) {
@@ -420,8 +421,9 @@ __global__ __launch_bounds__(GS_THREADS, 3) void scan_back_kernel(rrm_scan_desc 
     __shared__ __attribute__((aligned(16))) float sa[Z::ROWS * Z::WIDTH];
     __shared__ __attribute__((aligned(16))) float sb[Z::ROWS * Z::WIDTH];
     __shared__ __attribute__((aligned(16))) float sg[Z::ROWS * Z::WIDTH];
-    const int video = (int)(blockIdx.x / (unsigned)tiles);
-    const int c0 = (int)(blockIdx.x % (unsigned)tiles) * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
+    const unsigned id = from + blockIdx.x;
+    const int video = (int)(id / (unsigned)tiles);
+    const int c0 = (int)(id % (unsigned)tiles) * Z::WIDTH, width = min(d.c - c0, Z::WIDTH), row = (int)threadIdx.x / Z::LANES, j = (int)threadIdx.x;
     const Span<VEC> me((int)threadIdx.x % Z::LANES, c0, width);
     const int end = video_frames(lengths, video, d.t);
     const T* xp = x + video * d.x_video + me.at;
@@ -711,10 +713,11 @@ __global__ __launch_bounds__(GS_THREADS, 3) void chained_scan_back_kernel(rrm_sc
 
 // Few frames: a thread a vector of features, frame by frame.  A frame of 4096 features takes 3.5 us, most of it the launch.
 template <typename T, int VEC>
-__global__ __launch_bounds__(64) void short_scan_kernel(rrm_scan_desc d, const T* __restrict__ x, const T* __restrict__ f, const float* h0,
+__global__ __launch_bounds__(64) void short_scan_kernel(rrm_scan_desc d, unsigned from, const T* __restrict__ x, const T* __restrict__ f, const float* h0,
                                                         const int32_t* __restrict__ lengths, T* __restrict__ y, float* h_last,
                                                         float* __restrict__ marks) {
-    const int per = (d.c + 64 * VEC - 1) / (64 * VEC), video = (int)(blockIdx.x / (unsigned)per), c0 = (int)(blockIdx.x % (unsigned)per) * 64 * VEC;
+    const unsigned id = from + blockIdx.x, per = ((unsigned)d.c + 64 * VEC - 1) / (64 * VEC);
+    const int video = (int)(id / per), c0 = (int)(id % per) * 64 * VEC;
     const Span<VEC> me((int)threadIdx.x, c0, min(d.c - c0, 64 * VEC));
     if (me.first == VEC) return;
     const int end = video_frames(lengths, video, d.t);
@@ -769,7 +772,7 @@ struct Plan {
     bool chained;
     Plan(const rrm_scan_desc& d, bool backward, void* ws) {
         const int v = vec_of(d), width = v * Tile<1>::LANES;
-        ch.tiles = (d.c + width - 1) / width;
+        ch.tiles = (int)(((int64_t)d.c + width - 1) / width);
         ch.blocks = (d.t - 1) / (backward ? GS_BLOCK : forward_block(d)) + 1;
         ch.groups = (ch.blocks - 1) / GROUP + 1;
         chains = (int64_t)d.n * ch.tiles;
@@ -818,8 +821,10 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
         using T = decltype(t);
         constexpr int VEC = decltype(vec)::value;
         if (few_frames(d)) {
-            hipLaunchKernelGGL((short_scan_kernel<T, VEC>), dim3((unsigned)((int64_t)d.n * ((d.c + 64 * VEC - 1) / (64 * VEC)))), dim3(64), 0, s, d,
-                               (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
+            in_parts(d.n * (((int64_t)d.c + 64 * VEC - 1) / (64 * VEC)), [&](unsigned from, unsigned count) {
+                hipLaunchKernelGGL((short_scan_kernel<T, VEC>), dim3(count), dim3(64), 0, s, d, from, (const T*)x, (const T*)f, h0, lengths, (T*)y,
+                                   h_last, marks);
+            });
             return;
         }
         const Plan p(d, false, ws);
@@ -834,7 +839,10 @@ hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* 
             }
             chained(std::integral_constant<int, GS_BLOCK>{});
         } else
-            hipLaunchKernelGGL((scan_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch.tiles, (const T*)x, (const T*)f, h0, lengths, (T*)y, h_last, marks);
+            in_parts(p.chains, [&](unsigned from, unsigned count) {
+                hipLaunchKernelGGL((scan_kernel<T, VEC>), dim3(count), dim3(GS_THREADS), 0, s, d, p.ch.tiles, from, (const T*)x, (const T*)f, h0, lengths,
+                                   (T*)y, h_last, marks);
+            });
     });
     return hipGetLastError();
 }
@@ -855,7 +863,10 @@ hipError_t launch_gated_scan_backward(const rrm_scan_desc& d, const void* x, con
         if (p.chained)
             hipLaunchKernelGGL((chained_scan_back_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch, (const T*)x, (const T*)f, marks, lengths, (const T*)dy, dh_last, (T*)dx, (T*)df, dh0);
         else
-            hipLaunchKernelGGL((scan_back_kernel<T, VEC>), p.grid(), dim3(GS_THREADS), 0, s, d, p.ch.tiles, (const T*)x, (const T*)f, marks, lengths, (const T*)dy, dh_last, (T*)dx, (T*)df, dh0);
+            in_parts(p.chains, [&](unsigned from, unsigned count) {
+                hipLaunchKernelGGL((scan_back_kernel<T, VEC>), dim3(count), dim3(GS_THREADS), 0, s, d, p.ch.tiles, from, (const T*)x, (const T*)f, marks,
+                                   lengths, (const T*)dy, dh_last, (T*)dx, (T*)df, dh0);
+            });
     });
     return hipGetLastError();
 }

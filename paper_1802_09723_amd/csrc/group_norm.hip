@@ -31,10 +31,10 @@ struct HeldGeom {
 };
 
 // A workgroup's place: id -> sample, block; a sample's blocks, whose runs share cache lines, are on one XCD (ids go to the eight in turn)
-__device__ __forceinline__ bool held_place(int id, int n, int blocks, int& sample, int& block) {
-    const int k = id >> 3;
+__device__ __forceinline__ bool held_place(unsigned id, int n, int blocks, int& sample, int& block) {
+    const int k = (int)(id >> 3);
     block = k % blocks;
-    sample = (k / blocks) * 8 + (id & 7);
+    sample = (k / blocks) * 8 + (int)(id & 7);
     return sample < n;
 }
 
@@ -108,12 +108,12 @@ __device__ __forceinline__ void groups_of_rows(const float* part, int rows, int 
 }
 
 template <typename TX, typename TY, int VEC, int P, int THREADS>
-__global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom h, const TX* __restrict__ x, const float* __restrict__ gamma,
+__global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom h, unsigned from, const TX* __restrict__ x, const float* __restrict__ gamma,
                                                        const float* __restrict__ beta, TY* __restrict__ y, float* __restrict__ stats) {
     __shared__ float part[THREADS * VEC];
     __shared__ float gs[2][HELD_GROUPS];
     int sample, block;
-    if (!held_place((int)blockIdx.x, d.n, h.blocks, sample, block)) return;
+    if (!held_place(from + blockIdx.x, d.n, h.blocks, sample, block)) return;
     const int cg = d.c / d.groups, c0 = block * h.cb, cb = d.c - c0 < h.cb ? d.c - c0 : h.cb;
     const int slot = (int)threadIdx.x & (h.lanes - 1), row = (int)threadIdx.x / h.lanes, R = THREADS / h.lanes;
     const int rows = THREADS / (h.lanes > OP_WAVE ? h.lanes : OP_WAVE);  // of part
@@ -190,14 +190,14 @@ __global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom
 
 // sum1, sum2: [n][c], the samples' sums of dz and of dz * xh.  KEEP: dz stays in registers as well, else its slope is made twice
 template <typename TX, typename TY, int VEC, int P, int THREADS, bool KEEP>
-__global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, HeldGeom h, const TX* __restrict__ x, const float* __restrict__ stats,
+__global__ __launch_bounds__(THREADS) void held_back_kernel(rrm_norm_desc d, HeldGeom h, unsigned from, const TX* __restrict__ x, const float* __restrict__ stats,
                                                             const float* __restrict__ gamma, const float* __restrict__ beta,
                                                             const TY* __restrict__ dy, TX* __restrict__ dx, float* __restrict__ sum1,
                                                             float* __restrict__ sum2) {
     __shared__ float part[2 * THREADS * VEC];
     __shared__ float gs[2][HELD_GROUPS];
     int sample, block;
-    if (!held_place((int)blockIdx.x, d.n, h.blocks, sample, block)) return;
+    if (!held_place(from + blockIdx.x, d.n, h.blocks, sample, block)) return;
     const int cg = d.c / d.groups, c0 = block * h.cb, cb = d.c - c0 < h.cb ? d.c - c0 : h.cb;
     const int slot = (int)threadIdx.x & (h.lanes - 1), row = (int)threadIdx.x / h.lanes, R = THREADS / h.lanes;
     const int rows = THREADS / (h.lanes > OP_WAVE ? h.lanes : OP_WAVE);
@@ -416,9 +416,9 @@ struct JoinShape {
 };
 
 // One workgroup a group of a sample: the slices' and channels' means and squares become the group's
-__global__ __launch_bounds__(JOIN_THREADS) void join_stats_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, float* __restrict__ stats) {
+__global__ __launch_bounds__(JOIN_THREADS) void join_stats_kernel(rrm_norm_desc d, SliceGeom g, unsigned first, const float* __restrict__ part, float* __restrict__ stats) {
     __shared__ float lds[JOIN_THREADS / OP_WAVE];
-    const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
+    const int cg = d.c / d.groups, id = (int)(first + blockIdx.x), sample = id / d.groups, group = id % d.groups;
     const float* from = part + (int64_t)sample * g.slices * 2 * d.c + group * cg;
     const JoinShape j(cg);
     const float per = 1.0f / ((float)d.positions * (float)cg);
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_stats_kernel(rrm_norm_desc 
             q += e[d.c] + off * off * (k + 1 < g.slices ? whole : last);
         }
     const float r = 1.0f / sqrtf(sum_all(q, lds) * per + d.eps);
-    if (threadIdx.x == 0) stats[2 * (int64_t)blockIdx.x] = mean, stats[2 * (int64_t)blockIdx.x + 1] = r;
+    if (threadIdx.x == 0) stats[2 * (int64_t)id] = mean, stats[2 * (int64_t)id + 1] = r;
 }
 
 template <typename TX, typename TY, int VEC>
@@ -517,10 +517,10 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_sums_kernel(rrm_norm_desc
 }
 
 // One workgroup a group of a sample: the slices' sums of each channel, sum1 and sum2 [n][c], and the group's means of gamma dz and of gamma dz xh, [n][groups][2]
-__global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, const float* __restrict__ part, const float* __restrict__ gamma,
+__global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d, SliceGeom g, unsigned first, const float* __restrict__ part, const float* __restrict__ gamma,
                                                                  float* __restrict__ sum1, float* __restrict__ sum2, float* __restrict__ means) {
     __shared__ float lds[JOIN_THREADS / OP_WAVE], rows[2][JOIN_THREADS];
-    const int cg = d.c / d.groups, sample = (int)blockIdx.x / d.groups, group = (int)blockIdx.x % d.groups;
+    const int cg = d.c / d.groups, id = (int)(first + blockIdx.x), sample = id / d.groups, group = id % d.groups;
     const JoinShape j(cg);
     const int64_t all = (int64_t)d.n * g.slices;
     float p = 0.0f, q = 0.0f;
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_sums_kernel(rrm_norm_desc d
     const float per = 1.0f / ((float)d.positions * (float)cg);
     p = sum_all(p, lds) * per;
     q = sum_all(q, lds) * per;
-    if (threadIdx.x == 0) means[2 * (int64_t)blockIdx.x] = p, means[2 * (int64_t)blockIdx.x + 1] = q;
+    if (threadIdx.x == 0) means[2 * (int64_t)id] = p, means[2 * (int64_t)id + 1] = q;
 }
 
 template <typename TX, typename TY, int VEC>
@@ -598,9 +598,9 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_dx_kernel(rrm_norm_desc d
 
 // dbeta and dgamma: the samples' sums (no samples: zeros).  32 channels a workgroup, 32 threads a channel, joined in their order.
 __global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restrict__ sum1, const float* __restrict__ sum2, int n, int c,
-                                                           float* __restrict__ dgamma, float* __restrict__ dbeta) {
+                                                           unsigned first, float* __restrict__ dgamma, float* __restrict__ dbeta) {
     __shared__ float lds[2][32][32];
-    const int ch = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), k = (int)threadIdx.x >> 5;
+    const int ch = (int)(first + blockIdx.x) * 32 + ((int)threadIdx.x & 31), k = (int)threadIdx.x >> 5;
     float s1 = 0.0f, s2 = 0.0f;
     if (ch < c)
 #pragma unroll 4
@@ -699,7 +699,7 @@ int slice_vec(const rrm_norm_desc& d) { return d.c >= wide_of(d) ? wide_of(d) : 
 bool held(const rrm_norm_desc& d, bool backward) { return plan_held(d, wide_of(d), backward ? BACKWARD : FORWARD).which >= 0; }
 size_t group_bytes(const rrm_norm_desc& d) { return round256((size_t)d.n * d.groups * 8); }
 
-unsigned held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (unsigned)((int64_t)parts(d.n, 8) * 8 * p.g.blocks); }
+int64_t held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (int64_t)parts(d.n, 8) * 8 * p.g.blocks; }
 
 }  // namespace
 
@@ -718,8 +718,10 @@ hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float*
         const HeldPlan p = plan_held(d, WIDE, FORWARD);
         auto go = [&](auto vec, auto which) {
             constexpr HeldShape h = FORWARD[decltype(which)::value];
-            hipLaunchKernelGGL((held_kernel<TX, TY, decltype(vec)::value, h.p, h.threads>), dim3(held_grid(d, p)), dim3(h.threads), 0, s, d, p.g,
-                               (const TX*)x, gamma, beta, (TY*)y, stats);
+            in_parts(held_grid(d, p), [&](unsigned from, unsigned count) {
+                hipLaunchKernelGGL((held_kernel<TX, TY, decltype(vec)::value, h.p, h.threads>), dim3(count), dim3(h.threads), 0, s, d, p.g, from,
+                                   (const TX*)x, gamma, beta, (TY*)y, stats);
+            });
         };
         auto by_vec = [&](auto vec) {
             constexpr int VEC = decltype(vec)::value;
@@ -733,7 +735,9 @@ hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float*
                     const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
                     float* st = stats ? stats : (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
                     hipLaunchKernelGGL((slice_stats_kernel<TX, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, (float*)ws);
-                    hipLaunchKernelGGL(join_stats_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, st);
+                    in_parts((int64_t)d.n * d.groups, [&](unsigned from, unsigned count) {
+                        hipLaunchKernelGGL(join_stats_kernel, dim3(count), dim3(JOIN_THREADS), 0, s, d, g, from, (const float*)ws, st);
+                    });
                     hipLaunchKernelGGL((slice_apply_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, gamma, beta, st, (TY*)y);
                 }
             }
@@ -765,8 +769,10 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                 // (bfloat16, the largest: there are no registers for dz in 32 bits)
                 constexpr bool KEEP = sizeof(TX) == 4 || h.threads < 1024;
                 place_sums((float*)ws);
-                hipLaunchKernelGGL((held_back_kernel<TX, TY, decltype(vec)::value, h.p, h.threads, KEEP>), dim3(held_grid(d, p)), dim3(h.threads),
-                                   0, s, d, p.g, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, sum1, sum2);
+                in_parts(held_grid(d, p), [&](unsigned from, unsigned count) {
+                    hipLaunchKernelGGL((held_back_kernel<TX, TY, decltype(vec)::value, h.p, h.threads, KEEP>), dim3(count), dim3(h.threads),
+                                       0, s, d, p.g, from, (const TX*)x, stats, gamma, beta, (const TY*)dy, (TX*)dx, sum1, sum2);
+                });
             };
             auto by_vec = [&](auto vec) {
                 constexpr int VEC = decltype(vec)::value;
@@ -775,7 +781,7 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                     case 1: go(vec, std::integral_constant<int, 1>{}); break;
                     case 2: go(vec, std::integral_constant<int, 2>{}); break;
                     case 3: go(vec, std::integral_constant<int, 3>{}); break;
-                        default: {
+                    default: {
                         const SliceGeom g = plan_slices(d, VEC);
                         const dim3 grid((unsigned)((int64_t)d.n * g.slices * g.blocks));
                         float* to = (float*)((char*)ws + round256((size_t)2 * d.n * g.slices * d.c * 4));
@@ -783,8 +789,9 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
                         place_sums(to);
                         hipLaunchKernelGGL((slice_sums_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, (float*)ws);
-                        hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)(d.n * d.groups)), dim3(JOIN_THREADS), 0, s, d, g, (const float*)ws, gamma,
-                                           sum1, sum2, means);
+                        in_parts((int64_t)d.n * d.groups, [&](unsigned from, unsigned count) {
+                            hipLaunchKernelGGL(join_sums_kernel, dim3(count), dim3(JOIN_THREADS), 0, s, d, g, from, (const float*)ws, gamma, sum1, sum2, means);
+                        });
                         if (!dx) break;
                         hipLaunchKernelGGL((slice_dx_kernel<TX, TY, VEC>), grid, dim3(SLICE_THREADS), 0, s, d, g, (const TX*)x, stats, gamma, beta,
                                            (const TY*)dy, means, (TX*)dx);
@@ -795,7 +802,9 @@ hipError_t launch_group_norm_backward(const rrm_norm_desc& d, const void* x, con
         });
     if (hipError_t e = hipGetLastError()) return e;
     if ((dgamma || dbeta) && !one)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)parts(d.c, 32)), dim3(1024), 0, s, sum1, sum2, some ? d.n : 0, d.c, dgamma, dbeta);
+        in_parts(parts(d.c, 32), [&](unsigned from, unsigned count) {
+            hipLaunchKernelGGL(norm_params_kernel, dim3(count), dim3(1024), 0, s, sum1, sum2, some ? d.n : 0, d.c, from, dgamma, dbeta);
+        });
     return hipGetLastError();
 }
 

@@ -211,6 +211,14 @@ __host__ __device__ __forceinline__ void with_act(int act, F&& f) {
     }
 }
 
+// A launch takes fewer than 2^32 threads along an axis: f(first workgroup, workgroups) for each part of `total` of them.  Parts begin at whole eights, so
+// workgroups stay on their XCD.
+template <typename F>
+void in_parts(int64_t total, F&& f) {
+    constexpr int64_t MOST = 1 << 21;  // of up to 1024 threads
+    for (int64_t first = 0; first < total; first += MOST) f((unsigned)first, (unsigned)(total - first < MOST ? total - first : MOST));
+}
+
 #endif  // __HIPCC__
 
 // Launchers; descriptors have been checked, and something is to be done.  The *_scratch functions say how many bytes of

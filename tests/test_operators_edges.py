@@ -12,7 +12,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_operators import GATE, U, V, _norm_desc, gen
+from test_operators import GATE, SUM, U, V, _norm_desc, gen
 
 gpu = pytest.mark.gpu
 
@@ -228,3 +228,71 @@ def test_norm_of_very_many_positions(positions):
         want = r * (d[p].double() - p1 / positions - xh * q1 / positions)
         off = r * 4 * (s + slack) * (1 + xh.abs()) ** 2 * most
         close(dx.view(-1)[p], want, off + V * (want.abs() + off), "dx")
+
+
+@gpu
+@pytest.mark.parametrize("t", [1, 17])
+def test_scan_of_very_many_videos(t):
+    """More videos than one launch has workgroups for (2^32 threads along an axis)."""
+    n = (1 << 26) + 5 if t == 1 else (1 << 24) + 5
+    g = torch.Generator(device="cuda").manual_seed(t)
+    x, f = (torch.empty(n, t, 1, device="cuda", dtype=BF).normal_(generator=g) for _ in range(2))
+    h0 = torch.empty(n, 1, device="cuda").normal_(generator=g)
+    marks = rrm.gated_scan_marks(x)
+    y, last = rrm.gated_scan(x, f, h0, marks=marks)
+    slack = 8 * (SUM + GATE) * 2  # (values below 8)
+    h = h0[:, 0].double()
+    for k in range(t):
+        a = torch.sigmoid(f[:, k, 0].double())
+        h = a * h + (1 - a) * x[:, k, 0].double()
+        close(y[:, k, 0], h, slack + V * (h.abs() + slack), "y")
+    close(last[:, 0], h, slack, "h_last")
+    dx, df, dh0 = rrm.gated_scan_backward(y, x, f, marks)
+    before = [h0[:, 0].double()]  # the states again, for the gradients
+    for k in range(t - 1):
+        a = torch.sigmoid(f[:, k, 0].double())
+        before.append(a * before[-1] + (1 - a) * x[:, k, 0].double())
+    carry = torch.zeros_like(h)
+    gs = slack * t
+    for k in reversed(range(t)):
+        a, v, grad = torch.sigmoid(f[:, k, 0].double()), x[:, k, 0].double(), y[:, k, 0].double() + carry
+        want = (1 - a) * grad
+        close(dx[:, k, 0], want, gs + V * (want.abs() + gs), "dx")
+        want = grad * (before[k] - v) * a * (1 - a)
+        close(df[:, k, 0], want, 16 * gs + V * (want.abs() + 16 * gs), "df")
+        carry = a * grad
+    close(dh0[:, 0], carry, gs, "dh0")
+
+
+@gpu
+@pytest.mark.parametrize("n,c,groups", [((1 << 24) + 9, 2, 1), (2, (1 << 27) + 64, ((1 << 27) + 64) // 16)])
+def test_norm_of_very_many_samples_or_groups(n, c, groups):
+    """More samples, or channels of a sample, than one launch has workgroups for."""
+    cg = c // groups
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.empty(n, 1, c, device="cuda", dtype=BF).normal_(1.0, generator=g)
+    dy = torch.empty(n, 1, c, device="cuda", dtype=BF).normal_(0.5, generator=g)
+    stats = torch.empty(n, groups, 2, device="cuda")
+    # (two values next to one another have a large r: an eps that holds it to 30)
+    eps = 1e-3
+    y = rrm.group_norm_act(x, groups, eps=eps, stats=stats)
+    dx, dgamma, dbeta = rrm.group_norm_act_backward(dy, x, stats)
+    s1, s2, m2 = (torch.zeros(c, device="cuda", dtype=torch.float64) for _ in range(3))
+    flat = [t.view(n, groups, cg) for t in (x, dy, y, dx)]
+    step = max(1, (1 << 25) // (n * cg)) if n < 100 else groups
+    for k in range(0, groups, step):
+        v, d, gy, gdx = (t[:, k:k + step].double() for t in flat)
+        mean = v.mean(2, keepdim=True)
+        r = 1 / torch.sqrt(((v - mean) ** 2).mean(2, keepdim=True) + eps)
+        xh = (v - mean) * r
+        slack = SUM * (8 * r + 1) + GATE
+        close(gy, xh, slack + V * (xh.abs() + slack), "y")
+        want = r * (d - d.mean(2, keepdim=True) - xh * (d * xh).mean(2, keepdim=True))
+        off = r * 4 * (SUM + slack) * (1 + xh.abs()) ** 2 * (1 + d.abs().amax(2, keepdim=True))
+        close(gdx, want, off + V * (want.abs() + off), "dx")
+        at = slice(k * cg, (k + v.shape[1]) * cg)
+        s1[at], s2[at] = d.sum(0).view(-1), (d * xh).sum(0).view(-1)
+        m2[at] = (d.abs() * (SUM * (1 + xh.abs()) + slack)).sum(0).view(-1)
+    close(dbeta, s1, m2, "dbeta")
+    # 32 threads sum the samples of a channel one behind the other
+    close(dgamma, s2, m2 * (1 + math.sqrt(n / 32)), "dgamma")
