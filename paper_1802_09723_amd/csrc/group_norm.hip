@@ -170,10 +170,7 @@ __global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom
     __syncthreads();
     if (me.first == VEC) return;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {  // z of one multiply-add; beside the mean's own rounding the shift's is no more
-        ga[i] *= gs[1][gi[i]];
-        be[i] -= mean[i] * ga[i];
-    }
+    for (int i = 0; i < VEC; ++i) ga[i] *= gs[1][gi[i]];
     TY* ys = y + sample * d.y_sample + c;
     with_act(d.act, [&](auto act) {
 #pragma unroll
@@ -181,8 +178,8 @@ __global__ __launch_bounds__(THREADS) void held_kernel(rrm_norm_desc d, HeldGeom
             const int pos = row + j * R;
             if (pos >= d.positions) continue;
             float o[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) o[i] = act_value<decltype(act)::value>(v[j].get(i) * ga[i] + be[i]);
+#pragma unroll  // (the mean comes off first: a constant gives beta, whatever eps)
+            for (int i = 0; i < VEC; ++i) o[i] = act_value<decltype(act)::value>((v[j].get(i) - mean[i]) * ga[i] + be[i]);
             store_some<VEC>(ys + pos * d.y_position, o, me.keep);
         }
     });

@@ -296,3 +296,21 @@ def test_norm_of_very_many_samples_or_groups(n, c, groups):
     close(dbeta, s1, m2, "dbeta")
     # 32 threads sum the samples of a channel one behind the other
     close(dgamma, s2, m2 * (1 + math.sqrt(n / 32)), "dgamma")
+
+
+# -- values ------------------------------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("ty", [torch.float32, BF])
+@pytest.mark.parametrize("shape", [(1, 8, 8, 32, 4), (2, 16, 16, 64, 8), (3, 64, 64, 16, 2), (1, 256, 256, 32, 2)])
+def test_norm_of_constant_groups_is_beta(shape, ty):
+    """Groups of one value each, whose sums (of powers of two of them) are exact: z is beta, to the bit, for a small eps too.  Its own shift and scale
+    folded into one multiply-add would leave the rounding of mean / sqrt(eps)."""
+    n, h, w, c, groups = shape
+    beta = torch.tensor([0.1, 0.5, 0.25, -0.7], device="cuda").repeat(c // 4)
+    gamma = torch.linspace(0.5, 2.0, c, device="cuda")
+    for value in (1.0, 100.0, 1000.0, -3.0):
+        for eps in (1e-5, 1e-12, 1e-30):
+            x = torch.full((n, h, w, c), value, device="cuda", dtype=ty)
+            y = rrm.group_norm_act(x, groups, gamma, beta, eps=eps, out_dtype=torch.float32)
+            assert torch.equal(y, beta.expand_as(y)), (value, eps, float((y - beta).abs().max()))
