@@ -5,6 +5,9 @@ two (``gated_ff``: one) that the C calls take, and nothing is copied to make the
 in, and the workspace, are allocated by torch.  With ``stream`` a call runs as if that stream were the current one, its allocations
 included; the caller orders it behind what its inputs wait for, and what uses its results behind it.
 
+The calls are not differentiable by autograd: their gradients are the ``*_backward`` functions.  A tensor that requires a gradient is refused where autograd
+records (under ``torch.no_grad()``, and inside an ``autograd.Function``, it is not), as the results would silently carry none.
+
 What the checks of a call look at (shapes, strides, types) decides its descriptor and workspace too, so both are kept by it: a call with the
 shapes of an earlier one takes them from a table and goes on to the pointers.  (One frame of a live video, host time of a call:
 12 us with every check and structure made anew, 7 so.)
@@ -56,7 +59,7 @@ def _keep(key, desc, size_of: str, backward: int):
 
 def _look(t):
     """What the checks look at (of a tensor made for the call nothing: its like always passes)."""
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda)
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda, t.requires_grad and torch.is_grad_enabled())
 
 
 def _ptr(t):
@@ -80,6 +83,9 @@ def _expect(t, what: str, shape, dtype=None) -> None:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: requires a gradient, which the result would not carry: call under torch.no_grad() and take the "
+                         "gradient from the *_backward function")
 
 
 def _dense(t, what: str, shape, dtype) -> None:

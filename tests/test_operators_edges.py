@@ -314,3 +314,67 @@ def test_norm_of_constant_groups_is_beta(shape, ty):
             x = torch.full((n, h, w, c), value, device="cuda", dtype=ty)
             y = rrm.group_norm_act(x, groups, gamma, beta, eps=eps, out_dtype=torch.float32)
             assert torch.equal(y, beta.expand_as(y)), (value, eps, float((y - beta).abs().max()))
+
+
+# -- tensors that do not belong ------------------------------------------------------------------------------------------------------
+
+class Device(torch.Tensor):
+    """A tensor that says it is on a device"""
+    at = torch.device("cuda", 0)
+    is_cuda = True
+
+    @property
+    def device(self):
+        return self.at
+
+
+class OtherDevice(Device):
+    at = torch.device("cuda", 1)
+
+
+@pytest.fixture
+def without_a_device(monkeypatch):
+    """Calls end at a library that does nothing; tensors are CPU ones that say otherwise."""
+    class Library:
+        def __getattr__(self, name):
+            return (lambda *a: 0)
+
+    class Stream:
+        cuda_stream = 0x100
+
+    monkeypatch.setattr(ops, "lib", Library)
+    monkeypatch.setattr(ops, "_plans", {})
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: False)
+
+
+def inputs_of(name, kind=Device):
+    call, dtype, shapes = CALLS[name]
+    return call, [torch.zeros(shape, dtype=dtype).as_subclass(kind) for shape in shapes]
+
+
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "marks"])
+def test_gradients_are_not_lost_in_silence(name, without_a_device):
+    """Every input that requires a gradient is refused where autograd records, also when the same call has been made without."""
+    call, inputs = inputs_of(name)
+    call(inputs)
+    for t in inputs:
+        t.requires_grad_()
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(inputs)
+        with torch.no_grad():
+            call(inputs)
+        with pytest.raises(ValueError, match="no_grad"):
+            call(inputs)
+        t.requires_grad_(False)
+    call(inputs)
+
+
+def test_gradients_of_the_parameters_are_not_lost_in_silence(without_a_device):
+    call, (x,) = inputs_of("norm")
+    gamma, beta = (torch.zeros(8, requires_grad=True).as_subclass(Device) for _ in range(2))
+    for kw in (dict(gamma=gamma), dict(beta=beta)):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            rrm.group_norm_act(x, 2, **kw)
+        with torch.no_grad():
+            rrm.group_norm_act(x, 2, **kw)
