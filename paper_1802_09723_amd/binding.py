@@ -131,17 +131,24 @@ def _check(st: int, allow_range: bool = False) -> int:
     return st
 
 
-def _stream_ptr(stream) -> Optional[int]:
+def _stream_ptr(stream, device: Optional[int] = None) -> Optional[int]:
+    """``device``: where the call's tensors are; the current stream is the current device's, and has to be there."""
     if stream is None:
         import torch
         # torch.cuda.current_stream() builds a Stream object, 2.8 us of a step whose C call takes 2.9 (one int8 16 -> 16 layer of
         # 32 x 32, one live video: 6.6 us a step with it, 4.5 without)
         if torch.cuda.is_initialized():
             try:
-                return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+                here = torch._C._cuda_getDevice()
+                if device is not None and device != here:
+                    raise ValueError(f"tensors on device {device}, but the current device is {here}")
+                return torch._C._cuda_getCurrentRawStream(here) or None
             except AttributeError:  # (torch's own names, which another version need not have)
                 pass
-        return torch.cuda.current_stream().cuda_stream or None
+        current = torch.cuda.current_stream()
+        if device is not None and device != current.device.index:
+            raise ValueError(f"tensors on device {device}, but the current device is {current.device.index}")
+        return current.cuda_stream or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

@@ -44,22 +44,25 @@ class FFDesc(ctypes.Structure):
                 + [("unaligned", ctypes.c_int)])
 
 
-# (descriptor, reference to it, bytes of workspace) by what the checks looked at.  Emptied when it has grown past what a program's
+# (descriptor, reference to it, bytes of workspace, device) by what the checks looked at.  Emptied when it has grown past what a program's
 # shapes come to.
 _plans: dict = {}
 
 
-def _keep(key, desc, size_of: str, backward: int):
+def _keep(key, desc, size_of: str, backward: int, *tensors):
+    devices = {t.device.index for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError(f"tensors on several devices: {sorted(devices)}")
     if len(_plans) > 4096:
         _plans.clear()
     ref = ctypes.byref(desc)
-    _plans[key] = plan = (desc, ref, getattr(lib(), size_of)(ref, backward))
+    _plans[key] = plan = (desc, ref, getattr(lib(), size_of)(ref, backward), devices.pop())
     return plan
 
 
 def _look(t):
     """What the checks look at (of a tensor made for the call nothing: its like always passes)."""
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda, t.requires_grad and torch.is_grad_enabled())
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device, t.requires_grad and torch.is_grad_enabled())
 
 
 def _ptr(t):
@@ -182,10 +185,10 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
         _dense(stats, "stats", (n, groups, 2), torch.float32)
         positions = x.numel() // (n * c) if n and c else 0
         plan = _keep(key, NormDesc(n, positions, c, int(groups), _elem(x), _elem(out), _act(act), float(eps), *_outer_inner(x, "x"),
-                                   *_outer_inner(out, "out"), 0, 0), "rrm_group_norm_workspace", 0)
+                                   *_outer_inner(out, "out"), 0, 0), "rrm_group_norm_workspace", 0, x, out, gamma, beta, stats)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act(plan[1], x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
-                                    _stream_ptr(None)))
+                                    _stream_ptr(None, plan[3])))
     return out
 
 
@@ -208,10 +211,10 @@ def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "non
         _dense(beta, "beta", (c,), torch.float32)
         _dense(stats, "stats", (n, groups, 2), torch.float32)
         plan = _keep(key, NormDesc(n, h * w, c, int(groups), 0, 1, _act(act), float(eps), h * w * c, c, *_outer_inner(out, "out"), 0, 0),
-                     "rrm_group_norm_workspace", 0)
+                     "rrm_group_norm_workspace", 0, out, gamma, beta, stats)
     ws = _workspace(plan[2], out.device)
     _check(lib().rrm_group_norm_act(plan[1], layer.snapshot_ptrs()[1], _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
-                                    _stream_ptr(None)))
+                                    _stream_ptr(None, plan[3])))
     return out
 
 
@@ -245,10 +248,11 @@ def group_norm_act_backward(dy, x, stats, gamma=None, beta=None, act: str = "non
             _dense(t, what, (c,), torch.float32)
         positions = x.numel() // (n * c) if n and c else 0
         plan = _keep(key, NormDesc(n, positions, c, groups, _elem(x), _elem(dy), _act(act), 1.0, *_outer_inner(x, "x"),
-                                   *_outer_inner(dy, "dy"), *_outer_inner(dx, "dx")), "rrm_group_norm_workspace", 1)
+                                   *_outer_inner(dy, "dy"), *_outer_inner(dx, "dx")), "rrm_group_norm_workspace", 1, x, dy, stats, gamma, beta, dx, dgamma,
+                     dbeta)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act_backward(plan[1], x.data_ptr(), stats.data_ptr(), _ptr(gamma), _ptr(beta), dy.data_ptr(), dx.data_ptr(),
-                                             dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None)))
+                                             dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return dx, dgamma, dbeta
 
 
@@ -288,10 +292,10 @@ def gated_scan(x, f, h0=None, lengths=None, out=None, h_last=None, marks=None, s
         _dense(lengths, "lengths", (n,), torch.int32)
         _dense(marks, "marks", (n, -(-t // MARK_FRAMES), c), torch.float32)
         plan = _keep(key, ScanDesc(n, t, c, _elem(x), *_frames(x, "x"), *_frames(f, "f"), *_frames(out, "out"), 0, 0, 0, 0),
-                     "rrm_gated_scan_workspace", 0)
+                     "rrm_gated_scan_workspace", 0, x, f, h0, lengths, out, h_last, marks)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_scan(plan[1], x.data_ptr(), f.data_ptr(), _ptr(h0), _ptr(lengths), out.data_ptr(), h_last.data_ptr(), _ptr(marks),
-                                _ptr(ws), plan[2], _stream_ptr(None)))
+                                _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return out, h_last
 
 
@@ -321,10 +325,10 @@ def gated_scan_backward(dy, x, f, marks, lengths=None, dh_last=None, dx=None, df
         _dense(dh_last, "dh_last", (n, c), torch.float32)
         _dense(dh0, "dh0", (n, c), torch.float32)
         plan = _keep(key, ScanDesc(n, t, c, _elem(x), *_frames(x, "x"), *_frames(f, "f"), *_frames(dy, "dy"), *_frames(dx, "dx"),
-                                   *_frames(df, "df")), "rrm_gated_scan_workspace", 1)
+                                   *_frames(df, "df")), "rrm_gated_scan_workspace", 1, x, f, dy, marks, lengths, dh_last, dx, df, dh0)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_scan_backward(plan[1], x.data_ptr(), f.data_ptr(), marks.data_ptr(), _ptr(lengths), dy.data_ptr(), _ptr(dh_last),
-                                         dx.data_ptr(), df.data_ptr(), dh0.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None)))
+                                         dx.data_ptr(), df.data_ptr(), dh0.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return dx, df, dh0
 
 
@@ -358,9 +362,9 @@ def gated_ff(x, wg, wu, act: str = "silu", out=None, save=None, stream=None):
             saved = _row(g, "save[0]")
             if _row(u, "save[1]") != saved:
                 raise ValueError("save: both tensors need the same strides")
-        plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, saved, 0, 0, 0, int(loose)), "rrm_gated_ff_workspace", 0)
+        plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, saved, 0, 0, 0, int(loose)), "rrm_gated_ff_workspace", 0, x, wg, wu, out, g, u)
     ws = _workspace(plan[2], x.device)
-    _check(lib().rrm_gated_ff(plan[1], px, pg, pu, out.data_ptr(), _ptr(g), _ptr(u), _ptr(ws), plan[2], _stream_ptr(None)))
+    _check(lib().rrm_gated_ff(plan[1], px, pg, pu, out.data_ptr(), _ptr(g), _ptr(u), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return out
 
 
@@ -389,8 +393,8 @@ def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None,
         for t, what, shape in ((x, "x", (m, k)), (wg, "wg", (f, k)), (wu, "wu", (f, k)), (g, "g", (m, f)), (u, "u", (m, f)), (dh, "dh", (m, f)),
                                (dx, "dx", (m, k)), (dwg, "dwg", (f, k)), (dwu, "dwu", (f, k))):
             _expect(t, what, shape, bf)
-        plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, int(loose)), "rrm_gated_ff_workspace", 1)
+        plan = _keep(key, FFDesc(m, k, f, _act(act), *rows, int(loose)), "rrm_gated_ff_workspace", 1, x, wg, wu, dh, g, u, dx, dwg, dwu)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_gated_ff_backward(plan[1], px, pg, pu, g.data_ptr(), u.data_ptr(), dh.data_ptr(), dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(),
-                                       _ptr(ws), plan[2], _stream_ptr(None)))
+                                       _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return dx, dwg, dwu

@@ -341,6 +341,7 @@ def without_a_device(monkeypatch):
 
     class Stream:
         cuda_stream = 0x100
+        device = torch.device("cuda", 0)
 
     monkeypatch.setattr(ops, "lib", Library)
     monkeypatch.setattr(ops, "_plans", {})
@@ -378,3 +379,29 @@ def test_gradients_of_the_parameters_are_not_lost_in_silence(without_a_device):
             rrm.group_norm_act(x, 2, **kw)
         with torch.no_grad():
             rrm.group_norm_act(x, 2, **kw)
+
+
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "marks"])
+def test_tensors_of_several_devices_are_refused(name, without_a_device):
+    call, inputs = inputs_of(name)
+    call(inputs)
+    for k in range(1, len(inputs)):
+        mixed = [t.as_subclass(OtherDevice) if i == k else t for i, t in enumerate(inputs)]
+        with pytest.raises(ValueError, match="several devices"):
+            call(mixed)
+
+
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "marks"])
+def test_tensors_of_another_device_than_the_current_one_are_refused(name, without_a_device, monkeypatch):
+    """The launch would go to the current device: also when the same call was right before."""
+    call, inputs = inputs_of(name)
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0x100, raising=False)
+    call(inputs)
+    current[0] = 1
+    with pytest.raises(ValueError, match="current device is 1"):
+        call(inputs)
+    current[0] = 0
+    call(inputs)
