@@ -405,3 +405,26 @@ def test_tensors_of_another_device_than_the_current_one_are_refused(name, withou
         call(inputs)
     current[0] = 0
     call(inputs)
+
+
+# -- the package -----------------------------------------------------------------------------------------------------------------------
+
+def test_the_package_is_imported_without_torch():
+    """Building the library, and layers' shapes and names, need none of it; the operators bring it when they are asked for."""
+    code = """
+import sys
+sys.path.insert(0, sys.argv[1])
+import paper_1802_09723_amd as rrm
+import paper_1802_09723_amd.build
+assert "torch" not in sys.modules
+assert {"gated_ff", "gated_scan_marks", "group_norm_act_of"} <= set(dir(rrm))
+try:
+    rrm.nothing
+except AttributeError:
+    pass
+from paper_1802_09723_amd import gated_scan, operators
+assert rrm.gated_scan is gated_scan is operators.gated_scan and "torch" in sys.modules
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code, root], capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0, done.stderr
