@@ -378,6 +378,16 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
                                  const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* workspace,
                                  size_t workspace_bytes, void* hip_stream);
 
+/* Which form of its kernels a call with this descriptor takes (host only; for tests and measurements).
+ * norm: layout[0] the size of workgroup, 0 to 3, that holds a sample in registers, -1: slices; [1] channels of a workgroup (slices: their number)
+ * scan: layout[0] 0: a thread a feature, 1: a workgroup a chain of blocks, 2: many; [1] frames of a block (0: none)
+ * ff:   asked: 0 the forward pass, else 1 (dX) + 2 (dW); layout[0], [1] the tile shape (0 to 3; -1: few rows) and the parts of the summed axis of
+ *       the forward pass or dX, [2], [3] of dW, [4] whether one launch makes both (what is not asked for: -2, 0)
+ * Errors: the descriptor's, RRM_ERR_NULL. */
+rrm_status rrm_aux_norm_layout(const rrm_norm_desc* desc, int backward, int layout[2]);
+rrm_status rrm_aux_scan_layout(const rrm_scan_desc* desc, int backward, int layout[2]);
+rrm_status rrm_aux_ff_layout(const rrm_ff_desc* desc, int asked, int layout[5]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,7 +107,8 @@ def lib():
         L.rrm_gated_ff.argtypes = [B, P, P, P, P, P, P, P, S, P]
         L.rrm_gated_ff_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, S, P]
         L.rrm_scan_marks.argtypes = [I]
-        for f in ("rrm_group_norm_act", "rrm_group_norm_act_backward", "rrm_gated_scan", "rrm_gated_scan_backward", "rrm_gated_ff",
+        L.rrm_aux_norm_layout.argtypes = L.rrm_aux_scan_layout.argtypes = L.rrm_aux_ff_layout.argtypes = [B, I, P]
+        for f in ("rrm_aux_norm_layout", "rrm_aux_scan_layout", "rrm_aux_ff_layout", "rrm_group_norm_act", "rrm_group_norm_act_backward", "rrm_gated_scan", "rrm_gated_scan_backward", "rrm_gated_ff",
                   "rrm_gated_ff_backward", "rrm_scan_marks"):
             getattr(L, f).restype = I
         _lib = L

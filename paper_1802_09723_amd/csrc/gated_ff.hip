@@ -796,6 +796,21 @@ size_t ff_scratch(const rrm_ff_desc& d, bool backward) {
     return (backward ? 2 * grads_bytes(d) : 0) + padded_places(d, true, true).all + split_bytes(d, backward);
 }
 
+void ff_layout(const rrm_ff_desc& d, int asked, int* layout) {
+    layout[0] = layout[2] = -2;
+    layout[1] = layout[3] = layout[4] = 0;
+    if (asked == 0) {
+        const Plan p = forward_plan(d);
+        layout[0] = few_rows(d) ? -1 : p.shape;
+        layout[1] = few_rows(d) ? 1 : p.splits;
+        return;
+    }
+    const GradientsPlan p = gradients_plan(d, asked & 1, asked & 2);
+    if (asked & 1) layout[0] = p.x_shape, layout[1] = p.x_splits;
+    if (asked & 2) layout[2] = p.w_shape, layout[3] = p.w_splits;
+    layout[4] = p.together;
+}
+
 hipError_t launch_gated_ff(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* ws,
                            hipStream_t s) {
     hipError_t e = hipSuccess;

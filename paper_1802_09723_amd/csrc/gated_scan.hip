@@ -810,6 +810,14 @@ size_t scan_scratch(const rrm_scan_desc& d, bool backward) {
     return round256((size_t)Plan(d, backward, nullptr).words * sizeof(word_t));
 }
 
+void scan_layout(const rrm_scan_desc& d, bool backward, int* layout) {
+    layout[0] = layout[1] = 0;
+    if (d.t == 0 || (!backward && few_frames(d))) return;
+    const bool chained = Plan(d, backward, nullptr).chained;
+    layout[0] = chained ? 2 : 1;
+    layout[1] = backward ? (chained ? GS_BLOCK : BACK_BLOCK) : chained ? forward_block(d) : GS_BLOCK;
+}
+
 hipError_t launch_gated_scan(const rrm_scan_desc& d, const void* x, const void* f, const float* h0, const int32_t* lengths,
                              void* y, float* h_last, float* marks, void* ws, hipStream_t s) {
     if (d.t == 0) {

@@ -693,7 +693,7 @@ SliceGeom plan_slices(const rrm_norm_desc& d, int vec) {
 }
 int wide_of(const rrm_norm_desc& d) { return d.x_elem == RRM_F32 ? 4 : 8; }
 int slice_vec(const rrm_norm_desc& d) { return d.c >= wide_of(d) ? wide_of(d) : 1; }
-bool held(const rrm_norm_desc& d, bool backward) { return plan_held(d, wide_of(d), backward ? BACKWARD : FORWARD).which >= 0; }
+HeldPlan plan_held(const rrm_norm_desc& d, bool backward) { return plan_held(d, wide_of(d), backward ? BACKWARD : FORWARD); }
 size_t group_bytes(const rrm_norm_desc& d) { return round256((size_t)d.n * d.groups * 8); }
 
 int64_t held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (int64_t)parts(d.n, 8) * 8 * p.g.blocks; }
@@ -702,8 +702,14 @@ int64_t held_grid(const rrm_norm_desc& d, const HeldPlan& p) { return (int64_t)p
 
 // backward, held: the samples' sums [2][n][c]; else the slices' sums, (backward) the samples' and the groups' two values
 size_t norm_scratch(const rrm_norm_desc& d, bool backward) {
-    if (held(d, backward)) return backward ? round256((size_t)2 * d.n * d.c * 4) : 0;
+    if (plan_held(d, backward).which >= 0) return backward ? round256((size_t)2 * d.n * d.c * 4) : 0;
     return round256((size_t)2 * d.n * plan_slices(d, slice_vec(d)).slices * d.c * 4) + (backward ? round256((size_t)2 * d.n * d.c * 4) : 0) + group_bytes(d);
+}
+
+void norm_layout(const rrm_norm_desc& d, bool backward, int* layout) {
+    const HeldPlan p = plan_held(d, backward);
+    layout[0] = p.which;
+    layout[1] = p.which >= 0 ? p.g.cb : plan_slices(d, slice_vec(d)).slices;
 }
 
 hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float* gamma, const float* beta, void* y, float* stats,

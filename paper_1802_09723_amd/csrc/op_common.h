@@ -222,7 +222,10 @@ void in_parts(int64_t total, F&& f) {
 #endif  // __HIPCC__
 
 // Launchers; descriptors have been checked, and something is to be done.  The *_scratch functions say how many bytes of
-// workspace the same descriptor takes.
+// workspace the same descriptor takes, the *_layout functions which kernels (rrm_aux_*_layout).
+void norm_layout(const rrm_norm_desc& d, bool backward, int* layout);
+void scan_layout(const rrm_scan_desc& d, bool backward, int* layout);
+void ff_layout(const rrm_ff_desc& d, int asked, int* layout);
 size_t norm_scratch(const rrm_norm_desc& d, bool backward);
 hipError_t launch_group_norm(const rrm_norm_desc& d, const void* x, const float* gamma, const float* beta, void* y, float* stats,
                              void* ws, hipStream_t s);

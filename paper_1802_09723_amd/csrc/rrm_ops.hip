@@ -216,5 +216,30 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
     return finish(launch_gated_ff_backward(d, x, wg, wu, g, u, dh, dx, dwg, dwu, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
+rrm_status rrm_aux_norm_layout(const rrm_norm_desc* desc, int backward, int layout[2]) {
+    if (rrm_status st = check(desc)) return st;
+    if (!layout) return record_failure(RRM_ERR_NULL, "layout is NULL");
+    if (desc->n == 0 || desc->positions == 0) return record_failure(RRM_ERR_SHAPE, "group norm: nothing to do");
+    norm_layout(*desc, backward != 0, layout);
+    return RRM_OK;
+}
+
+rrm_status rrm_aux_scan_layout(const rrm_scan_desc* desc, int backward, int layout[2]) {
+    if (rrm_status st = check(desc)) return st;
+    if (!layout) return record_failure(RRM_ERR_NULL, "layout is NULL");
+    if (desc->n == 0 || desc->c == 0) return record_failure(RRM_ERR_SHAPE, "gated scan: nothing to do");
+    scan_layout(*desc, backward != 0, layout);
+    return RRM_OK;
+}
+
+rrm_status rrm_aux_ff_layout(const rrm_ff_desc* desc, int asked, int layout[5]) {
+    if (rrm_status st = check(desc)) return st;
+    if (!layout) return record_failure(RRM_ERR_NULL, "layout is NULL");
+    if (asked < 0 || asked > 3) return record_failure(RRM_ERR_OPTION, "feed-forward: asked is 0, or 1 (dX) + 2 (dW)");
+    if (desc->m == 0) return record_failure(RRM_ERR_SHAPE, "feed-forward: nothing to do");
+    ff_layout(*desc, asked, layout);
+    return RRM_OK;
+}
+
 #pragma GCC visibility pop
 }  // extern "C"
