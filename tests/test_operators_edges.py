@@ -12,7 +12,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_operators import GATE, SUM, U, V, _norm_desc, gen
+from test_operators import GATE, SUM, U, V, _norm_desc, act64, gen
 
 gpu = pytest.mark.gpu
 
@@ -428,3 +428,179 @@ assert rrm.gated_scan is gated_scan is operators.gated_scan and "torch" in sys.m
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", code, root], capture_output=True, text=True, timeout=100)
     assert done.returncode == 0, done.stderr
+
+
+# -- the feed-forward block's tiles ------------------------------------------------------------------------------------------------------
+
+def ff_layout(m, k, f, asked):
+    d = ops.FFDesc(m, k, f, 2, k, k, k, f, f, k, k, k, 0)
+    layout = (ctypes.c_int * 5)()
+    assert rrm.lib().rrm_aux_ff_layout(ctypes.byref(d), asked, layout) == 0
+    return list(layout)
+
+
+# Shapes of every kind of tile, over more than four steps of 64 of the summed axis and by parts of it or not, ragged everywhere; rows of k that are copied
+# and padded (odd k), and rows that are read where they lie
+FF_FORWARD = {
+    (0, False): [(4807, 305, 853), (2773, 304, 1529)], (0, True): [(4327, 4919, 67), (4123, 4072, 69)],
+    (1, False): [(193, 321, 4075), (261, 320, 3491)], (1, True): [(17, 1995, 1479), (17, 1280, 2647)],
+    (2, False): [(4709, 349, 385), (1095, 312, 1803)], (2, True): [(2109, 4757, 17), (4299, 2328, 23)],
+    (3, False): [(19, 321, 17), (19, 312, 17)], (3, True): [(17, 1081, 19), (19, 1048, 19)],
+}
+FF_DX = {
+    (0, False): [(3451, 2559, 301), (3535, 2576, 329)], (0, True): [(2243, 137, 3841), (4463, 168, 2463)],
+    (1, False): [(451, 4225, 311), (4747, 400, 305)], (1, True): [(4197, 17, 465), (2085, 24, 979)],
+    (2, False): [(4733, 839, 303), (965, 4288, 301)], (2, True): [(2049, 17, 2021), (4315, 24, 1001)],
+    (3, False): [(19, 17, 305), (23, 24, 305)], (3, True): [(17, 17, 469), (17, 24, 525)],
+}
+FF_DW = {
+    (0, False): [(311, 2179, 1801), (325, 2184, 1803)], (0, True): [(3523, 131, 4769), (4985, 136, 2971)],
+    (1, False): [(313, 129, 4505), (313, 144, 4749)], (1, True): [(4197, 17, 465), (2085, 24, 979)],
+    (2, False): [(319, 439, 4181), (309, 408, 4743)], (2, True): [(4863, 17, 1057), (2413, 24, 2211)],
+    (3, False): [(315, 17, 19), (343, 24, 17)], (3, True): [(969, 19, 17), (997, 24, 19)],
+}
+# one launch for dX and both dW: (tile, dX by parts, dW by parts)
+FF_BOTH = {
+    (0, False, False): (905, 4413, 469), (0, False, True): (3373, 1241, 139), (0, True, False): (129, 1305, 2557), (0, True, True): (4969, 139, 1091),
+    (1, False, False): (17, 3995, 401), (1, False, True): (4087, 161, 119), (1, True, False): (17, 1349, 1003), (1, True, True): (1059, 17, 1075),
+    (2, False, False): (391, 4763, 197), (2, False, True): (4605, 607, 69), (2, True, False): (71, 1243, 2063), (2, True, True): (1127, 17, 2201),
+    (3, False, False): (17, 19, 17), (3, False, True): (1001, 17, 17), (3, True, False): (19, 17, 449), (3, True, True): (987, 17, 243),
+}
+# a launch each: (tile of dX, of dW)
+FF_APART = {
+    (0, 1): (4299, 3749, 65), (0, 2): (4289, 3597, 147), (0, 3): (3307, 4667, 129), (1, 0): (215, 1851, 3891), (1, 1): (289, 2685, 3677),
+    (1, 2): (621, 1453, 2671), (1, 3): (2863, 1405, 1437), (2, 0): (271, 4327, 3031), (2, 1): (1541, 4863, 273), (2, 2): (579, 2649, 3039),
+    (2, 3): (4879, 1589, 547), (3, 0): (265, 1467, 4367), (3, 2): (315, 3155, 2437),
+}
+
+
+def ff_case(m, k, f):
+    g = torch.Generator(device="cuda").manual_seed(m + 3 * k + 7 * f)
+
+    def normal(*shape, scale=1.0):
+        return torch.empty(shape, device="cuda").normal_(0.0, scale, generator=g).bfloat16()
+
+    return normal(m, k), normal(f, k, scale=k ** -0.5), normal(f, k, scale=k ** -0.5), normal(m, f)
+
+
+def rounded(slack, want):
+    """slack, and the rounding to bfloat16"""
+    return slack + V * (want.abs() + slack)
+
+
+def ff_forward_close(x, wg, wu, act, h, g, u):
+    """as test_operators' ff_check, on the device"""
+    x64, wg64, wu64 = x.double(), wg.double(), wu.double()
+    g64, u64 = x64 @ wg64.t(), x64 @ wu64.t()
+    sg, su = SUM * (x64.abs() @ wg64.abs().t()), SUM * (x64.abs() @ wu64.abs().t())
+    close(g, g64, rounded(sg, g64), "g")
+    close(u, u64, rounded(su, u64), "u")
+    a64 = act64(act, g64)
+    close(h, a64 * u64, rounded((1.2 * sg + GATE * (1 + g64.abs())) * (u64.abs() + su) + a64.abs() * su, a64 * u64), "h")
+
+
+def ff_backward_close(x, wg, wu, dh, g, u, act, dx=None, dw=None):
+    g64 = g.double().requires_grad_()
+    p = act64(act, g64)
+    slope = torch.autograd.grad(p.sum(), g64)[0]
+    p, u64, d64 = p.detach(), u.double(), dh.double()
+    dg, du = d64 * u64 * slope, d64 * p
+    # dG and dU are rounded before the products: V of each term, at random signs; eight deviations of such a sum
+    eg, eu = dg.abs() * (V + GATE) + GATE * (d64 * u64).abs(), du.abs() * (V + GATE) + GATE * d64.abs()
+
+    def off(e, w):
+        return SUM * (e / V).matmul(w.abs()) + 8 * torch.sqrt((e * e).matmul(w * w)) + GATE * e.matmul(w.abs())
+
+    x64, wg64, wu64 = x.double(), wg.double(), wu.double()
+    if dx is not None:
+        want = dg @ wg64 + du @ wu64
+        close(dx, want, rounded(off(eg, wg64) + off(eu, wu64), want), "dx")
+    if dw is not None:
+        for got, d, e, what in ((dw[0], dg, eg, "dwg"), (dw[1], du, eu, "dwu")):
+            want = d.t() @ x64
+            close(got, want, rounded(off(e.t(), x64), want), what)
+
+
+def ff_saved(x, wg, wu):
+    """projections for a backward pass by itself"""
+    return (x.float() @ wg.float().t()).bfloat16(), (x.float() @ wu.float().t()).bfloat16()
+
+
+def ff_gradients(x, wg, wu, g, u, dh, act, dx, dwg, dwu):
+    """The C call: the gradients that are not given are not asked for."""
+    (m, k), f = x.shape, wg.shape[0]
+    d = ops.FFDesc(m, k, f, ops.ACTS[act], k, k, k, f, f, k, k, k, 0)
+    need = rrm.lib().rrm_gated_ff_workspace(ctypes.byref(d), 1)
+    ws = torch.empty(need, device="cuda", dtype=torch.uint8)
+    at = [t if t is None else t.data_ptr() for t in (x, wg, wu, g, u, dh, dx, dwg, dwu)]
+    assert rrm.lib().rrm_gated_ff_backward(ctypes.byref(d), *at, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+
+
+def act_of(m, k, f):
+    return ("silu", "gelu")[(m + k + f) // 2 % 2]
+
+
+@gpu
+@pytest.mark.parametrize("tile,split,shape", [(*q, s) for q, v in FF_FORWARD.items() for s in v])
+def test_ff_forward_of_every_tile(tile, split, shape):
+    layout = ff_layout(*shape, 0)
+    assert layout[0] == tile and (layout[1] > 1) == split, layout
+    x, wg, wu, _ = ff_case(*shape)
+    m, k, f = shape
+    act = act_of(*shape)
+    g, u = torch.empty(m, f, device="cuda", dtype=BF), torch.empty(m, f, device="cuda", dtype=BF)
+    h = rrm.gated_ff(x, wg, wu, act, save=(g, u))
+    ff_forward_close(x, wg, wu, act, h, g, u)
+    assert torch.equal(rrm.gated_ff(x, wg, wu, act), h)
+    # not-a-numbers and infinities stay in their row and feature, also in the last ones
+    x[m - 1, k - 1], x[1, k // 2], wg[f - 1, k - 1], wu[f // 2, 0] = math.nan, math.inf, math.nan, math.inf
+    spoilt = rrm.gated_ff(x, wg, wu, "none")
+    x[m - 1, k - 1], x[1, k // 2], wg[f - 1, k - 1], wu[f // 2, 0] = 0, 0, 0, 0
+    clean = rrm.gated_ff(x, wg, wu, "none")
+    assert not torch.isfinite(spoilt[[1, m - 1]]).any() and not torch.isfinite(spoilt[:, f // 2]).any()
+    for t in (spoilt, clean):
+        t[[1, m - 1]] = 0
+        t[:, [f // 2, f - 1]] = 0
+    # (elsewhere the zeros put in their places count for nothing: those rows and features were not the others')
+    assert torch.equal(spoilt, clean)
+
+
+@gpu
+@pytest.mark.parametrize("tile,split,shape", [(*q, s) for q, v in FF_DX.items() for s in v])
+def test_ff_input_gradient_of_every_tile(tile, split, shape):
+    layout = ff_layout(*shape, 1)
+    assert layout[0] == tile and (layout[1] > 1) == split, layout
+    x, wg, wu, dh = ff_case(*shape)
+    g, u = ff_saved(x, wg, wu)
+    dx = torch.full_like(x, 7.0)
+    ff_gradients(x, wg, wu, g, u, dh, act_of(*shape), dx, None, None)
+    ff_backward_close(x, wg, wu, dh, g, u, act_of(*shape), dx=dx)
+
+
+@gpu
+@pytest.mark.parametrize("tile,split,shape", [(*q, s) for q, v in FF_DW.items() for s in v])
+def test_ff_weights_gradients_of_every_tile(tile, split, shape):
+    layout = ff_layout(*shape, 2)
+    assert layout[2] == tile and (layout[3] > 1) == split, layout
+    x, wg, wu, dh = ff_case(*shape)
+    g, u = ff_saved(x, wg, wu)
+    dw = torch.full_like(wg, 7.0), torch.full_like(wu, 7.0)
+    ff_gradients(x, wg, wu, g, u, dh, act_of(*shape), None, *dw)
+    ff_backward_close(x, wg, wu, dh, g, u, act_of(*shape), dw=dw)
+
+
+@gpu
+@pytest.mark.parametrize("form", [*FF_BOTH, *FF_APART], ids=str)
+def test_ff_gradients_together_and_apart(form):
+    shape = FF_BOTH[form] if form in FF_BOTH else FF_APART[form]
+    layout = ff_layout(*shape, 3)
+    if form in FF_BOTH:
+        assert layout[4] == 1 and (layout[0], layout[1] > 1, layout[3] > 1) == form, layout
+    else:
+        assert layout[4] == 0 and (layout[0], layout[2]) == form, layout
+    x, wg, wu, dh = ff_case(*shape)
+    g, u = ff_saved(x, wg, wu)
+    act = act_of(*shape)
+    got = rrm.gated_ff_backward(dh, x, wg, wu, g, u, act)
+    ff_backward_close(x, wg, wu, dh, g, u, act, got[0], got[1:])
+    assert all(torch.equal(a, b) for a, b in zip(got, rrm.gated_ff_backward(dh, x, wg, wu, g, u, act)))
