@@ -12,7 +12,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_operators import GATE, SUM, U, V, _norm_desc, act64, gen
+from test_operators import DT, GATE, SUM, U, V, _norm_desc, act64, gen, norm64
 
 gpu = pytest.mark.gpu
 
@@ -604,3 +604,124 @@ def test_ff_gradients_together_and_apart(form):
     got = rrm.gated_ff_backward(dh, x, wg, wu, g, u, act)
     ff_backward_close(x, wg, wu, dh, g, u, act, got[0], got[1:])
     assert all(torch.equal(a, b) for a, b in zip(got, rrm.gated_ff_backward(dh, x, wg, wu, g, u, act)))
+
+
+# -- the norm's forms --------------------------------------------------------------------------------------------------------------------
+
+def norm_layout(n, positions, c, groups, x_elem, backward):
+    d = ops.NormDesc(n, positions, c, groups, x_elem, 0, 0, 1e-5, positions * c, c, positions * c, c, positions * c, c)
+    layout = (ctypes.c_int * 2)()
+    assert rrm.lib().rrm_aux_norm_layout(ctypes.byref(d), backward, layout) == 0
+    return layout[0], layout[1]
+
+
+# n, positions, c, groups: forms (the size of workgroup and its channels; -1: in slices) of fp32 forward and backward, of bf16 forward and backward
+NORM_FORMS = {
+    # each size of workgroup; runs of channels as narrow as they get, and widened where there are workgroups enough
+    (5000, 1, 9, 3): ((0, 9), (0, 9), (0, 9), (0, 9)), (3000, 1, 64, 4): ((0, 64), (0, 64), (0, 64), (0, 64)),
+    (1024, 7, 105, 7): ((0, 120), (0, 120), (0, 105), (0, 105)), (1100, 30, 24, 3): ((0, 32), (0, 32), (0, 24), (0, 24)),
+    (600, 10, 64, 8): ((0, 32), (0, 32), (0, 32), (0, 32)), (520, 63, 250, 25): ((1, 40), (1, 40), (1, 80), (1, 80)),
+    (64, 784, 128, 32): ((2, 16), (2, 16), (2, 32), (2, 32)), (129, 1001, 13, 13): ((2, 9), (2, 9), (2, 12), (2, 12)),
+    (8, 196, 512, 8): ((2, 64), (2, 64), (2, 64), (2, 64)), (300, 4000, 8, 1): ((3, 8), (3, 8), (2, 8), (2, 8)),
+    (64, 3136, 64, 32): ((3, 16), (3, 8), (3, 16), (3, 16)), (140, 2000, 40, 5): ((3, 16), (3, 16), (3, 32), (3, 32)),
+    (130, 3000, 40, 8): ((3, 15), (3, 5), (3, 30), (3, 15)), (256, 3000, 35, 5): ((3, 14), (3, 7), (3, 28), (3, 14)),
+    (130, 900, 17, 1): ((3, 17), (3, 17), (2, 17), (2, 17)), (300, 1, 8192, 1): ((-1, 1), (-1, 1), (3, 8192), (3, 8192)),
+    # slices: long samples, few workgroups, groups wider than a workgroup
+    (1, 22650, 36, 6): ((-1, 354), (-1, 354), (-1, 177), (-1, 177)), (1, 60000, 16, 2): ((-1, 235), (-1, 235), (-1, 118), (-1, 118)),
+    (1, 70000, 3, 1): ((-1, 274), (-1, 274), (-1, 274), (-1, 274)), (2, 3000, 1030, 10): ((-1, 250), (-1, 250), (-1, 500), (-1, 500)),
+    (1, 40, 9000, 3): ((-1, 10), (-1, 10), (-1, 10), (-1, 10)),
+}
+
+
+@gpu
+@pytest.mark.parametrize("types", [("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")], ids="-".join)
+@pytest.mark.parametrize("shape", NORM_FORMS, ids=str)
+def test_norm_of_every_form(shape, types):
+    """Element by element, with gradients in which the group's two means count as much as dz itself: dy has a mean and a part along xh."""
+    n, positions, c, groups = shape
+    e = types[0] == "bf16"
+    assert (norm_layout(*shape, int(e), 0), norm_layout(*shape, int(e), 1)) == NORM_FORMS[shape][2 * e:2 * e + 2]
+    cg, act = c // groups, ("silu", "none", "gelu", "relu")[(positions + groups) % 4]
+    gn = torch.Generator(device="cuda").manual_seed(n + c)
+
+    def normal(*s, shift=0.0, scale=1.0):
+        return torch.empty(s, device="cuda").normal_(shift, scale, generator=gn)
+
+    def grouped(t):
+        return t.view(n, positions, groups, cg)
+
+    def mean(t):
+        return grouped(t).mean((1, 3), keepdim=True).expand(n, positions, groups, cg).reshape(n, positions, c)
+
+    x = (normal(n, positions, c, scale=1.5) + normal(n, 1, c)).to(DT[types[0]])
+    gamma, beta = normal(c, shift=1.0, scale=0.2), normal(c, scale=0.3)
+    # the definition, its eps such that a group of few values has no r above 30
+    eps = 1e-3
+    v = x.double()
+    mu = mean(v)
+    r = 1 / torch.sqrt(mean((v - mu) ** 2) + eps)
+    xh = (v - mu) * r
+    z = (xh * gamma.double() + beta.double()).requires_grad_()
+    y64 = act64(act, z)
+    slope = torch.autograd.grad(y64.sum(), z)[0]
+    y64, z = y64.detach(), z.detach()
+    # what xh and z may be off by: sums in trees, the mean's own rounding times r
+    top = grouped(v).abs().amax((1, 3), keepdim=True).expand(n, positions, groups, cg).reshape(n, positions, c)
+    e_xh = SUM * (r * top + xh.abs())
+    e_z = gamma.double().abs() * e_xh + 4 * U * (z.abs() + beta.double().abs())
+    stats = torch.empty(n, groups, 2, device="cuda")
+    y = rrm.group_norm_act(x, groups, gamma, beta, act, eps=eps, out_dtype=DT[types[1]], stats=stats)
+
+    def whole(slack, want, got):
+        return slack + (V if got.dtype is BF else U) * (want.abs() + slack)
+
+    close(y, y64, whole(1.2 * e_z + GATE * (1 + z.abs()), y64, y), "y")
+    dy = (0.5 + 0.7 * xh + normal(n, positions, c)).to(DT[types[1]])
+    if act == "relu":  # where the sign of z may fall either way no gradient comes in
+        dy[z.abs() <= 4 * e_z] = 0
+    d = dy.double()
+    dz = d * slope
+    e_dz = d.abs() * (1.2 * e_z + GATE)
+    ga = gamma.double()
+    p, q = mean(ga * dz), mean(ga * dz * xh)
+    e_p = mean(ga.abs() * e_dz) + SUM * mean((ga * dz).abs())
+    e_q = mean(ga.abs() * (e_dz * xh.abs() + dz.abs() * e_xh)) + SUM * mean((ga * dz * xh).abs())
+    want = r * (ga * dz - p - xh * q)
+    off = r * (ga.abs() * e_dz + e_p + xh.abs() * e_q + q.abs() * e_xh + 8 * U * ((ga * dz).abs() + p.abs() + (xh * q).abs())) + SUM * want.abs()
+    dx, dgamma, dbeta = rrm.group_norm_act_backward(dy, x, stats, gamma, beta, act)
+    close(dx, want, whole(off, want, dx), "dx")
+    if act != "relu" and n * positions * c > 1000 and cg * positions > 8:
+        # (the bound is one that a gradient without either mean does not keep)
+        assert ((r * p).abs() > whole(off, want, dx)).any() and ((r * xh * q).abs() > whole(off, want, dx)).any()
+    close(dbeta, dz.sum((0, 1)), (e_dz + SUM * dz.abs()).sum((0, 1)), "dbeta")
+    close(dgamma, (dz * xh).sum((0, 1)), (e_dz * xh.abs() + dz.abs() * e_xh + SUM * (dz * xh).abs()).sum((0, 1)), "dgamma")
+    again = rrm.group_norm_act_backward(dy, x, stats, gamma, beta, act)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dgamma, dbeta)))
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, 9000, 12, 3), (2, 400, 40, 4)])
+def test_gradients_in_slices_and_in_large_workgroups_against_differences(shape):
+    """The derivative along random directions against the difference quotient of the definition in 64 bits."""
+    n, positions, c, groups = shape
+    assert n == 2 or norm_layout(*shape, 0, 1)[0] == -1
+    g = gen(n)
+    args = [torch.randn(n, positions, c, generator=g), 1 + 0.1 * torch.randn(c, generator=g), torch.randn(c, generator=g)]
+    dy = 0.5 + torch.randn(n, positions, c, generator=g)
+    stats = torch.empty(n, groups, 2, device="cuda")
+    dev = [a.cuda() for a in args]
+    rrm.group_norm_act(dev[0], groups, dev[1], dev[2], "silu", stats=stats)
+    grads = rrm.group_norm_act_backward(dy.cuda(), dev[0], stats, dev[1], dev[2], "silu")
+
+    def loss(v):
+        return float((norm64(v[0], groups, v[1], v[2], "silu")[0] * dy.double()).sum())
+
+    step = 1e-5
+    for k in range(3):
+        d = torch.randn(args[k].shape, generator=g).double()
+        lo, hi = [a.double() for a in args], [a.double() for a in args]
+        lo[k], hi[k] = lo[k] - step * d, hi[k] + step * d
+        quotient = (loss(hi) - loss(lo)) / (2 * step)
+        got = float((grads[k].cpu().double() * d).sum())
+        # step^2 of the third derivatives (of 36000 values, some units each), 1e-16 / step of the loss (some thousands), roundings of the gradient
+        assert abs(got - quotient) <= 1e-6 * float(grads[k].cpu().double().norm() * d.norm()) + 1e-6, (k, got, quotient)
