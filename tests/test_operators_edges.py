@@ -725,3 +725,68 @@ def test_gradients_in_slices_and_in_large_workgroups_against_differences(shape):
         got = float((grads[k].cpu().double() * d).sum())
         # step^2 of the third derivatives (of 36000 values, some units each), 1e-16 / step of the loss (some thousands), roundings of the gradient
         assert abs(got - quotient) <= 1e-6 * float(grads[k].cpu().double().norm() * d.norm()) + 1e-6, (k, got, quotient)
+
+
+# -- the scan's long blocks ----------------------------------------------------------------------------------------------------------------
+
+def scan_layout(n, t, c, elem, backward):
+    d = ops.ScanDesc(n, t, c, elem, t * c, c, t * c, c, t * c, c, t * c, c, t * c, c)
+    layout = (ctypes.c_int * 2)()
+    assert rrm.lib().rrm_aux_scan_layout(ctypes.byref(d), backward, layout) == 0
+    return layout[0], layout[1]
+
+
+@gpu
+@pytest.mark.parametrize("dtype,t", [("f32", 16384), ("f32", 16700), ("f32", 24577), ("bf16", 16700)])
+@pytest.mark.parametrize("c", [3, 5, 70])
+def test_long_scans_that_end_at_borders(dtype, t, c):
+    """Videos that end with a block of frames (128, 256), a group of 32 blocks (4096, 8192), one beside them, or at once; x and f out of a joint tensor at
+    odd addresses, frames before videos, not-a-numbers behind the ends; the same bits in every call."""
+    ends = [t, 8192, 8193, 256, 0, 16384, 4095, 1]
+    n = len(ends)
+    blocks = 256 if dtype == "f32" else 128
+    assert scan_layout(n, t, c, int(dtype == "bf16"), 0) == (2, blocks) and scan_layout(n, t, c, int(dtype == "bf16"), 1) == (2, 128)
+    g = torch.Generator(device="cuda").manual_seed(t + c)
+    joint = torch.empty(t, n, 2 * c + 3, device="cuda").normal_(generator=g)
+    joint[..., 1 + c:1 + 2 * c] += 4 * torch.rand(c, device="cuda", generator=g)
+    joint = joint.to(DT[dtype]).transpose(0, 1)
+    x, f = joint[..., 1:1 + c], joint[..., 1 + c:1 + 2 * c]
+    h0, dh = (torch.empty(n, c, device="cuda").normal_(generator=g) for _ in range(2))
+    dy = torch.empty(n, t, c, device="cuda").normal_(generator=g).to(DT[dtype])
+    lengths = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    live = (torch.arange(t, device="cuda") < lengths.view(n, 1))[..., None]
+    a = torch.where(live, torch.sigmoid(f.double()), 1.0)
+    o = torch.where(live, torch.sigmoid(-f.double()), 0.0)
+    x64, d64 = x.double(), torch.where(live, dy.double(), 0.0)
+    for i, end in enumerate(ends):
+        x[i, end:], f[i, end:], dy[i, end:] = math.nan, math.inf, math.nan
+    hs, grads = torch.empty(n, t + 1, c, device="cuda", dtype=torch.float64), torch.empty_like(d64)
+    hs[:, 0] = h0.double()
+    b = o * x64
+    for k in range(t):
+        torch.addcmul(b[:, k], a[:, k], hs[:, k], out=hs[:, k + 1])
+    carry = dh.double()
+    for k in range(t - 1, -1, -1):
+        torch.add(carry, d64[:, k], out=grads[:, k])
+        carry = grads[:, k] * a[:, k]
+    marks = rrm.gated_scan_marks(x)
+    out = torch.full((n, t, c + 2), 7.0, device="cuda", dtype=DT[dtype])
+    y, last = rrm.gated_scan(x, f, h0, lengths=lengths, out=out[..., 1:1 + c], marks=marks)
+    got = rrm.gated_scan_backward(dy, x, f, marks, lengths=lengths, dh_last=dh)
+    assert (out[..., 0] == 7).all() and (out[..., 1 + c] == 7).all()
+    half = V if dtype == "bf16" else U
+    # as in test_scan_of_many_frames
+    slack = 5 * (SUM + 2 * U * 64 + GATE) * 2
+    want = torch.where(live, hs[:, 1:], 0.0)
+    close(y, want, slack + half * (want.abs() + slack), "y")
+    close(last, hs[:, t], slack, "h_last")
+    close(marks, hs[:, 0:t:64], slack, "marks")
+    gs = slack * max(1.0, float(grads.abs().max()) / 5)
+    for have, want, s, what in ((got[0], o * grads, gs, "dx"), (got[1], grads * (hs[:, :-1] - x64) * a * o, gs * 10, "df"), (got[2], carry, gs, "dh0")):
+        close(have, want, s + half * (want.abs() + s), what)
+    assert not y[~live.expand_as(y)].any() and not got[0][~live.expand_as(y)].any() and not got[1][~live.expand_as(y)].any()
+    for _ in range(2):
+        marks2 = rrm.gated_scan_marks(x)
+        y2, last2 = rrm.gated_scan(x, f, h0, lengths=lengths, marks=marks2)
+        assert torch.equal(y2, y) and torch.equal(last2, last) and torch.equal(marks2, marks)
+        assert all(torch.equal(p, q) for p, q in zip(got, rrm.gated_scan_backward(dy, x, f, marks, lengths=lengths, dh_last=dh)))
