@@ -105,6 +105,35 @@ def test_a_call_on_another_stream_beside_one_that_uses_freed_memory(name):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@gpu
+def test_a_captured_call_on_another_stream():
+    """A stream that joins a capture, and its results back on the first one: replays give what eager calls do."""
+    x, f = (torch.randn(2, 700, 24, generator=gen(i)).cuda() for i in range(2))
+    side = torch.cuda.Stream()
+
+    def both():
+        here = torch.cuda.current_stream()
+        a = rrm.group_norm_act(x, 4, act="silu")
+        side.wait_stream(here)
+        y, last = rrm.gated_scan(a, f, stream=side)
+        here.wait_stream(side)
+        return rrm.group_norm_act(y, 4), last
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for k in range(4):
+        x.copy_(torch.randn(2, 700, 24, generator=gen(k + 5)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 # -- sizes at the ends of the range ----------------------------------------------------------------------------------------------
 
 def norm_parts64(x, groups, eps=1e-5):
