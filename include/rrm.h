@@ -291,7 +291,10 @@ rrm_status rrm_aux_probe_copy(void* dst, const void* src, size_t bytes, void* hi
  * elements of an output at one place).  Strides of tensors that a call does not take are not looked at.
  *
  * Sums, statistics, states and gates are held in 32 bits whatever the element type; a result is rounded once, to
- * nearest even.  No atomics: the same call gives the same bits.
+ * nearest even.  Every sum has one order, and nothing depends on which workgroup comes first: the same call gives the same bits.
+ * (A scan of few long videos is cut into blocks whose workgroups hand their states on through the workspace, with atomic counters, loads
+ * and stores.  A block waits only for such as run already; the wait is bounded all the same, at some seconds.  Were it to run out, frames of
+ * that block and of those behind it would be not-a-numbers where no input is one, with RRM_OK.)
  *
  * Errors of all of them: RRM_ERR_NULL, RRM_ERR_SHAPE (sizes, strides), RRM_ERR_DTYPE (element types), RRM_ERR_OPTION
  * (activation, eps), RRM_ERR_STATE (h_last given as h0), RRM_ERR_ALIGN, RRM_ERR_WORKSPACE (too small), RRM_ERR_HIP. */
@@ -368,12 +371,13 @@ typedef struct {
 
 size_t rrm_gated_ff_workspace(const rrm_ff_desc* desc, int backward);
 
-/* g, u: both or neither; for a backward pass they receive G and U, rounded to bfloat16 */
+/* g, u: both or neither; for a backward pass they receive G and U, rounded to bfloat16 (half the memory and traffic of 32 bits) */
 rrm_status rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, void* h, void* g, void* u,
                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*      dG = dH * U * act'(G)     dU = dH * act(G)     dX = dG Wg + dU Wu     dWg = dG^T X     dWu = dU^T X
- * dG and dU enter the products in bfloat16.  dx, or dwg and dwu together, may be NULL. */
+ * dG and dU enter the products in bfloat16, as the matrix cores take them.  A gradient is off by 0.0030 of its norm, of which rounding the result
+ * alone would leave 0.0017, G and U in 32 bits 0.0023, dG and dU in 32 bits 0.0025.  dx, or dwg and dwu together, may be NULL. */
 rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const void* g,
                                  const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* workspace,
                                  size_t workspace_bytes, void* hip_stream);

@@ -4,10 +4,14 @@
 //      dG = dH * U * act'(G)     dU = dH * act(G)     dX = dG Wg + dU Wu     dWg = dG^T X     dWu = dU^T X
 //
 // Both projections are one product: a wavefront's blocks of 32 columns belong to the one and the other in turn, so act(G) * U is made of two
-// registers of one lane, and G and U meet memory only where the backward pass is to have them.  Backward, dG and dU are made once (in bfloat16, as the
-// products take them; every element goes into k products of each of the two gradients), dX sums both products in one accumulator, and both dW are
-// tiles of one launch.  No operand is transposed in memory: what lies across the summed axis is turned on its way from LDS to the
-// registers.  All sums are held in 32 bits.
+// registers of one lane, and G and U meet memory only where the backward pass is to have them.  Backward, dG and dU are made once, dX sums both
+// products in one accumulator, and both dW are tiles of one launch.  No operand is transposed in memory: what lies across the summed axis is
+// turned on its way from LDS to the registers.  All sums are held in 32 bits.
+//
+// Two roundings to bfloat16 stand between them.  G and U are kept for the backward pass in it: 32 bits would be four more bytes a hidden value and row to
+// write, to hold and to read.  dG and dU are made in it, as the matrix cores take them; each goes into k products of each gradient, and two bfloat16 parts of each
+// would double those.  Relative error of a gradient (1024 x 512 -> 1024, silu): 0.0030; rounding the result alone leaves 0.0017, with G and U in 32 bits
+// 0.0023, with dG and dU 0.0025.
 #include "op_common.h"
 
 namespace rrm {
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void gradients_kernel(Product dx, P
 
 // Few rows (up to 16): the weights are the traffic, and each is read once, from memory straight into the fragments of the
 // matrix cores.  A workgroup makes 16 hidden features; its eight wavefronts take eight parts of the summed axis and meet in LDS.
-// One row, 4096 -> 4096: 14.1 us, 4.8 TB/s, all that a copy reaches.
+// One row, 4096 -> 4096: 14.1 us, 4.8 TB/s, with weights out of the 256 MB cache, 16.7 with weights out of memory.
 constexpr int FEW_WAVES = 8, FEW_F = 16, FEW_ROWS = 16;
 typedef float v4f __attribute__((ext_vector_type(4)));
 
@@ -729,8 +733,11 @@ GradientsPlan gradients_plan(const rrm_ff_desc& d, bool dx, bool dw) {
     return {px.shape, pw.shape, px.splits, pw.splits, false};
 }
 
-// Up to so many rows the weights go from memory into the fragments (few_rows_kernel): 4096 -> 4096, 1 / 16 / 32 / 64 rows
-// 14.6 / 16.9 / 18.5 / 26.7 us so, 19 by tiles; 4096 -> 9216 36 / 44 / 53 / 77 us and 40.
+// Up to so many rows the weights go from memory into the fragments (few_rows_kernel).  us so and by tiles, weights out of memory, 1 / 8 / 16 rows: 4096 ->
+// 4096 16.7 / 17.3 / 18.5 and 20.3 / 20.9 / 22.0; 4096 -> 9216 38.2 / 41.1 / 45.4 and 41.6 / 41.5 / 42.4; 1001 -> 2050 7.7 / 8.8 / 9.4 and
+// 17.2 / 17.3 / 17.7.  The rule is by rows alone, and loses where weights are wide and rows many (16 rows, 9216 features: 7%) or the weights, some 150 MB, stay in
+// the 256 MB cache (4096 -> 9216 31.2 / 34.3 / 37.7 and 23.9 / 24.0 / 24.4; 4096 -> 4096 14.1 / 15.2 / 16.1 and 17.6 / 17.7 / 18.0).  Beyond 16 rows each
+// set of 16 reads the weights again: 4096 -> 4096 32 rows 28 us and 19.
 bool few_rows(const rrm_ff_desc& d) { return d.m <= FEW_ROWS; }
 
 // The tile kernel copies whole, aligned 16-byte chunks: rows that are not made of them are copied to the workspace first, padded with zeros.

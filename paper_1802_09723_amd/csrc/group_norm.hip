@@ -22,8 +22,8 @@ constexpr int64_t HELD_FEW = 20000;
 // A workgroup has the `cb` channels of whole groups of one sample, all positions; a thread keeps up to P vectors of VEC neighbouring
 // channels (always the same channels) of positions R apart in registers.  So x (backward: and dy) is read once, the variance is summed about the
 // mean, and the result leaves without another look at memory.
-// Measured: 64 x 56 x 56 x 64, fp32 in and bf16 out, 20.8 us, 3.7 TB/s; 64 x 28 x 28 x 128 bf16, one round of workgroups, 12.3 us forward and
-// 14.3 backward: their start, the reads, the sums and the writes one after the other, nothing beside them.
+// Measured: 64 x 56 x 56 x 64, fp32 in and bf16 out, 21.0 us, 3.7 TB/s; 64 x 28 x 28 x 128 bf16, one round of workgroups, 12.4 us forward and
+// 14.2 backward: their start, the reads, the sums and the writes one after the other, nothing beside them.
 struct HeldGeom {
     int cb, blocks;  // channels of a workgroup; workgroups of a sample
     int lanes;       // threads of a position, a power of two
@@ -374,7 +374,8 @@ __global__ __launch_bounds__(SLICE_THREADS) void slice_stats_kernel(rrm_norm_des
     float mean[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) mean[i] = first_mean[lane * VEC + i], s[0][i] = 0.0f;
-    // (the slice again, out of the caches: some tens of kilobytes)
+    // (the slice again: out of the caches where it is some tens of kilobytes; there are some 1025 slices at the most, so those of a sample beyond the 256 MB of
+    // the last cache come from memory twice)
 #pragma unroll 4
     for (int p = t.p0 + t.row; p < t.p1; p += t.step) {
         load_vec<VEC>(xs + p * d.x_position, v);

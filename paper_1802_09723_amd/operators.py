@@ -10,7 +10,7 @@ records (under ``torch.no_grad()``, and inside an ``autograd.Function``, it is n
 
 What the checks of a call look at (shapes, strides, types) decides its descriptor and workspace too, so both are kept by it: a call with the
 shapes of an earlier one takes them from a table and goes on to the pointers.  (One frame of a live video, host time of a call:
-12 us with every check and structure made anew, 7 so.)
+12 us with every check and structure made anew, 8 to 9 so.)
 """
 from __future__ import annotations
 
