@@ -382,6 +382,86 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
                                  const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* workspace,
                                  size_t workspace_bytes, void* hip_stream);
 
+/* Linear attention over the t frames of n videos, h heads with keys of dk and values of dv features, each head with a decay of its own:
+ *      lambda = exp(log_decay_head)        S_t = lambda S_{t-1} + k_t^T v_t        o_t = scale * q_t S_t        S [dk][dv]
+ * A video of lengths[i] < t frames ends there: what q, k, v and do hold behind is not looked at (not-a-numbers included), o, dq, dk and dv
+ * are 0 there, and s_last is the state after its last frame (s0 for a video of no frames).  One frame of live videos is t = 1, with s0 the state
+ * before and s_last the state after it; there s_last may be s0.  Inputs of several heads may be one (a head's stride of 0); their gradients come head
+ * by head.  log_decay is at most 0 in a memory that fades (minus infinity: nothing of the frames before); its decays are not learned, there is no gradient.
+ *
+ * A bfloat16 call multiplies on the matrix cores in bfloat16: the scores with their decays, and the state where a query reads it, are rounded to
+ * it; the state itself, and what it takes up of each frame, are held in 32 bits. */
+typedef struct {
+    int n, t, h, dk, dv; /* n, t and h may be 0; t at most 2^31 - 256, n * h 2^28, dk and dv 1 to 256 */
+    int elem;            /* rrm_elem of q, k, v, o and their gradients */
+    float scale;
+    int64_t q_video, q_frame, q_head, k_video, k_frame, k_head, v_video, v_frame, v_head; /* strides */
+    int64_t o_video, o_frame, o_head;                                                     /* do lies by those of o */
+    int64_t dq_video, dq_frame, dq_head, dk_video, dk_frame, dk_head, dv_video, dv_frame, dv_head;
+} rrm_decay_desc;
+
+size_t rrm_decay_attention_workspace(const rrm_decay_desc* desc, int backward);
+
+/* log_decay  float32 [h]                        lengths  int32 [n], NULL = t each (held to [0, t])
+ * s0         float32 [n][h][dk][dv], NULL = 0   s_last   the same or NULL */
+rrm_status rrm_decay_attention(const rrm_decay_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
+                               const float* s0, const int32_t* lengths, void* o, float* s_last, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+
+/* With D_t = lambda D_{t+1} + scale * q_t^T do_t, from D = ds_last + scale * q^T do at a video's last frame:
+ *      dq_t = scale * S_t do_t        dk_t = D_t v_t        dv_t = k_t D_t        ds0 = lambda D_1 (no frames: ds_last)
+ * S is made again from s0, k and v.  ds_last and s0 may be NULL (= 0); dq, dk, dv and ds0 may each be NULL. */
+rrm_status rrm_decay_attention_backward(const rrm_decay_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
+                                        const float* s0, const int32_t* lengths, const void* d_o, const float* ds_last, void* dq,
+                                        void* dk, void* dv, float* ds0, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* What stands between two blocks of a residual network, on m rows of c features: the norm behind the one, its gate, the residual scale and sum,
+ * and the norm before the next,
+ *      p = b * rb * post, rb = 1 / sqrt(mean(b^2) + eps)  (post_norm = 0: p = b)
+ *      r = x + scale * sigmoid(gate) * p
+ *      u = r * rr * pre, rr = 1 / sqrt(mean(r^2) + eps)
+ * in one pass over x, b and the gate.  Without b (NULL; no gate, scale or post_norm) r is x and not written: the norm before the first block. */
+typedef struct {
+    int m, c;           /* m may be 0; c 1 to 16384 */
+    int x_elem, b_elem; /* rrm_elem of x, r and their gradients; of b, gate, u and theirs */
+    int post_norm;
+    float eps;          /* > 0 */
+    int64_t x_row, b_row, gate_row, r_row, u_row, dx_row, db_row, dgate_row; /* strides; dr lies by r_row, du by u_row */
+} rrm_residual_desc;
+
+/* gate, b-typed [m][c], NULL = no gate (factor 1)         scale, post, pre  float32 [c], NULL = 1
+ * r, u     either may be NULL; r may be x                   stats  float32 [m][2] or NULL: receives rb and rr for the backward pass */
+rrm_status rrm_residual_norm(const rrm_residual_desc* desc, const void* x, const void* b, const void* gate, const float* scale,
+                             const float* post, const float* pre, void* r, void* u, float* stats, void* hip_stream);
+
+size_t rrm_residual_norm_workspace(const rrm_residual_desc* desc); /* of the backward pass */
+
+/* With rh = r * rr, bh = b * rb, sg = sigmoid(gate), w = du * pre and means over a row:
+ *      dx = dr + rr * (w - rh * mean(w rh))     dpre = sum du rh        dgate = dx * scale * p * sg (1 - sg)     dscale = sum dx sg p
+ *      dp = dx * scale * sg                     dpost = sum dp bh       db = rb * (dp post - bh * mean(dp post bh))   (post_norm = 0: dp)
+ * x and b as the forward pass took them (r is made again, in 32 bits).  dr or du may be NULL (= 0); every result may be NULL. */
+rrm_status rrm_residual_norm_backward(const rrm_residual_desc* desc, const void* dr, const void* du, const void* x, const void* b,
+                                      const float* stats, const void* gate, const float* scale, const float* post, const float* pre,
+                                      void* dx, void* db, void* dgate, float* dscale, float* dpost, float* dpre, void* workspace,
+                                      size_t workspace_bytes, void* hip_stream);
+
+/* A weight's update made orthogonal by Newton-Schulz products: n matrices G [rows][cols], each by itself,
+ *      X = G / (|G| + eps)  (|G|: root of the sum of squares)        `steps` times:  A = X X^T,  X = a X + (b A + c A^2) X
+ * (with A = X^T X, X = a X + X (b A + c A^2) where rows > cols, which is the same).  The result is bfloat16.  Between the products X, A and
+ * b A + c A^2 are held in half precision, X at 256 times its size, so that singular values down to some 1e-6 of the norm count: polynomials
+ * that leave singular values below 200 are meant.  Not-a-numbers and infinities of a matrix are its own. */
+typedef struct {
+    int n, rows, cols; /* n 0 to 65535; rows and cols 1 to 65536, tensors of up to 2^40 elements */
+    int elem;          /* rrm_elem of G */
+    int steps;         /* 1 to 100 */
+    float a, b, c;     /* the polynomial */
+    float eps;         /* >= 0 */
+    int64_t g_matrix, g_row, x_matrix, x_row; /* strides */
+} rrm_orth_desc;
+
+size_t rrm_orthogonalize_workspace(const rrm_orth_desc* desc);
+rrm_status rrm_orthogonalize(const rrm_orth_desc* desc, const void* g, void* x, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Which form of its kernels a call with this descriptor takes (host only; for tests and measurements).
  * norm: layout[0] the size of workgroup, 0 to 3, that holds a sample in registers, -1: slices; [1] channels of a workgroup (slices: their number)
  * scan: layout[0] 0: a thread a feature, 1: a workgroup a chain of blocks, 2: many; [1] frames of a block (0: none)

@@ -10,8 +10,8 @@ from .binding import (  # noqa: F401
 )
 
 # (operators imports torch, which takes a second or more: not before one of its names is asked for)
-_OPERATORS = ("gated_ff", "gated_ff_backward", "gated_scan", "gated_scan_backward", "gated_scan_marks", "group_norm_act",
-              "group_norm_act_backward", "group_norm_act_of")
+_OPERATORS = ("decay_attention", "decay_attention_backward", "gated_ff", "gated_ff_backward", "gated_scan", "gated_scan_backward", "gated_scan_marks", "group_norm_act",
+              "group_norm_act_backward", "group_norm_act_of", "orthogonalize", "residual_norm", "residual_norm_backward")
 
 
 def __getattr__(name):

@@ -106,10 +106,19 @@ def lib():
         L.rrm_gated_scan_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, S, P]
         L.rrm_gated_ff.argtypes = [B, P, P, P, P, P, P, P, S, P]
         L.rrm_gated_ff_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_decay_attention_workspace.argtypes = [B, I]
+        L.rrm_residual_norm_workspace.argtypes = L.rrm_orthogonalize_workspace.argtypes = [B]
+        L.rrm_decay_attention_workspace.restype = L.rrm_residual_norm_workspace.restype = L.rrm_orthogonalize_workspace.restype = S
+        L.rrm_decay_attention.argtypes = [B, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_decay_attention_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_residual_norm.argtypes = [B, P, P, P, P, P, P, P, P, P, P]
+        L.rrm_residual_norm_backward.argtypes = [B, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, S, P]
+        L.rrm_orthogonalize.argtypes = [B, P, P, P, S, P]
         L.rrm_scan_marks.argtypes = [I]
         L.rrm_aux_norm_layout.argtypes = L.rrm_aux_scan_layout.argtypes = L.rrm_aux_ff_layout.argtypes = [B, I, P]
         for f in ("rrm_aux_norm_layout", "rrm_aux_scan_layout", "rrm_aux_ff_layout", "rrm_group_norm_act", "rrm_group_norm_act_backward", "rrm_gated_scan", "rrm_gated_scan_backward", "rrm_gated_ff",
-                  "rrm_gated_ff_backward", "rrm_scan_marks"):
+                  "rrm_gated_ff_backward", "rrm_scan_marks", "rrm_decay_attention", "rrm_decay_attention_backward", "rrm_residual_norm", "rrm_residual_norm_backward",
+                  "rrm_orthogonalize"):
             getattr(L, f).restype = I
         _lib = L
     return _lib

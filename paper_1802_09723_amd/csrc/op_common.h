@@ -243,5 +243,19 @@ hipError_t launch_gated_ff(const rrm_ff_desc& d, const void* x, const void* wg, 
                            hipStream_t s);
 hipError_t launch_gated_ff_backward(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, const void* g,
                                     const void* u, const void* dh, void* dx, void* dwg, void* dwu, void* ws, hipStream_t s);
+size_t decay_scratch(const rrm_decay_desc& d, bool backward);
+hipError_t launch_decay_attention(const rrm_decay_desc& d, const void* q, const void* k, const void* v, const float* log_decay, const float* s0,
+                                  const int32_t* lengths, void* o, float* s_last, void* ws, hipStream_t s);
+hipError_t launch_decay_attention_backward(const rrm_decay_desc& d, const void* q, const void* k, const void* v, const float* log_decay,
+                                           const float* s0, const int32_t* lengths, const void* d_o, const float* ds_last, void* dq,
+                                           void* dk, void* dv, float* ds0, void* ws, hipStream_t s);
+size_t residual_scratch(const rrm_residual_desc& d);
+hipError_t launch_residual_norm(const rrm_residual_desc& d, const void* x, const void* b, const void* gate, const float* scale, const float* post,
+                                const float* pre, void* r, void* u, float* stats, hipStream_t s);
+hipError_t launch_residual_norm_backward(const rrm_residual_desc& d, const void* dr, const void* du, const void* x, const void* b,
+                                         const float* stats, const void* gate, const float* scale, const float* post, const float* pre,
+                                         void* dx, void* db, void* dgate, float* dscale, float* dpost, float* dpre, void* ws, hipStream_t s);
+size_t orth_scratch(const rrm_orth_desc& d);
+hipError_t launch_orthogonalize(const rrm_orth_desc& d, const void* g, void* x, void* ws, hipStream_t s);
 
 }  // namespace rrm

@@ -44,19 +44,40 @@ class FFDesc(ctypes.Structure):
                 + [("unaligned", ctypes.c_int)])
 
 
+class DecayDesc(ctypes.Structure):
+    """``rrm_decay_desc``"""
+    _fields_ = ([(k, ctypes.c_int) for k in ("n", "t", "h", "dk", "dv", "elem")] + [("scale", ctypes.c_float)]
+                + [(f"{x}_{axis}", ctypes.c_int64) for x in ("q", "k", "v", "o", "dq", "dk", "dv") for axis in ("video", "frame", "head")])
+
+
+class ResidualDesc(ctypes.Structure):
+    """``rrm_residual_desc``"""
+    _fields_ = ([(k, ctypes.c_int) for k in ("m", "c", "x_elem", "b_elem", "post_norm")] + [("eps", ctypes.c_float)]
+                + [(f"{x}_row", ctypes.c_int64) for x in ("x", "b", "gate", "r", "u", "dx", "db", "dgate")])
+
+
+class OrthDesc(ctypes.Structure):
+    """``rrm_orth_desc``"""
+    _fields_ = ([(k, ctypes.c_int) for k in ("n", "rows", "cols", "elem", "steps")] + [(k, ctypes.c_float) for k in ("a", "b", "c", "eps")]
+                + [(k, ctypes.c_int64) for k in ("g_matrix", "g_row", "x_matrix", "x_row")])
+
+
 # (descriptor, reference to it, bytes of workspace, device) by what the checks looked at.  Emptied when it has grown past what a program's
 # shapes come to.
 _plans: dict = {}
 
 
-def _keep(key, desc, size_of: str, backward: int, *tensors):
+def _keep(key, desc, size_of, backward, *tensors):
+    """``size_of``: the C function that says how large the workspace is, None where there is none; ``backward``: its second argument, None
+    where it takes one."""
     devices = {t.device.index for t in tensors if t is not None}
     if len(devices) > 1:
         raise ValueError(f"tensors on several devices: {sorted(devices)}")
     if len(_plans) > 4096:
         _plans.clear()
     ref = ctypes.byref(desc)
-    _plans[key] = plan = (desc, ref, getattr(lib(), size_of)(ref, backward), devices.pop())
+    args = (ref,) if backward is None else (ref, backward)
+    _plans[key] = plan = (desc, ref, getattr(lib(), size_of)(*args) if size_of else 0, devices.pop())
     return plan
 
 
@@ -155,7 +176,7 @@ def _elsewhere(stream, call, *args):
     with torch.cuda.stream(stream):
         got = call(*args)
     for t in got if isinstance(got, tuple) else (got,):
-        if all(t is not a for a in args):
+        if t is not None and all(t is not a for a in args):
             t.record_stream(before)
     return got
 
@@ -398,3 +419,230 @@ def gated_ff_backward(dh, x, wg, wu, g, u, act: str = "silu", dx=None, dwg=None,
     _check(lib().rrm_gated_ff_backward(plan[1], px, pg, pu, g.data_ptr(), u.data_ptr(), dh.data_ptr(), dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(),
                                        _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return dx, dwg, dwu
+
+
+# -- linear attention with a decay for each head -----------------------------------------------------------------------
+
+def _heads(t, what: str):
+    """Strides of videos, frames and heads."""
+    _adjacent(t, what)
+    return t.stride(0), t.stride(1), t.stride(2)
+
+
+def decay_attention(q, k, v, log_decay, scale=None, s0=None, lengths=None, out=None, s_last=None, stream=None):
+    """``rrm_decay_attention``: (o, s_last) of linear attention over the frames, ``q`` and ``k`` [n, t, h, dk], ``v`` [n, t, h, dv] float32 or
+    bfloat16 (dk and dv up to 256), with the decay exp(``log_decay``) a frame of each head (float32 [h]), from the state ``s0`` (float32 [n, h, dk, dv]; None:
+    zeros).  ``scale``: of the scores, None: dk ** -0.5.  ``lengths`` int32 [n]: frames of each video.  For one frame (t = 1) ``s_last`` may be
+    ``s0``.  Heads that share queries, keys or values take them expanded (a stride of 0)."""
+    if stream is not None:
+        return _elsewhere(stream, decay_attention, q, k, v, log_decay, scale, s0, lengths, out, s_last)
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v: expected [n, t, h, features]")
+    n, t, h, dk = q.shape
+    dv = v.shape[-1]
+    made = (out is None, s_last is None)
+    if out is None:
+        out = v.new_empty((n, t, h, dv))
+    if s_last is None:
+        s_last = q.new_empty((n, h, dk, dv), dtype=torch.float32)
+    key = ("decay", scale, _look(q), _look(k), _look(v), _look(log_decay), _look(s0), _look(lengths), made[0] or _look(out), made[1] or _look(s_last))
+    plan = _plans.get(key)
+    if plan is None:
+        _expect(q, "q", (n, t, h, dk))
+        _expect(k, "k", (n, t, h, dk), q.dtype)
+        _expect(v, "v", (n, t, h, dv), q.dtype)
+        _expect(out, "out", (n, t, h, dv), q.dtype)
+        _dense(log_decay, "log_decay", (h,), torch.float32)
+        _dense(s0, "s0", (n, h, dk, dv), torch.float32)
+        _dense(s_last, "s_last", (n, h, dk, dv), torch.float32)
+        _dense(lengths, "lengths", (n,), torch.int32)
+        plan = _keep(key, DecayDesc(n, t, h, dk, dv, _elem(q), dk ** -0.5 if scale is None else float(scale), *_heads(q, "q"), *_heads(k, "k"),
+                                    *_heads(v, "v"), *_heads(out, "out"), *[0] * 9), "rrm_decay_attention_workspace", 0, q, k, v, log_decay, s0, lengths,
+                     out, s_last)
+    ws = _workspace(plan[2], q.device)
+    _check(lib().rrm_decay_attention(plan[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(s0), _ptr(lengths), out.data_ptr(),
+                                     s_last.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
+    return out, s_last
+
+
+def decay_attention_backward(do, q, k, v, log_decay, scale=None, s0=None, lengths=None, ds_last=None, dq=None, dk=None, dv=None, ds0=None, stream=None):
+    """``rrm_decay_attention_backward``: (dq, dk, dv, ds0) from ``do``, the forward pass's inputs and the gradient ``ds_last`` (float32
+    [n, h, dk, dv]; None: zeros) of the last state.  Gradients of expanded inputs come head by head, for the caller to sum."""
+    if stream is not None:
+        return _elsewhere(stream, decay_attention_backward, do, q, k, v, log_decay, scale, s0, lengths, ds_last, dq, dk, dv, ds0)
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v: expected [n, t, h, features]")
+    n, t, h, fk = q.shape
+    fv = v.shape[-1]
+    made = [g is None for g in (dq, dk, dv, ds0)]
+    if dq is None:
+        dq = q.new_empty((n, t, h, fk))
+    if dk is None:
+        dk = q.new_empty((n, t, h, fk))
+    if dv is None:
+        dv = v.new_empty((n, t, h, fv))
+    if ds0 is None:
+        ds0 = q.new_empty((n, h, fk, fv), dtype=torch.float32)
+    key = ("decay back", scale, _look(do), _look(q), _look(k), _look(v), _look(log_decay), _look(s0), _look(lengths), _look(ds_last),
+           made[0] or _look(dq), made[1] or _look(dk), made[2] or _look(dv), made[3] or _look(ds0))
+    plan = _plans.get(key)
+    if plan is None:
+        for x, what, f in ((q, "q", fk), (k, "k", fk), (v, "v", fv), (do, "do", fv), (dq, "dq", fk), (dk, "dk", fk), (dv, "dv", fv)):
+            _expect(x, what, (n, t, h, f), q.dtype)
+        _dense(log_decay, "log_decay", (h,), torch.float32)
+        for x, what in ((s0, "s0"), (ds_last, "ds_last"), (ds0, "ds0")):
+            _dense(x, what, (n, h, fk, fv), torch.float32)
+        _dense(lengths, "lengths", (n,), torch.int32)
+        plan = _keep(key, DecayDesc(n, t, h, fk, fv, _elem(q), fk ** -0.5 if scale is None else float(scale), *_heads(q, "q"), *_heads(k, "k"),
+                                    *_heads(v, "v"), *_heads(do, "do"), *_heads(dq, "dq"), *_heads(dk, "dk"), *_heads(dv, "dv")),
+                     "rrm_decay_attention_workspace", 1, do, q, k, v, log_decay, s0, lengths, ds_last, dq, dk, dv, ds0)
+    ws = _workspace(plan[2], q.device)
+    _check(lib().rrm_decay_attention_backward(plan[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _ptr(s0), _ptr(lengths),
+                                              do.data_ptr(), _ptr(ds_last), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ds0.data_ptr(), _ptr(ws), plan[2],
+                                              _stream_ptr(None, plan[3])))
+    return dq, dk, dv, ds0
+
+
+# -- norms behind and before a block, its gate and residual scale --------------------------------------------------------
+
+def _rows(t, what: str):
+    """Rows of the last axis and their stride: the axes before it have to collapse to one."""
+    _adjacent(t, what)
+    if t.dim() < 2:
+        raise ValueError(f"{what}: expected [.., c]")
+    rows, step = 1, 0
+    for size, stride in zip(t.shape[-2::-1], t.stride()[-2::-1]):
+        if size == 1:
+            continue
+        if rows == 1:
+            step = stride
+        elif stride != step * rows:
+            raise ValueError(f"{what}: the axes before the last must collapse to one")
+        rows *= size
+    return step if rows > 1 else t.shape[-1]
+
+
+def residual_norm(x, b=None, gate=None, scale=None, post=None, pre=None, eps: float = 1e-6, out=None, u=None, u_dtype=None, stats=None, stream=None):
+    """``rrm_residual_norm``: (r, u) with r = ``x`` + ``scale`` * sigmoid(``gate``) * norm(``b``) * ``post`` and u = norm(r) * ``pre``, norms over
+    the last axis without a mean.  ``x`` [.., c] float32 or bfloat16, the residual stream; ``b``, a block's output, and ``gate`` of its shape, of one of these types; ``scale``,
+    ``post`` and ``pre`` float32 [c].  None for ``gate`` or ``scale``: a factor of 1; for ``post``: no norm behind the block; for ``pre``: no u, and
+    None in its place; for ``b``: r is x itself (the norm before the first block).  u has b's type, or ``u_dtype``.  ``out`` may be ``x``.
+    ``stats``, float32 [.., 2], receives what the backward pass needs."""
+    if stream is not None:
+        return _elsewhere(stream, residual_norm, x, b, gate, scale, post, pre, eps, out, u, u_dtype, stats)
+    made = (b is not None and out is None, pre is not None and u is None)
+    if made[0]:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if made[1]:
+        u = torch.empty_like(x, dtype=u_dtype or (x.dtype if b is None else b.dtype), memory_format=torch.contiguous_format)
+    key = ("residual", eps, u_dtype, _look(x), _look(b), _look(gate), _look(scale), _look(post), _look(pre), made[0] or _look(out), made[1] or _look(u), _look(stats))
+    plan = _plans.get(key)
+    if plan is None:
+        c = x.shape[-1] if x.dim() else 0
+        if b is None and not (gate is None and scale is None and post is None and out is None):
+            raise ValueError("gate, scale, post, out: without b there is nothing for them")
+        if pre is None and u is not None:
+            raise ValueError("u: there is none without pre")
+        if b is None and pre is None:
+            raise ValueError("b, pre: expected one of them")
+        kind = (u if b is None else b).dtype
+        _expect(x, "x", x.shape)
+        _expect(b, "b", x.shape)
+        _expect(gate, "gate", x.shape, kind)
+        _expect(out, "out", x.shape, x.dtype)
+        _expect(u, "u", x.shape, u_dtype or kind)
+        if u is not None and u.dtype is not kind:
+            raise ValueError(f"u: expected {kind}, as b, got {u.dtype}")
+        for w, what in ((scale, "scale"), (post, "post"), (pre, "pre")):
+            _dense(w, what, (c,), torch.float32)
+        _dense(stats, "stats", (*x.shape[:-1], 2), torch.float32)
+        row = [0 if t is None else _rows(t, what) for t, what in ((x, "x"), (b, "b"), (gate, "gate"), (out, "out"), (u, "u"))]
+        plan = _keep(key, ResidualDesc(x.numel() // c if c else 0, c, _elem(x), _elem(u if b is None else b), post is not None, float(eps), *row, 0, 0, 0), None, None,
+                     x, b, gate, scale, post, pre, out, u, stats)
+    _check(lib().rrm_residual_norm(plan[1], x.data_ptr(), _ptr(b), _ptr(gate), _ptr(scale), _ptr(post), _ptr(pre), _ptr(out), _ptr(u), _ptr(stats),
+                                   _stream_ptr(None, plan[3])))
+    return x if b is None else out, u
+
+
+def residual_norm_backward(dr, du, x, b, stats, gate=None, scale=None, post=None, pre=None, dx=None, db=None, dgate=None, dscale=None, dpost=None, dpre=None,
+                           stream=None):
+    """``rrm_residual_norm_backward``: (dx, db, dgate, dscale, dpost, dpre) from ``dr`` (of x's type) and ``du`` (of u's; either may be None), the
+    forward pass's inputs and the ``stats`` that it left; None in the place of what the forward pass had not."""
+    if stream is not None:
+        return _elsewhere(stream, residual_norm_backward, dr, du, x, b, stats, gate, scale, post, pre, dx, db, dgate, dscale, dpost, dpre)
+    has = (True, b is not None, gate is not None, scale is not None, post is not None, pre is not None)
+    given = (dx, db, dgate, dscale, dpost, dpre)
+    got = []
+    for want, g, like in zip(has, given, (x, b, gate, scale, post, pre)):
+        got.append(torch.empty_like(like, memory_format=torch.contiguous_format) if want and g is None else g)
+    dx, db, dgate, dscale, dpost, dpre = got
+    key = ("residual back", _look(dr), _look(du), _look(x), _look(b), _look(stats), _look(gate), _look(scale), _look(post), _look(pre),
+           *[g is None and want or _look(g) for g, want in zip(given, has)])
+    plan = _plans.get(key)
+    if plan is None:
+        c = x.shape[-1] if x.dim() else 0
+        if b is None and not (gate is None and scale is None and post is None):
+            raise ValueError("gate, scale, post: without b there is nothing for them")
+        if du is not None and pre is None:
+            raise ValueError("du: there is no u without pre")
+        for want, g, what in zip(has, given, ("dx", "db", "dgate", "dscale", "dpost", "dpre")):
+            if g is not None and not want:
+                raise ValueError(f"{what}: the forward pass had no such input")
+        kind = b.dtype if b is not None else du.dtype if du is not None else x.dtype
+        for t, what, dtype in ((x, "x", None), (dr, "dr", x.dtype), (dx, "dx", x.dtype), (b, "b", kind), (gate, "gate", kind), (du, "du", kind), (db, "db", kind),
+                               (dgate, "dgate", kind)):
+            _expect(t, what, x.shape, dtype)
+        for w, what in ((scale, "scale"), (post, "post"), (pre, "pre"), (dscale, "dscale"), (dpost, "dpost"), (dpre, "dpre")):
+            _dense(w, what, (c,), torch.float32)
+        _dense(stats, "stats", (*x.shape[:-1], 2), torch.float32)
+        row = [0 if t is None else _rows(t, what) for t, what in ((x, "x"), (b, "b"), (gate, "gate"), (dr, "dr"), (du, "du"), (dx, "dx"), (db, "db"), (dgate, "dgate"))]
+        elem = 1 if kind is torch.bfloat16 else _elem(x if b is None and du is None else b if b is not None else du)
+        plan = _keep(key, ResidualDesc(x.numel() // c if c else 0, c, _elem(x), elem, post is not None, 1.0, *row), "rrm_residual_norm_workspace", None,
+                     dr, du, x, b, stats, gate, scale, post, pre, *got)
+    ws = _workspace(plan[2], x.device)
+    _check(lib().rrm_residual_norm_backward(plan[1], _ptr(dr), _ptr(du), x.data_ptr(), _ptr(b), stats.data_ptr(), _ptr(gate), _ptr(scale), _ptr(post), _ptr(pre),
+                                            *[_ptr(g) for g in got], _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
+    return dx, db, dgate, dscale, dpost, dpre
+
+
+# -- a weight's update made orthogonal ------------------------------------------------------------------------------------
+
+def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None, stream=None):
+    """``rrm_orthogonalize``: of each matrix of ``g`` [.., rows, cols], float32 or bfloat16, the Newton-Schulz iteration
+    X <- a X + (b A + c A^2) X, A = X X^T, from g / (|g| + ``eps``), with ``coefficients`` (a, b, c); bfloat16, in ``out`` or a new tensor.  The default coefficients raise
+    small singular values fast and leave all of them between some 0.7 and 1.2; (1.875, -1.25, 0.375) converges to 1."""
+    if stream is not None:
+        return _elsewhere(stream, orthogonalize, g, steps, coefficients, eps, out)
+    made = out is None
+    if made:
+        out = torch.empty_like(g, dtype=torch.bfloat16, memory_format=torch.contiguous_format)
+    key = ("orth", steps, coefficients, eps, _look(g), made or _look(out))
+    plan = _plans.get(key)
+    if plan is None:
+        if g.dim() < 2:
+            raise ValueError("g: expected [.., rows, cols]")
+        a, b, c = coefficients
+        _expect(g, "g", g.shape)
+        _expect(out, "out", g.shape, torch.bfloat16)
+        rows, cols = g.shape[-2:]
+        if not g.numel() and (rows == 0 or cols == 0):
+            raise ValueError("g: matrices without elements")
+        n = g.numel() // (rows * cols)
+        places = []
+        for t, what in ((g, "g"), (out, "out")):
+            _adjacent(t, what)
+            lead = 1
+            step = 0
+            for size, stride in zip(t.shape[-3::-1], t.stride()[-3::-1]):
+                if size == 1:
+                    continue
+                if lead == 1:
+                    step = stride
+                elif stride != step * lead:
+                    raise ValueError(f"{what}: the axes before the last two must collapse to one")
+                lead *= size
+            places += [step, t.stride(-2) if rows > 1 else cols]
+        plan = _keep(key, OrthDesc(n, rows, cols, _elem(g), int(steps), float(a), float(b), float(c), float(eps), *places), "rrm_orthogonalize_workspace", None, g, out)
+    ws = _workspace(plan[2], g.device)
+    _check(lib().rrm_orthogonalize(plan[1], g.data_ptr(), out.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
+    return out

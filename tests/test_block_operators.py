@@ -1,0 +1,651 @@
+"""Linear attention with decays, the norms around a block and orthogonal updates against plain implementations in 64 bits, at sizes, strides, masks and
+types where they can go wrong; their gradients against the formulas (autograd in 64 bits) and against differences; their refusals.
+
+Tolerances, with u = 2^-24 (float32), v = 2^-8 (bfloat16) and w = 2^-11 (half precision) as what one rounding is off by, relative to the value:
+  a result rounded to its type is off by a rounding of itself, and by what it was off before.
+
+  Attention.  A state takes up a frame with at most four roundings of what it holds (the decay, its product, the frame's product, their sum): an error
+  state E_t = lambda E_{t-1} + 4 u A_t beside A_t = lambda A_{t-1} + |k_t|^T |v_t|, the state of the magnitudes, bounds what S_t is off by; scores that are
+  summed first and then applied, in any grouping of the frames, have no more roundings.  A result scale q_t S_t is off by scale |q_t| (E_t + 64 u A_t), the
+  second for the two sums over features and frames; in bfloat16 each term is rounded once more on its way (with its score, or with the
+  state that the query reads): v scale |q_t| A_t.
+
+  Norms: see residual_slack.  Orthogonal updates: see newton_schulz.
+"""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_1802_09723_amd as rrm
+from paper_1802_09723_amd import operators as ops
+from paper_1802_09723_amd.binding import RRMError
+
+gpu = pytest.mark.gpu
+
+U, V, W = 2.0 ** -24, 2.0 ** -8, 2.0 ** -11
+SUM = 32 * U
+GATE = 16 * U
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+F64 = torch.float64
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def check(got, want, slack, what):
+    """|got - want| <= slack (a number or a tensor), plus the rounding of got's type; same shape, finite where want is."""
+    got_d, want = got.detach().cpu().double(), want.detach().cpu()
+    slack = slack.detach().cpu() if torch.is_tensor(slack) else slack
+    assert got_d.shape == want.shape, f"{what}: shape {tuple(got_d.shape)} != {tuple(want.shape)}"
+    half = V if got.dtype == torch.bfloat16 else U
+    lim = slack + half * (want.abs() + slack) + 1e-38
+    err = (got_d - want).abs()
+    bad = ~(err <= lim)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {err[bad].max()} where {(lim + 0 * err)[bad].max()} is allowed"
+
+
+# -- linear attention with a decay for each head -----------------------------------------------------------------------
+
+def decays(h):
+    return torch.log1p(-torch.exp2(-torch.linspace(2.0, 8.0, h, dtype=F64))).float() if h > 1 else torch.tensor([-0.03])
+
+
+def attend64(q, k, v, log_decay, scale, s0, lengths):
+    """(o, s_last) by the recurrence, differentiable"""
+    n, t, h, dk = q.shape
+    lam = torch.exp(log_decay.double()).view(1, h, 1, 1)
+    s, rows = s0, []
+    for j in range(t):
+        live = (torch.tensor([j < e for e in lengths], device=q.device)).view(n, 1, 1, 1)
+        kj, vj, qj = (torch.where(live[..., 0], a[:, j], torch.zeros((), dtype=F64, device=q.device)) for a in (k, v, q))
+        s = torch.where(live, lam * s + kj[..., :, None] * vj[..., None, :], s)
+        rows.append(scale * (qj[..., None] * s).sum(-2))
+    return (torch.stack(rows, 1) if rows else torch.zeros(n, t, h, v.shape[-1], dtype=F64, device=q.device)), s
+
+
+def attend_slack(q, k, v, log_decay, scale, s0, lengths, back, kind):
+    """What (o, s_last) may be off by: see above.  `back`: last frame first, the state decays behind a frame."""
+    n, t, h, _ = q.shape
+    lam = torch.exp(log_decay.double()).view(h, 1, 1)
+    so, ss = torch.zeros(n, t, h, v.shape[-1], dtype=F64, device=q.device), torch.zeros_like(s0)
+    q, k, v = q.abs(), k.abs(), v.abs()
+    for i in range(n):
+        a, e = s0[i].abs(), torch.zeros_like(s0[i])
+        frames = range(lengths[i])
+        for j in (reversed(frames) if back else frames):
+            if not back:
+                a, e = lam * a, lam * e
+            a = a + k[i, j][..., :, None] * v[i, j][..., None, :]
+            e = e + 4 * U * a
+            so[i, j] = scale * (q[i, j][..., None] * (e + (64 * U + (V if kind == "bf16" else 0)) * a)).sum(-2)
+            if back:
+                a, e = lam * a, lam * e
+        ss[i] = e
+    return so, ss
+
+
+def attention_case(n, t, h, dk, dv, kind, ragged, seed, device="cpu"):
+    g = gen(seed)
+    lengths = None
+    if ragged:
+        lengths = torch.randint(0, t + 1, (n,), generator=g, dtype=torch.int32)
+        lengths[0] = t
+        if n > 1:
+            lengths[-1] = 0
+        if n > 2:
+            lengths[1] = 1
+    data = {}
+    for name, d in (("q", dk), ("k", dk), ("v", dv), ("do", dv)):
+        a = torch.randn(n, t, h, d, generator=g).to(DT[kind])
+        data[name] = a
+    data["s0"], data["ds_last"] = 3 * torch.randn(n, h, dk, dv, generator=g), torch.randn(n, h, dk, dv, generator=g)
+    return data, lengths
+
+
+def run_attention(data, lengths, log_decay, scale, kind, what=""):
+    """The forward and backward pass on the GPU against the recurrence in 64 bits"""
+    n, t, h, dk = data["q"].shape
+    ends = [t] * n if lengths is None else lengths.tolist()
+    d64 = {k: a.double() for k, a in data.items()}
+    leaves = [d64[k].clone().requires_grad_() for k in ("q", "k", "v", "s0")]
+    o, s_last = attend64(leaves[0], leaves[1], leaves[2], log_decay, scale, leaves[3], ends)
+    want = torch.autograd.grad((o, s_last), leaves, (d64["do"], d64["ds_last"]), allow_unused=True)
+    want = [torch.zeros_like(a) if g is None else g for a, g in zip(leaves, want)]
+    dev = {k: a.cuda() for k, a in data.items()}
+    ld, le = log_decay.cuda(), None if lengths is None else lengths.cuda()
+    if lengths is not None:  # not-a-numbers behind the ends
+        gone = torch.arange(t).view(1, t, 1, 1) >= lengths.view(n, 1, 1, 1)
+        for k in ("q", "k", "v", "do"):
+            dev[k].masked_fill_(gone.cuda(), math.nan)
+    got_o, got_s = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld, scale, s0=dev["s0"], lengths=le)
+    so, ss = attend_slack(d64["q"], d64["k"], d64["v"], log_decay, scale, d64["s0"], ends, False, kind)
+    check(got_o, o, so, what + "o")
+    check(got_s, s_last, ss, what + "s_last")
+    dq, dk_, dv_, ds0 = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld, scale, s0=dev["s0"], lengths=le, ds_last=dev["ds_last"])
+    turned = {k: d64[k].transpose(-1, -2) for k in ("s0", "ds_last")}
+    sq, _ = attend_slack(d64["do"], d64["v"], d64["k"], log_decay, scale, turned["s0"], ends, False, kind)
+    sk, _ = attend_slack(d64["v"], d64["do"], scale * d64["q"], log_decay, 1.0, turned["ds_last"], ends, True, kind)
+    sv, s0s = attend_slack(d64["k"], scale * d64["q"], d64["do"], log_decay, 1.0, d64["ds_last"], ends, True, kind)
+    check(dq, want[0], sq, what + "dq")
+    check(dk_, want[1], sk, what + "dk")
+    check(dv_, want[2], sv, what + "dv")
+    check(ds0, want[3], s0s, what + "ds0")
+
+
+ATTENTION = [
+    # n, t, h, dk, dv
+    (1, 1, 1, 1, 1),
+    (2, 1, 3, 64, 64),
+    (1, 2, 2, 5, 7),
+    (3, 63, 2, 16, 33),
+    (2, 64, 1, 64, 64),
+    (2, 65, 2, 128, 72),
+    (3, 130, 3, 33, 128),
+    (2, 140, 2, 256, 40),
+    (1, 100, 1, 96, 256),
+    (4, 17, 2, 64, 130),
+    (3, 200, 2, 80, 136),
+    (2, 129, 1, 200, 200),
+    (1, 66, 1, 255, 17),
+    (2, 256, 2, 31, 31),
+]
+
+
+@gpu
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", ATTENTION)
+def test_attention_forward_and_backward(shape, kind, ragged):
+    data, lengths = attention_case(*shape, kind, ragged, sum(shape))
+    run_attention(data, lengths, decays(shape[2]), shape[3] ** -0.5, kind)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -5.0, -90.0, -math.inf])
+def test_attention_decays(decay, kind):
+    """Memories that do not fade, fade at once, or have none of the frames before (0 * infinity is nowhere)."""
+    data, lengths = attention_case(2, 150, 2, 32, 48, kind, True, 77)
+    run_attention(data, lengths, torch.tensor([decay, -0.2]), 0.3, kind)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attention_without_states_scale_and_ends(kind):
+    """Defaults: no state before, none of its gradient after, scale dk ** -0.5; lengths held to [0, t]."""
+    data, _ = attention_case(3, 70, 2, 36, 20, kind, False, 5)
+    data["s0"].zero_()
+    data["ds_last"].zero_()
+    ld = decays(2).cuda()
+    dev = {k: a.cuda() for k, a in data.items()}
+    o, s = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld)
+    o2, s2 = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld, 36 ** -0.5, s0=dev["s0"])
+    assert torch.equal(o, o2) and torch.equal(s, s2)
+    a = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld)
+    b = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld, 36 ** -0.5, s0=dev["s0"], ds_last=dev["ds_last"])
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    le = torch.tensor([70, 500, -3], dtype=torch.int32, device="cuda")
+    o3, s3 = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld, lengths=le)
+    assert torch.equal(o3[:2], o[:2]) and not o3[2].any() and not s3[2].any() and torch.equal(s3[:2], s[:2])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attention_frame_by_frame(kind):
+    """Live frames, the state in place, against the clip."""
+    n, t, h, dk, dv = 3, 37, 2, 48, 80
+    data, _ = attention_case(n, t, h, dk, dv, kind, False, 9)
+    dev = {k: a.cuda() for k, a in data.items()}
+    ld, d64 = decays(h), {k: a.double() for k, a in data.items()}
+    so, ss = attend_slack(d64["q"], d64["k"], d64["v"], ld, 0.2, d64["s0"], [t] * n, False, kind)
+    o, s_last = attend64(d64["q"], d64["k"], d64["v"], ld, 0.2, d64["s0"], [t] * n)
+    state, ldc = dev["s0"].clone(), ld.cuda()
+    for j in range(t):
+        out, same = rrm.decay_attention(*(dev[k][:, j:j + 1] for k in ("q", "k", "v")), ldc, 0.2, s0=state, s_last=state)
+        assert same is state
+        check(out[:, 0], o[:, j], so[:, j], f"frame {j}")
+    check(state, s_last, ss, "state")
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("lo", [0, 1, 3, 8])
+def test_attention_strides(lo, kind):
+    """Features out of wider tensors at every alignment, in and out; frames outside of videos; heads that share keys."""
+    n, t, h, dk, dv = 2, 70, 3, 40, 24
+    wide = torch.randn(n, t, h, dk + 30, generator=gen(lo)).to(DT[kind]).cuda()
+    q = wide[..., lo:lo + dk]
+    k = torch.randn(t, n, h, dk, generator=gen(lo + 1)).to(DT[kind]).cuda().transpose(0, 1)
+    v = torch.randn(n, h, t, dv + 9, generator=gen(lo + 2)).to(DT[kind]).cuda()[..., 2:2 + dv].transpose(1, 2)
+    ld = decays(h).cuda()
+    back = torch.full((n, t, h, dv + 11), 7.0, device="cuda", dtype=DT[kind])
+    out = back[..., 3:3 + dv]
+    _, s = rrm.decay_attention(q, k, v, ld, 0.5, out=out)
+    want, s2 = rrm.decay_attention(q.contiguous(), k.contiguous(), v.contiguous(), ld, 0.5)
+    assert torch.equal(out, want) and torch.equal(s, s2)
+    assert (back[..., :3] == 7).all() and (back[..., 3 + dv:] == 7).all()
+    whole = [torch.full((n, h, t, d + 5), 7.0, device="cuda", dtype=DT[kind]) for d in (dk, dk, dv)]
+    dq, dk_, dv_ = (w[..., 1:-4].transpose(1, 2) for w in whole)
+    do = torch.randn(n, t, h, dv, generator=gen(4)).to(DT[kind]).cuda()
+    rrm.decay_attention_backward(do.transpose(0, 1).contiguous().transpose(0, 1), q, k, v, ld, 0.5, dq=dq, dk=dk_, dv=dv_)
+    ref = rrm.decay_attention_backward(do, q.contiguous(), k.contiguous(), v.contiguous(), ld, 0.5)
+    for a, b in zip((dq, dk_, dv_), ref):
+        assert torch.equal(a, b)
+    for w in whole:
+        assert (w[..., :1] == 7).all() and (w[..., -4:] == 7).all()
+    shared = k[:, :, :1].expand(n, t, h, dk)
+    a = rrm.decay_attention(q, shared, v, ld, 0.5)
+    b = rrm.decay_attention(q, shared.contiguous(), v, ld, 0.5)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    a = rrm.decay_attention_backward(do, q, shared, v, ld, 0.5)
+    b = rrm.decay_attention_backward(do, q, shared.contiguous(), v, ld, 0.5)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+
+
+@gpu
+def test_attention_is_by_video_and_head():
+    """Not-a-numbers of one video's head stay in it, and in the frames from theirs on."""
+    data, _ = attention_case(3, 200, 3, 16, 16, "f32", False, 3)
+    dev = {k: a.cuda() for k, a in data.items()}
+    dev["v"][1, 90, 2, 5] = math.nan
+    dev["k"][2, 130, 0, 0] = math.inf
+    o, _ = rrm.decay_attention(dev["q"], dev["k"], dev["v"], decays(3).cuda(), s0=dev["s0"])
+    ok = torch.isfinite(o).all(-1).cpu()
+    assert not ok[1, 90:, 2].any() and not ok[2, 130:, 0].any()
+    # (frames before theirs in the same stretch of 64 multiply them by weights of 0)
+    ok[1, 64:, 2] = ok[2, 128:, 0] = True
+    assert ok.all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 9001, 2, 64, 48), (2, 5003, 1, 128, 128), (1, 4100, 1, 136, 72)])
+def test_attention_long(shape, kind):
+    """Few heads over many frames: the time axis is divided.  Against the recurrence in 64 bits, with ends in several places."""
+    n, t, h, dk, dv = shape
+    for lengths in (None, torch.tensor([t - 1357] + [64] * (n - 1), dtype=torch.int32)):
+        data, _ = attention_case(n, t, h, dk, dv, kind, False, t)
+        ends = [t] * n if lengths is None else lengths.tolist()
+        dev = {k: a.cuda() for k, a in data.items()}
+        d64 = {k: a.double() for k, a in dev.items()}
+        ld = decays(h).cuda()
+        le = None if lengths is None else lengths.cuda()
+        o, s_last = attend64(d64["q"], d64["k"], d64["v"], ld, 0.1, d64["s0"], ends)
+        so, ss = attend_slack(d64["q"], d64["k"], d64["v"], ld, 0.1, d64["s0"], ends, False, kind)
+        got, s = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld, 0.1, s0=dev["s0"], lengths=le)
+        check(got, o, so, "o")
+        check(s, s_last, ss, "s_last")
+        # the gradients are the same walk: of v by last frames first, of q by turned states
+        dq, dk_, dv_, ds0 = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld, 0.1, s0=dev["s0"], lengths=le, ds_last=dev["ds_last"])
+        grad, want = d64["ds_last"].clone(), [torch.zeros_like(d64[k]) for k in ("k", "v")]
+        lam = torch.exp(ld.double()).view(h, 1, 1)
+        for i in range(n):
+            for j in range(ends[i] - 1, -1, -1):
+                grad[i] += 0.1 * d64["q"][i, j][..., None] * d64["do"][i, j][..., None, :]
+                want[0][i, j] = (grad[i] * d64["v"][i, j][..., None, :]).sum(-1)
+                want[1][i, j] = (grad[i] * d64["k"][i, j][..., None]).sum(-2)
+                grad[i] *= lam
+        state, want_q = d64["s0"].clone(), torch.zeros_like(d64["q"])
+        for i in range(n):
+            for j in range(ends[i]):
+                state[i] = lam * state[i] + d64["k"][i, j][..., None] * d64["v"][i, j][..., None, :]
+                want_q[i, j] = 0.1 * (state[i] * d64["do"][i, j][..., None, :]).sum(-1)
+        t_s0, t_last = d64["s0"].transpose(-1, -2), d64["ds_last"].transpose(-1, -2)
+        check(dq, want_q, attend_slack(d64["do"], d64["v"], d64["k"], ld, 0.1, t_s0, ends, False, kind)[0], "dq")
+        check(dk_, want[0], attend_slack(d64["v"], d64["do"], 0.1 * d64["q"], ld, 1.0, t_last, ends, True, kind)[0], "dk")
+        sv, s0s = attend_slack(d64["k"], 0.1 * d64["q"], d64["do"], ld, 1.0, d64["ds_last"], ends, True, kind)
+        check(dv_, want[1], sv, "dv")
+        check(ds0, grad, s0s, "ds0")
+
+
+@gpu
+def test_attention_gradients_against_differences():
+    data, _ = attention_case(1, 70, 1, 8, 8, "f32", False, 12)
+    dev = {k: a.cuda() for k, a in data.items()}
+    ld = torch.tensor([-0.05], device="cuda")
+
+    def loss(x):
+        o, s = rrm.decay_attention(x["q"], x["k"], x["v"], ld, 0.5, s0=x["s0"])
+        return float((o.double() * dev["do"].double()).sum() + (s.double() * dev["ds_last"].double()).sum())
+
+    grads = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld, 0.5, s0=dev["s0"], ds_last=dev["ds_last"])
+    for name, g in zip(("q", "k", "v", "s0"), grads):
+        way = torch.randn(dev[name].shape, generator=gen(1)).cuda()
+        up, down = (loss({**dev, name: dev[name] + e * way}) for e in (0.5, -0.5))
+        # (linear in each of them alone: the difference is exact but for rounding)
+        slope = float((g.double() * way.double()).sum())
+        size = float((g.double() * way.double()).abs().sum())
+        assert abs(up - down - slope) <= 2e-4 * size, name
+
+
+@gpu
+def test_attention_of_nothing():
+    ld = torch.tensor([-0.1, -0.2], device="cuda")
+    q = torch.empty(3, 0, 2, 4, device="cuda")
+    v = torch.empty(3, 0, 2, 5, device="cuda")
+    s0 = torch.randn(3, 2, 4, 5, device="cuda")
+    o, s = rrm.decay_attention(q, q, v, ld, s0=s0)
+    assert o.shape == v.shape and torch.equal(s, s0)
+    dq, dk, dv, ds0 = rrm.decay_attention_backward(v, q, q, v, ld, s0=s0, ds_last=s0)
+    assert dq.shape == q.shape and dv.shape == v.shape and torch.equal(ds0, s0)
+    assert not rrm.decay_attention(q, q, v, ld)[1].any()
+    e = torch.empty(0, 9, 2, 4, device="cuda")
+    assert rrm.decay_attention(e, e, e, ld)[0].shape == e.shape
+
+
+# -- norms behind and before a block -------------------------------------------------------------------------------------
+
+def residual64(x, b, gate, scale, post, pre, eps):
+    p = b
+    if post is not None:
+        p = b / torch.sqrt((b * b).mean(-1, keepdim=True) + eps) * post
+    q = torch.ones_like(b)
+    if gate is not None:
+        q = torch.sigmoid(gate)
+    if scale is not None:
+        q = q * scale
+    r = x + q * p
+    u = None if pre is None else r / torch.sqrt((r * r).mean(-1, keepdim=True) + eps) * pre
+    return r, u
+
+
+def residual_slack(x, b, gate, scale, post, pre, eps, dr=None, du=None):
+    """What the results may be off by, elementwise.  rb and rr are roots of sums held as trees (SUM of themselves), a gate is off by GATE, so r by
+    dr_ = SUM |x| + (SUM + GATE) |q p|; rr besides by its share of r's error, rms(dr_) rr; rh by 48 u a + 96 u kappa |rh| where a = rr (|x| + |q p|) and kappa = 1 +
+    rms(a) takes account of x and q p that cancel; then what the formulas make of these."""
+    rb = 1 / torch.sqrt((b * b).mean(-1, keepdim=True) + eps) if post is not None else 1.0
+    bh = b * rb
+    p = bh * post if post is not None else bh
+    sg = torch.sigmoid(gate) if gate is not None else torch.ones_like(b)
+    q = sg * scale if scale is not None else sg
+    r = x + q * p
+    rr = 1 / torch.sqrt((r * r).mean(-1, keepdim=True) + eps)
+    off = SUM * x.abs() + (SUM + GATE) * (q * p).abs()
+    out = {"r": off}
+    if pre is not None:
+        out["u"] = pre.abs() * rr * (off + r.abs() * (SUM + rr * torch.sqrt((off * off).mean(-1, keepdim=True))))
+    if dr is None and du is None:
+        return out
+    mean = lambda z: z.mean(-1, keepdim=True)  # noqa: E731
+    w = du * pre if du is not None else torch.zeros_like(x)
+    dr = torch.zeros_like(x) if dr is None else dr
+    a = rr * (x.abs() + (q * p).abs())
+    kappa = 1 + torch.sqrt(mean(a * a))
+    rh = r * rr
+    m1 = mean(w * rh)
+    dx = dr + rr * (w - rh * m1)
+    off = 64 * U * (dr.abs() + rr * w.abs()) + rr * 400 * U * kappa * a * mean(w.abs() * a)
+    dp = dx * q
+    off_dp = q.abs() * off + 20 * U * dp.abs()
+    pb = torch.ones_like(x) * (post if post is not None else 1.0)
+    off_m2 = 2 * mean((pb * bh).abs() * off_dp) + 32 * U * mean((pb * bh * q).abs() * (dr.abs() + rr * w.abs() + rr * rh.abs() * m1.abs()))
+    slope = (sg * (1 - sg) * p * (scale if scale is not None else 1.0)).abs()
+    out["dx"] = off
+    out["dgate"] = slope * off + (3 * GATE + SUM) * (slope * dx.abs())
+    if post is not None:
+        out["db"] = rb * (pb.abs() * off_dp + bh.abs() * off_m2) + 64 * U * rb * ((dp * pb).abs() + bh.abs() * mean((dp * pb * bh).abs()))
+    else:
+        out["db"] = off_dp
+    rows = tuple(range(x.dim() - 1))
+    every = lambda off, mag: (off + (SUM + GATE) * mag).sum(rows)  # noqa: E731
+    out["dscale"] = every((sg * p).abs() * off, (dx * sg * p).abs())
+    out["dpost"] = every(bh.abs() * off_dp, (dp * bh).abs())
+    if du is not None:
+        out["dpre"] = every(du.abs() * 150 * U * kappa * a, (du * rh).abs())
+    return out
+
+
+RESIDUAL = [(1, 1), (3, 2), (5, 16), (17, 33), (2, 128), (9, 129), (40, 512), (33, 513), (6, 1001), (3, 1024), (70, 1500), (2, 2048), (5, 4095), (2, 4096),
+            (3, 5000), (2, 8192), (2, 8193), (1, 16384), (2100, 24), (1300, 640)]
+
+
+def residual_case(m, c, kinds, parts, seed):
+    g = gen(seed)
+    tx, tb = DT[kinds[0]], DT[kinds[1]]
+    d = {"x": (2 * torch.randn(m, c, generator=g) + torch.randn(c, generator=g)).to(tx), "b": (0.7 * torch.randn(m, c, generator=g)).to(tb),
+         "gate": torch.randn(m, c, generator=g).to(tb), "scale": 0.5 + 0.1 * torch.randn(c, generator=g), "post": 1 + 0.2 * torch.randn(c, generator=g),
+         "pre": 1 + 0.2 * torch.randn(c, generator=g), "dr": torch.randn(m, c, generator=g).to(tx), "du": torch.randn(m, c, generator=g).to(tb)}
+    for k in ("gate", "scale", "post", "pre"):
+        if k not in parts:
+            d[k] = None
+    if "pre" not in parts:
+        d["du"] = None
+    return d
+
+
+def run_residual(d, eps, what=""):
+    names = ("x", "b", "gate", "scale", "post", "pre")
+    d64 = {k: None if v is None else v.double() for k, v in d.items()}
+    leaves = {k: d64[k].clone().requires_grad_() for k in names if d64[k] is not None}
+    r, u = residual64(*(leaves.get(k) for k in names), eps)
+    outs, grads = ((r,), (d64["dr"],)) if u is None else ((r, u), (d64["dr"], d64["du"]))
+    want = dict(zip(leaves, torch.autograd.grad(outs, list(leaves.values()), grads)))
+    slack = residual_slack(*(d64[k] for k in names), eps, d64["dr"], d64["du"])
+    dev = {k: None if v is None else v.cuda() for k, v in d.items()}
+    stats = torch.empty(*d["x"].shape[:-1], 2, device="cuda")
+    got_r, got_u = rrm.residual_norm(*(dev[k] for k in names), eps, stats=stats)
+    check(got_r, r, slack["r"], what + "r")
+    if u is None:
+        assert got_u is None
+    else:
+        check(got_u, u, slack["u"], what + "u")
+    got = rrm.residual_norm_backward(dev["dr"], dev["du"], dev["x"], dev["b"], stats, dev["gate"], dev["scale"], dev["post"], dev["pre"])
+    for k, g in zip(names, got):
+        if k not in leaves:
+            assert g is None
+        else:
+            check(g, want[k], slack["d" + k], what + "d" + k)
+
+
+@gpu
+@pytest.mark.parametrize("kinds", [("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("shape", RESIDUAL)
+def test_residual_forward_and_backward(shape, kinds):
+    run_residual(residual_case(*shape, kinds, ("gate", "scale", "post", "pre"), sum(shape)), 1e-6)
+
+
+@gpu
+@pytest.mark.parametrize("kinds", [("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("parts", [(), ("pre",), ("gate",), ("scale", "pre"), ("post", "pre"), ("gate", "post"), ("gate", "scale", "pre"), ("scale", "post", "pre")])
+def test_residual_parts(parts, kinds):
+    for shape in ((7, 72), (5, 3000)):
+        run_residual(residual_case(*shape, kinds, parts, len(parts)), 1e-5)
+
+
+@gpu
+def test_residual_norm_alone():
+    """Without a block: the norm before the first, with its gradients; r is x itself."""
+    x = torch.randn(3, 5, 200, generator=gen(1))
+    pre = torch.rand(200, generator=gen(2)) + 0.5
+    du, dr = torch.randn(3, 5, 200, generator=gen(3)), torch.randn(3, 5, 200, generator=gen(4))
+    xd = x.cuda()
+    stats = torch.empty(3, 5, 2, device="cuda")
+    r, u = rrm.residual_norm(xd, pre=pre.cuda(), stats=stats)
+    assert r is xd
+    x64, p64 = x.double().requires_grad_(), pre.double().requires_grad_()
+    want = x64 / torch.sqrt((x64 * x64).mean(-1, keepdim=True) + 1e-6) * p64
+    zero = torch.zeros_like(x64)
+    slack = residual_slack(x64.detach(), zero.detach(), None, None, None, p64.detach(), 1e-6, dr.double(), du.double())
+    check(u, want, slack["u"], "u")
+    gx, gp = torch.autograd.grad(want, (x64, p64), du.double())
+    dx, db, dgate, dscale, dpost, dpre = rrm.residual_norm_backward(dr.cuda(), du.cuda(), xd, None, stats, pre=pre.cuda())
+    assert db is None and dgate is None and dscale is None and dpost is None
+    check(dx, gx + dr.double(), slack["dx"], "dx")
+    check(dpre, gp, slack["dpre"], "dpre")
+    # one of the two gradients alone
+    only = rrm.residual_norm_backward(None, du.cuda(), xd, None, stats, pre=pre.cuda())[0]
+    check(only, gx, slack["dx"], "dx of du alone")
+    passed = rrm.residual_norm_backward(dr.cuda(), None, xd, None, stats, pre=pre.cuda())
+    assert torch.equal(passed[0].cpu(), dr) and not passed[5].any()
+    half = rrm.residual_norm(xd, pre=pre.cuda(), u_dtype=torch.bfloat16)[1]
+    check(half, want, slack["u"], "u in bfloat16")
+
+
+@gpu
+@pytest.mark.parametrize("lo", [0, 1, 2, 8])
+def test_residual_strides(lo):
+    m, c = 6, 300
+    wide = torch.randn(m, c + 40, generator=gen(lo)).cuda()
+    x = wide[:, lo:lo + c]
+    b = torch.randn(m, 2 * c, generator=gen(lo + 1)).bfloat16().cuda()[:, 1:1 + c]
+    gate = torch.randn(m, c + 3, generator=gen(lo + 2)).bfloat16().cuda()[:, 3:]
+    w = [torch.rand(c, device="cuda") + 0.5 for _ in range(3)]
+    outs = [torch.full((m, c + 9), 7.0, device="cuda", dtype=t) for t in (torch.float32, torch.bfloat16)]
+    r, u = (o[:, 2:2 + c] for o in outs)
+    stats = torch.empty(m, 2, device="cuda")
+    rrm.residual_norm(x, b, gate, *w, out=r, u=u, stats=stats)
+    r2, u2 = rrm.residual_norm(x.contiguous(), b.contiguous(), gate.contiguous(), *w)
+    assert torch.equal(r, r2) and torch.equal(u, u2)
+    for o in outs:
+        assert (o[:, :2] == 7).all() and (o[:, 2 + c:] == 7).all()
+    dr, du = torch.randn(m, c + 1, device="cuda")[:, 1:], torch.randn(m, c + 2, device="cuda").bfloat16()[:, :c]
+    grads = [torch.full((m, c + 7), 7.0, device="cuda", dtype=t) for t in (torch.float32, torch.bfloat16, torch.bfloat16)]
+    dx, db, dgate = (o[:, 3:3 + c] for o in grads)
+    got = rrm.residual_norm_backward(dr, du, x, b, stats, gate, *w, dx=dx, db=db, dgate=dgate)
+    ref = rrm.residual_norm_backward(dr.contiguous(), du.contiguous(), x.contiguous(), b.contiguous(), stats, gate.contiguous(), *w)
+    for a, e in zip(got, ref):
+        assert torch.equal(a, e)
+    for o in grads:
+        assert (o[:, :3] == 7).all() and (o[:, 3 + c:] == 7).all()
+    # in place, and one row for all of them
+    y = x.contiguous()
+    r3, u3 = rrm.residual_norm(y, b, gate, *w, out=y)
+    assert r3 is y and torch.equal(y, r2) and torch.equal(u3, u2)
+    one = gate[:1].expand(m, c)
+    assert torch.equal(rrm.residual_norm(x, b, one, *w)[0], rrm.residual_norm(x, b, one.contiguous(), *w)[0])
+
+
+@gpu
+def test_residual_is_by_row():
+    """Rows of zeros give zeros; a row's not-a-numbers and infinities are its own."""
+    x, b = torch.randn(300, 96, device="cuda"), torch.randn(300, 96, device="cuda")
+    x[7], b[7] = 0, 0
+    b[11, 3] = math.nan
+    x[13, 5] = math.inf
+    w = torch.ones(96, device="cuda")
+    r, u = rrm.residual_norm(x, b, None, None, w, w)
+    ok = torch.isfinite(u).all(-1)
+    want = torch.ones(300, dtype=torch.bool, device="cuda")
+    want[11] = want[13] = False
+    assert torch.equal(ok, want)
+    assert not r[7].any() and not u[7].any()
+
+
+@gpu
+def test_residual_of_nothing():
+    x = torch.empty(0, 40, device="cuda")
+    w = torch.ones(40, device="cuda")
+    stats = torch.empty(0, 2, device="cuda")
+    r, u = rrm.residual_norm(x, x, x, w, w, w, stats=stats)
+    assert r.shape == u.shape == (0, 40)
+    got = rrm.residual_norm_backward(x, x, x, x, stats, x, w, w, w)
+    assert got[0].shape == (0, 40) and not any(g.any() for g in got[3:])
+
+
+# -- orthogonal updates ------------------------------------------------------------------------------------------------
+
+def poly(co, s):
+    return co[0] * s + co[1] * s ** 3 + co[2] * s ** 5
+
+
+def newton_schulz(g, steps, co, eps):
+    """The iteration in 64 bits, and what its result may be off by in the Frobenius norm.
+
+    A step as it is computed rounds X, A = X X^T and B = b A + c A^2 to half precision, each off by w of itself, elementwise and so in the norm; with |X| <= x the
+    largest singular value and |X|_F = f that adds at most  w f (1 + |a| + x^2 (|b| + 2 |c| x^2 + |b| + |c| x^2) + ..) <= 4 w f (|a| + |b| x^2 + |c| x^4)  to the new X.  What
+    X is off by before a step is multiplied by no more than the largest of |p(s) - p(t)| / |s - t| and |p(s) + p(t)| / (s + t) over its singular
+    values (the derivative of a function of singular values in that norm), here with a twentieth for what is not linear in it."""
+    x = g / (torch.linalg.norm(g) + eps)
+    off = W * float(torch.linalg.norm(x))
+    for _ in range(steps):
+        u, s, vh = torch.linalg.svd(x, full_matrices=False)
+        a, b = s[:, None], s[None, :]
+        pa, pb = poly(co, a), poly(co, b)
+        apart = (a - b).abs()
+        grow = torch.where(apart > 1e-9, (pa - pb).abs() / apart.clamp(min=1e-9), (co[0] + 3 * co[1] * a ** 2 + 5 * co[2] * a ** 4).abs() + 0 * b)
+        grow = max(float(grow.max()), float(((pa + pb).abs() / (a + b + 1e-300)).max()), abs(co[0]))
+        top, f = float(s[0]), float(torch.linalg.norm(x))
+        off = 1.05 * grow * off + 4 * W * f * (abs(co[0]) + abs(co[1]) * top ** 2 + abs(co[2]) * top ** 4)
+        x = (u * poly(co, s)) @ vh
+    return x, off
+
+
+FAST = (3.4445, -4.7750, 2.0315)
+SURE = (1.875, -1.25, 0.375)
+ORTH = [(1, 1), (1, 9), (9, 1), (5, 7), (16, 16), (33, 130), (130, 33), (64, 512), (128, 128), (129, 127), (257, 300), (300, 70), (520, 264)]
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", ORTH)
+def test_orthogonalize(shape, kind):
+    g = (1e-3 * torch.randn(2, *shape, generator=gen(sum(shape))) * torch.exp(0.5 * torch.randn(2, shape[0], 1, generator=gen(1)))).to(DT[kind])
+    for steps, co in ((1, FAST), (2, SURE), (5, FAST)):
+        got = rrm.orthogonalize(g.cuda(), steps, co).cpu().double()
+        for i in range(2):
+            want, off = newton_schulz(g[i].double(), steps, co, 1e-7)
+            # (the result's own rounding beside it)
+            lim = off + V * (float(torch.linalg.norm(want)) + off)
+            err = float(torch.linalg.norm(got[i] - want))
+            assert err <= lim, f"{steps} steps {co}: {err} > {lim}"
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(24, 24), (40, 200), (200, 40), (128, 512)])
+def test_orthogonalize_converges(shape):
+    """The polynomial that keeps 1 where it is: the matrix's polar factor, off by the last step's roundings alone, as its derivative at 1 is 0."""
+    u, _, vh = torch.linalg.svd(torch.randn(*shape, generator=gen(2), dtype=F64), full_matrices=False)
+    few = min(shape)
+    g = (u * torch.linspace(0.5, 1.5, few, dtype=F64)) @ vh
+    got = rrm.orthogonalize(g.float().cuda(), 14, SURE).cpu().double()
+    want = u @ vh
+    lim = (4 * W * sum(map(abs, SURE)) + W + V) * math.sqrt(few) * 1.1
+    assert float(torch.linalg.norm(got - want)) <= lim
+
+
+@gpu
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e20])
+def test_orthogonalize_has_no_scale(size):
+    """G's size counts only beside eps."""
+    g = torch.randn(48, 80, generator=gen(3))
+    a = rrm.orthogonalize(g.cuda(), eps=0.0).float()
+    b = rrm.orthogonalize((g.double() * size).float().cuda(), eps=0.0).float()
+    # (inputs that differ in their rounding)
+    want, off = newton_schulz(g.double(), 5, FAST, 0.0)
+    lim = off + V * (float(torch.linalg.norm(want)) + off)
+    for got in (a, b):
+        assert float(torch.linalg.norm(got.cpu().double() - want)) <= lim
+
+
+@gpu
+def test_orthogonalize_matrices_strides_and_nothing():
+    g = torch.randn(2, 3, 40, 56, generator=gen(4))
+    d = g.cuda()
+    every = rrm.orthogonalize(d)
+    assert every.shape == g.shape and every.dtype is torch.bfloat16
+    for i in range(2):
+        for j in range(3):
+            assert torch.equal(rrm.orthogonalize(d[i, j]), every[i, j])
+    wide = torch.zeros(6, 43, 61, device="cuda")
+    wide[:, 1:41, 3:59] = d.view(6, 40, 56)
+    back = torch.full((6, 41, 59), 7.0, device="cuda", dtype=torch.bfloat16)
+    rrm.orthogonalize(wide[:, 1:41, 3:59], out=back[:, :40, 2:58])
+    assert torch.equal(back[:, :40, 2:58], every.view(6, 40, 56))
+    back[:, :40, 2:58] = 7
+    assert (back == 7).all()
+    zeros = torch.zeros(2, 17, 30, device="cuda")
+    assert not rrm.orthogonalize(zeros).any() and not rrm.orthogonalize(zeros, eps=0.0).any()
+    assert rrm.orthogonalize(torch.empty(0, 5, 6, device="cuda")).shape == (0, 5, 6)
+    bad = d.view(6, 40, 56).clone()
+    bad[2, 3, 4] = math.nan
+    got = rrm.orthogonalize(bad)
+    ok = torch.isfinite(got.float()).view(6, -1).all(-1).tolist()
+    assert ok == [True, True, False, True, True, True]
+    assert torch.equal(got[3], every.view(6, 40, 56)[3])
