@@ -26,6 +26,11 @@ struct Walk {
     float taken, given;  // factors of k^T v as the state takes it up, and of the result
     const float* log_decay;
     const int32_t* lengths;
+    // In chunks, a launch takes `dk` of the state's keys, from `first_key` on, of `keys` in all (q and k begin with them).  What the keys before give waits in
+    // `part`, fp32 [n][t][h][dv]: written by a launch that is not the last, added by one that is not the first.
+    int first_key, keys;
+    bool adds, leaves;
+    float* part;
 };
 
 __device__ __forceinline__ int frames_of(const Walk& w, int video) {
@@ -129,17 +134,18 @@ __global__ __launch_bounds__(256) void step_kernel(Walk w, unsigned first) {
 //      result_i = sum over j up to i of lambda^(i-j) (q_i . k_j) v_j + lambda^(i+1) q_i W        W' = lambda^C W + sum of lambda^(C-1-j) k_j^T v_j
 // (where the state decays behind a frame: lambda^i and lambda^(C-j)).  Only non-negative powers occur, so no decay overflows.
 //
-// A workgroup has a tile of DV columns of a head's state, in registers in 32 bits, and walks a stretch of frames; a wavefront makes 32 x 32 results and holds
-// 32 columns of the state.  q, k, v of the next chunk are fetched into registers while this one is multiplied.  Products are v_mfma_f32_32x32x16_bf16 (fp32
-// tensors: v_mfma_f32_32x32x2_f32).  In bfloat16 two operands are rounded: the scores with their decays, and the copy of the state that queries read;
-// lambda^(C-1-j) v_j goes into the state as three bfloat16 parts, which hold all 24 bits of it, as the state's rounding errors would stay for as long as it remembers.
-typedef float v16f __attribute__((ext_vector_type(16)));
+// A workgroup has a tile of DV columns of a head's state, in registers in 32 bits, and walks a stretch of frames; a wavefront has 16 of the columns and makes
+// the results of all C frames in them.  q, k, v of the next chunk are fetched into registers while this one is multiplied.  Products are
+// v_mfma_f32_16x16x32_bf16 (fp32 tensors: v_mfma_f32_16x16x4_f32); the state's registers are an operand as they stand, and the scores, made once, meet the
+// wavefronts through LDS.  In bfloat16 two operands are rounded: the scores with their decays, and the state where queries read it;
+// lambda^(C-1-j) v_j goes into the state as three bfloat16 parts, which hold all 24 bits of it, as the state's rounding errors stay for as long as it remembers.
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v8f __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds4_t;
 
-// Eight elements along the summed axis of one row of an operand, of the 16 that a step takes
+// Eight elements along the summed axis of one row of an operand, of the 32 that a step takes
 template <typename T>
 struct FragmentOf;
 template <>
@@ -153,71 +159,99 @@ struct FragmentOf<float> {
 template <typename T>
 using Fragment = typename FragmentOf<T>::type;
 
-__device__ __forceinline__ v16f multiply(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ v16f multiply(v8f a, v8f b, v16f c) {
+// Lane l of the result: row 4 (l / 16) + register of a, column l % 16 (a row of b)
+__device__ __forceinline__ v4f multiply(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f multiply(v8f a, v8f b, v4f c) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
     return c;
 }
-// Rows that lie along the summed axis: lane l has row l % 32, and the eight from (l / 32) * 8 on
-__device__ __forceinline__ v8bf along(const unsigned char* row, int step, int half, const __bf16*) {
-    return *reinterpret_cast<const v8bf*>(row + step * 32 + half * 16);
+// Rows that lie along the summed axis: lane l has row l % 16, and the eight from 8 (l / 16) on
+__device__ __forceinline__ v8bf along(const unsigned char* row, int step, int g, const __bf16*) { return *reinterpret_cast<const v8bf*>(row + step * 64 + g * 16); }
+__device__ __forceinline__ v8f along(const unsigned char* row, int step, int g, const float*) {
+    struct {
+        float4 lo, hi;
+    } v;
+    v.lo = *reinterpret_cast<const float4*>(row + step * 128 + g * 32);
+    v.hi = *reinterpret_cast<const float4*>(row + step * 128 + g * 32 + 16);
+    return __builtin_bit_cast(v8f, v);
 }
-__device__ __forceinline__ v8f along(const unsigned char* row, int step, int half, const float*) {
-    return *reinterpret_cast<const v8f*>(row + step * 64 + half * 32);
+// The same with the eight that lane l holds of two results' rows, 4 (l / 16) + {0 .. 3, 16 .. 19}: the order of the state in its registers
+__device__ __forceinline__ v8bf along_state(const unsigned char* row, int step, int g, const __bf16*) {
+    struct {
+        u32x2 lo, hi;
+    } v;
+    v.lo = *reinterpret_cast<const u32x2*>(row + step * 64 + g * 8);
+    v.hi = *reinterpret_cast<const u32x2*>(row + step * 64 + g * 8 + 32);
+    return __builtin_bit_cast(v8bf, v);
 }
-// Rows that lie across it, turned on the way from LDS: lane l has column c0 + l % 32, and frames 4 (l / 32) + {0 .. 3, 8 .. 11} of the step's
-// 16: the order in which the registers of a product hold its rows, so that scores need no turning
+__device__ __forceinline__ v8f along_state(const unsigned char* row, int step, int g, const float*) {
+    struct {
+        float4 lo, hi;
+    } v;
+    v.lo = *reinterpret_cast<const float4*>(row + step * 128 + g * 16);
+    v.hi = *reinterpret_cast<const float4*>(row + step * 128 + g * 16 + 64);
+    return __builtin_bit_cast(v8f, v);
+}
+// Rows that lie across it, turned on the way from LDS: lane l has column c0 + l % 16, and the step's frames from 8 (l / 16) on
 template <int PITCH>
 __device__ __forceinline__ v8bf across(const unsigned char* tile, int c0, int step, int lane, const __bf16*) {
-    const unsigned char* at = tile + (step * 16 + (lane >> 5) * 4 + ((lane >> 2) & 3)) * PITCH + c0 * 2 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const unsigned char* at = tile + (step * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3)) * PITCH + c0 * 2 + (lane & 3) * 8;
     struct {
         v4s lo, hi;
     } v;
     v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(at));
-    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(at + 8 * PITCH));
+    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(at + 4 * PITCH));
     return __builtin_bit_cast(v8bf, v);
 }
 template <int PITCH>
 __device__ __forceinline__ v8f across(const unsigned char* tile, int c0, int step, int lane, const float*) {
     v8f v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        v[e] = *reinterpret_cast<const float*>(tile + (step * 16 + (lane >> 5) * 4 + (e & 3) + (e >> 2) * 8) * PITCH + (c0 + (lane & 31)) * 4);
+    for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float*>(tile + (step * 32 + (lane >> 4) * 8 + e) * PITCH + (c0 + (lane & 15)) * 4);
     return v;
 }
 __device__ __forceinline__ float power(int e, float log2_decay) { return __builtin_amdgcn_exp2f((float)e * log2_decay); }
 // (a decay of 0: its zeroth power is 1)
 __device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.44269504088896f, -16384.0f); }
 
-// Stretches of the time axis, of `frames` frames each (whole chunks), a workgroup each: states[s] is the state before stretch s + 1, [pair][k][v]
-// as the forward pass lays them, or what stretch s alone adds to it.
+// Stretches of the time axis, of `frames` frames each (whole chunks), a workgroup each (none: the walk goes frame by frame): states[s] is the state before stretch
+// s + 1, [pair][k][v] as the forward pass lays them, or what stretch s alone adds to it.
 struct Stretches {
     int count, frames;
     float* states;
 };
 
+// An offset behind every buffer's end: reads zeros, writes nothing
+constexpr unsigned NOWHERE = 0xfffffff0u;
+
+// A barrier that waits for LDS alone: what is fetched of the next chunk stays on its way (__syncthreads would wait for it)
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <typename T, int DK, int DV, int C>
 struct Chunk {
-    static constexpr int IB = C / 32, DB = DV / 32, WAVES = IB * DB, THREADS = 64 * WAVES, SB = DK / 32 / IB;
-    static constexpr int E = (int)sizeof(T), EPC = 16 / E;  // bytes of an element, elements of 16 bytes
-    static constexpr int PK = DK * E + 32, PV = DV * E + 64;  // bytes between rows in LDS: reads of a wavefront meet different banks
-    static constexpr int QK_BYTES = C * PK, V_BYTES = C * PV, S_BYTES = DV * PK;
-    static constexpr int LDS = 2 * QK_BYTES + V_BYTES + S_BYTES, LDS_STATES = QK_BYTES + V_BYTES;
-    static constexpr int NK = C * DK / EPC / THREADS, NV = C * DV / EPC / THREADS;  // 16-byte chunks a thread stages
-    static_assert(NK * THREADS * EPC == C * DK && NV * THREADS * EPC == C * DV, "whole chunks a thread");
+    static constexpr int WAVES = DV / 16, THREADS = 64 * WAVES;
+    static constexpr int E = (int)sizeof(T), EPC = 16 / E;                                // bytes of an element, elements of 16 bytes
+    static constexpr int PK = DK * E + 16, PV = DV * E + 32, PP = C * E + 16;             // bytes between rows in LDS: reads of a wavefront meet different banks
+    static constexpr int QK_BYTES = C * PK, V_BYTES = C * PV, P_BYTES = C * PP;
+    static constexpr int LDS = 2 * QK_BYTES + V_BYTES + P_BYTES, LDS_STATES = QK_BYTES + V_BYTES;
+    static constexpr int NK = C * DK / EPC / THREADS, NV = C * DV / EPC / THREADS;        // 16-byte pieces a thread stages ..
+    static constexpr int RK = THREADS / (DK / EPC), RV = THREADS / (DV / EPC);            // .. of rows so far apart
+    static constexpr int AT_ONCE = WAVES * (163840 / LDS < 2 ? 1 : 2) / 4;                // wavefronts on a SIMD
+    static_assert(NK * RK == C && NV * RV == C, "whole pieces a thread");
 };
 
-// STATES: what a stretch alone adds to the state (q and the results are not touched)
-template <typename T, int DK, int DV, int C, bool STATES>
-__global__ __launch_bounds__((Chunk<T, DK, DV, C>::THREADS)) void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
+// STATES: what a stretch alone adds to the state (q and the results are not touched).  EXACT: rows of q, k and v are whole pieces of 16 bytes.
+template <typename T, int DK, int DV, int C, bool STATES, bool EXACT>
+__global__ __launch_bounds__((Chunk<T, DK, DV, C>::THREADS)) __attribute__((amdgpu_waves_per_eu(Chunk<T, DK, DV, C>::AT_ONCE, Chunk<T, DK, DV, C>::AT_ONCE)))
+void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     using K = Chunk<T, DK, DV, C>;
-    constexpr int IB = K::IB, SB = K::SB, EPC = K::EPC, STEPS = C / 16;
+    constexpr int SB = DK / 16, IB = C / 16, STEPS = C / 32, EPC = K::EPC;
     __shared__ __attribute__((aligned(256))) unsigned char lds[STATES ? K::LDS_STATES : K::LDS];
     unsigned char* const ks = lds;
     unsigned char* const vs = ks + K::QK_BYTES;
     unsigned char* const qs = vs + K::V_BYTES;
-    unsigned char* const ss = qs + K::QK_BYTES;
+    unsigned char* const ps = qs + K::QK_BYTES;
     const T* const tag = nullptr;
 
     // tiles of one head's state read the same q and k: beside one another on one XCD (workgroups go to the eight in turn)
@@ -229,187 +263,184 @@ __global__ __launch_bounds__((Chunk<T, DK, DV, C>::THREADS)) void walk_kernel(Wa
     const int stretch = (int)(unit % st.count);
     const int pair = (int)(unit / st.count), video = pair / w.h, head = pair - video * w.h;
     const int end = frames_of(w, video), last = end > 0 ? (end - 1) / st.frames : 0;
-    const int f0 = stretch * st.frames;                                     // (counted from the end where the walk goes back)
-    const int have = end - f0 < st.frames ? end - f0 : st.frames;           // frames of this stretch, none or fewer behind the end
+    const int f0 = stretch * st.frames;                            // (counted from the end where the walk goes back)
+    const int have = end - f0 < st.frames ? end - f0 : st.frames;  // frames of this stretch, none or fewer behind the end
     if (STATES && stretch >= last) return;
 
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5, lr = lane & 31;
-    const int ib = wave % IB, db = wave / IB;
-    const int c0 = slice * DV;  // first column
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, lr = lane & 15;
+    const int c0 = slice * DV, vcols = w.dv - c0;  // first column; columns from it on
     const T* q = (const T*)w.q.p + video * w.q.video + head * w.q.head;
     const T* k = (const T*)w.k.p + video * w.k.video + head * w.k.head;
-    const T* v = (const T*)w.v.p + video * w.v.video + head * w.v.head + c0;
+    const T* v = (const T*)w.v.p + video * w.v.video + head * w.v.head;
     T* o = (T*)const_cast<void*>(w.o.p) + video * w.o.video + head * w.o.head + c0;
-    const int vcols = w.dv - c0;
-    const int64_t area = (int64_t)w.dk * w.dv;
-    const int col = c0 + db * 32 + lr;  // of the state, this lane's
+    const int64_t area = (int64_t)w.keys * w.dv;
+    const int col = c0 + wave * 16 + lr;  // of the state, this lane's
 
-    // the state: block i, register 4 q + e: row (ib + i IB) 32 + 8 q + 4 half + e
-    v16f state[SB];
-    auto state_at = [&](int i, int r) { return (ib + i * IB) * 32 + 8 * (r >> 2) + 4 * half + (r & 3); };
-    auto place = [&](int row) { return w.turned ? (int64_t)col * w.dk + row : (int64_t)row * w.dv + col; };
+    // the state: block i, register r: row 16 i + 4 g + r
+    v4f state[SB];
+    const int64_t row_step = w.turned ? 1 : w.dv, corner = (w.turned ? (int64_t)col * w.keys : col) + w.first_key * row_step;
     const float* from = nullptr;
     if (!STATES) from = stretch == 0 ? (w.s_in ? w.s_in + pair * area : nullptr) : st.states + ((int64_t)(stretch - 1) * w.n * w.h + pair) * area;
 #pragma unroll
     for (int i = 0; i < SB; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = state_at(i, r);
-            state[i][r] = from && have >= 0 && row < w.dk && col < w.dv ? from[place(row)] : 0.0f;
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * i + 4 * g + r;
+            state[i][r] = from && have >= 0 && row < w.dk && col < w.dv ? from[corner + row * row_step] : 0.0f;
         }
 
     const float decay = log2_of(w.t > 0 ? w.log_decay[head] : 0.0f);
     const int late = w.back ? 0 : 1;
 
-    u32x4 hq[STATES ? 1 : K::NK], hk[K::NK], hv[K::NV];
-    auto fetch_one = [&](const T* p, int64_t frame, int row, int c, int cols, int n) -> u32x4 {  // row of a chunk of n frames
-        if (row >= n || c >= cols) return u32x4{0, 0, 0, 0};
-        const T* at = p + (w.back ? -row : row) * frame + c;
-        if (c + EPC <= cols) {
-            unsigned int x[4];
-            load_words<4>(at, x);
-            return u32x4{x[0], x[1], x[2], x[3]};
-        }
-        u32x4 x = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < EPC - 1; ++e)
-            if (c + e < cols) {
-                if constexpr (sizeof(T) == 4) x[e] = __float_as_uint((float)at[e]);
-                else x[e >> 1] |= (unsigned int)__builtin_bit_cast(unsigned short, at[e]) << (16 * (e & 1));
-            }
-        return x;
+    // This thread's 16 bytes of every RK-th row of q and k (of every RV-th of v): rows row + i RK, columns c on.  The last piece of a row that no whole
+    // pieces make up begins early.  (frames lie at most 2^22 elements apart: offsets within a chunk have 32 bits)
+    struct Part {
+        int row, c;
+        bool in, whole;
+        unsigned at;  // bytes from the lowest of the chunk's frames in memory ..
+        int apart;    // .. and between the rows
     };
-    auto fetch = [&](int f) __attribute__((always_inline)) {  // the chunk from frame f0 + f on
-        const int n = have - f;
-        const int64_t at = w.back ? end - 1 - f0 - f : f0 + f;
-        if (!STATES)
+    auto part_of = [&](int per, int rows, int64_t frame, int c0, int cols) {  // per: pieces in a row of LDS; columns c0 .. c0 + cols
+        Part p;
+        p.row = tid / per, p.c = tid % per * EPC;
+        p.in = p.c < cols, p.whole = p.c + EPC <= cols;
+        if (!EXACT && !p.whole) p.c = cols - EPC;
+        p.at = (unsigned)(((w.back ? rows - 1 - p.row : p.row) * frame + c0 + p.c) * K::E);
+        p.apart = (int)(rows * frame * K::E);
+        return p;
+    };
+    const Part pq = part_of(DK / EPC, K::RK, w.q.frame, 0, w.dk), pk = part_of(DK / EPC, K::RK, w.k.frame, 0, w.dk),
+               pv = part_of(DV / EPC, K::RV, w.v.frame, c0, vcols);
+    // (an offset behind a buffer's end reads zeros: no branches, and loads stay on their way)
+    auto fetch_rows = [&](u32x4* held, auto count, auto rows, const T* p, int64_t frame, const Part& part, int f) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value, R = decltype(rows)::value;
+        const int none = have - f < C ? C - (have - f) : 0;
+        const int64_t lowest = w.back ? (int64_t)(end - 1 - f0 - f) + none - (C - 1) : (int64_t)f0 + f - none;
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + lowest * frame), 0, 0x7fffffff, 0x00027000);
 #pragma unroll
-            for (int i = 0; i < K::NK; ++i) {
-                const int x = i * K::THREADS + tid;
-                hq[STATES ? 0 : i] = fetch_one(q + at * w.q.frame, w.q.frame, x / (DK / EPC), x % (DK / EPC) * EPC, w.dk, n);
-            }
-#pragma unroll
-        for (int i = 0; i < K::NK; ++i) {
-            const int x = i * K::THREADS + tid;
-            hk[i] = fetch_one(k + at * w.k.frame, w.k.frame, x / (DK / EPC), x % (DK / EPC) * EPC, w.dk, n);
+        for (int i = 0; i < N; ++i) {
+            held[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, part.in && part.row + i * R >= none ? part.at : NOWHERE,
+                                                            (w.back ? N - 1 - i : i) * part.apart, 0);
         }
+    };
+    const std::integral_constant<int, K::NK> nk;
+    const std::integral_constant<int, K::NV> nv;
+    const std::integral_constant<int, K::RK> rk;
+    const std::integral_constant<int, K::RV> rv;
+    u32x4 hq[STATES ? 1 : K::NK], hk[K::NK], hv[K::NV];
+    auto fetch = [&](int f) __attribute__((always_inline)) {  // the chunk from frame f0 + f on
+        fetch_rows(hk, nk, rk, k, w.k.frame, pk, f);
+        if constexpr (!STATES) fetch_rows(hq, nk, rk, q, w.q.frame, pq, f);
+        fetch_rows(hv, nv, rv, v, w.v.frame, pv, f);
+    };
+    auto put_row = [&](unsigned char* to, const Part& part, const u32x4& x) __attribute__((always_inline)) {
+        if (EXACT || part.whole) {
+            *reinterpret_cast<u32x4*>(to + part.c * K::E) = x;  // (behind the last column: zeros)
+        } else if (part.in) {
 #pragma unroll
-        for (int i = 0; i < K::NV; ++i) {
-            const int x = i * K::THREADS + tid;
-            hv[i] = fetch_one(v + at * w.v.frame, w.v.frame, x / (DV / EPC), x % (DV / EPC) * EPC, vcols, n);
+            for (int e = 0; e < EPC; ++e) {
+                if (part.c + e < 0) continue;  // (of the tile before)
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<unsigned int*>(to + (part.c + e) * 4) = x[e];
+                else *reinterpret_cast<unsigned short*>(to + (part.c + e) * 2) = (unsigned short)(x[e >> 1] >> (16 * (e & 1)));
+            }
         }
     };
     auto put = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < K::NK; ++i) {
-            const int x = i * K::THREADS + tid, at = x / (DK / EPC) * K::PK + x % (DK / EPC) * 16;
-            if (!STATES) *reinterpret_cast<u32x4*>(qs + at) = hq[STATES ? 0 : i];
-            *reinterpret_cast<u32x4*>(ks + at) = hk[i];
+            put_row(ks + (pk.row + i * K::RK) * K::PK, pk, hk[i]);
+            if constexpr (!STATES) put_row(qs + (pk.row + i * K::RK) * K::PK, pk, hq[i]);
         }
 #pragma unroll
-        for (int i = 0; i < K::NV; ++i) {
-            const int x = i * K::THREADS + tid;
-            *reinterpret_cast<u32x4*>(vs + x / (DV / EPC) * K::PV + x % (DV / EPC) * 16) = hv[i];
-        }
+        for (int i = 0; i < K::NV; ++i) put_row(vs + (pv.row + i * K::RV) * K::PV, pv, hv[i]);
     };
-    auto put_state = [&]() __attribute__((always_inline)) {  // [column][row]
-#pragma unroll
-        for (int i = 0; i < SB; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                unsigned char* at = ss + (db * 32 + lr) * K::PK + state_at(i, r) * K::E;
-                if constexpr (sizeof(T) == 4) {
-                    *reinterpret_cast<float4*>(at) = make_float4(state[i][r], state[i][r + 1], state[i][r + 2], state[i][r + 3]);
-                } else {
-                    u32x2 x;
-                    x.x = bf16_pair(state[i][r], state[i][r + 1]), x.y = bf16_pair(state[i][r + 2], state[i][r + 3]);
-                    *reinterpret_cast<u32x2*>(at) = x;
-                }
-            }
-    };
+    // once: zeros behind the last column, and above the diagonal of the scores
+    if (!EXACT) {
+        for (int i = tid; i < (STATES ? K::LDS_STATES : K::LDS) / 16; i += K::THREADS) *reinterpret_cast<u32x4*>(lds + i * 16) = u32x4{0, 0, 0, 0};
+        meet();
+    } else if (!STATES) {
+        for (int i = tid; i < K::P_BYTES / 16; i += K::THREADS) *reinterpret_cast<u32x4*>(ps + i * 16) = u32x4{0, 0, 0, 0};
+        meet();
+    }
 
-    // lambda^(i-j) of a block of scores on the diagonal and of one below it (lane: i = l % 32; register 4 q + e: j = 8 q + 4 half + e)
-    float on[16], below[IB > 1 ? 16 : 1];
-    if (!STATES)
+    const unsigned o_at = (unsigned)(((w.back ? 15 - lr : lr) * w.o.frame + wave * 16 + 4 * g) * K::E);  // a result, as Part::at
+
+    // lambda^(C-1-j) of the frames as `across` has them: lambda^(31-j) within a step, and the steps behind it
+    float enter[8], steps[STEPS];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int d = lr - (8 * (r >> 2) + 4 * half + (r & 3));
-            on[r] = d >= 0 ? w.given * w.taken * power(d, decay) : 0.0f;
-            if (IB > 1) below[IB > 1 ? r : 0] = w.given * w.taken * power(d + 32, decay);
-        }
-    const float read = w.given * power(ib * 32 + lr + late, decay);
-    float enter[STEPS][8], carry;  // lambda^(n-1-j) of the frames as `across` has them, lambda^n
-    auto weights = [&](int n) __attribute__((always_inline)) {
+    for (int e = 0; e < 8; ++e) enter[e] = w.taken * power(32 - late - g * 8 - e, decay);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int d = n - late - (s * 16 + half * 4 + (e & 3) + (e >> 2) * 8);
-                enter[s][e] = w.taken * power(d > 0 ? d : 0, decay);  // (behind the last frame: of zeros)
-            }
-        carry = power(n, decay);
-    };
-    weights(C);
+    for (int s = 0; s < STEPS; ++s)
+        steps[s] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(power(C - 32 - 32 * s, decay))));
 
     if (have > 0) fetch(0);
     for (int f = 0; f < have; f += C) {
-        const int n = have - f;
-        if (f > 0) __syncthreads();
+        // a chunk of fewer frames has them in its last rows, zeros before: every power but two stays as it is
+        const int none = have - f < C ? C - (have - f) : 0;
+        const float carry = power(C - none, decay);
+        if (f > 0) meet();
         put();
-        if (!STATES) put_state();
         if (f + C < have) fetch(f + C);
-        __syncthreads();
-        if (n < C) weights(n);
-        v16f out;
-        Fragment<T> score[STATES ? 1 : STEPS];
+        meet();
+        v4f out[STATES ? 1 : IB];
         if constexpr (!STATES) {
-            const unsigned char* const mine = qs + (ib * 32 + lr) * K::PK;
+            // blocks of scores on and below the diagonal, a wavefront each: lane: i = 16 ib + l % 16; register r: j = 16 jb + 4 g + r
+            for (int b = wave; b < IB * (IB + 1) / 2; b += K::WAVES) {
+                const int ib = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3, jb = b - ib * (ib + 1) / 2;
+                v4f p = {0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) out[r] = 0.0f;
+                for (int s = 0; s < DK / 32; ++s)
+                    p = multiply(along(ks + (jb * 16 + lr) * K::PK, s, g, tag), along(qs + (ib * 16 + lr) * K::PK, s, g, tag), p);
+                unsigned char* const to = ps + (ib * 16 + lr) * K::PP + (jb * 16 + 4 * g) * K::E;
+                float x[4];
 #pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                out = multiply(along(ss + (db * 32 + lr) * K::PK, s, half, tag), along(mine, s, half, tag), out);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) out[r] *= read;
-#pragma unroll
-            for (int jb = 0; jb < IB; ++jb)
-                if (jb <= ib) {
-                    v16f p;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) p[r] = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < DK / 16; ++s) p = multiply(along(ks + (jb * 32 + lr) * K::PK, s, half, tag), along(mine, s, half, tag), p);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float x = p[r] * (jb == ib ? on[r] : below[IB > 1 ? r : 0]);
-                        if constexpr (sizeof(T) == 4) score[STATES ? 0 : jb * 2 + (r >> 3)][r & 7] = x;
-                        else score[STATES ? 0 : jb * 2 + (r >> 3)][r & 7] = (__bf16)x;
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const int d = (ib - jb) * 16 + lr - 4 * g - r;
+                    x[r] = p[r] * (d >= 0 ? w.given * w.taken * power(d, decay) : 0.0f);
                 }
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+                else *reinterpret_cast<u32x2*>(to) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+            }
+            // what the state before gives: its registers are the operand
+#pragma unroll
+            for (int ib = 0; ib < IB; ++ib) out[ib] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < DK / 32; ++s) {
+                Fragment<T> x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (sizeof(T) == 4) x[e] = state[2 * s + (e >> 2)][e & 3];
+                    else x[e] = (__bf16)state[2 * s + (e >> 2)][e & 3];
+                }
+#pragma unroll
+                for (int ib = 0; ib < IB; ++ib) out[ib] = multiply(x, along_state(qs + (ib * 16 + lr) * K::PK, s, g, tag), out[ib]);
+            }
+#pragma unroll
+            for (int ib = 0; ib < IB; ++ib) {
+                const int d = ib * 16 + lr - none + late;
+                out[ib] *= w.given * power(d > 0 ? d : 0, decay);
+            }
+            meet();
         }
 #pragma unroll
-        for (int i = 0; i < SB; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) state[i][r] *= carry;
+        for (int i = 0; i < SB; ++i) state[i] *= carry;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const Fragment<T> fv = across<K::PV>(vs, db * 32, s, lane, tag);
+            const Fragment<T> fv = across<K::PV>(vs, wave * 16, s, lane, tag);
             if constexpr (!STATES)
-                if (s / 2 <= ib) out = multiply(fv, score[STATES ? 0 : s], out);
-            Fragment<T> fk[SB];
 #pragma unroll
-            for (int i = 0; i < SB; ++i) fk[i] = across<K::PK>(ks, (ib + i * IB) * 32, s, lane, tag);
+                for (int ib = 2 * s; ib < IB; ++ib) out[ib] = multiply(fv, along(ps + (ib * 16 + lr) * K::PP, s, g, tag), out[ib]);
             if constexpr (sizeof(T) == 4) {
                 Fragment<T> x;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = fv[e] * enter[s][e];
+                for (int e = 0; e < 8; ++e) x[e] = fv[e] * enter[e] * steps[s];
 #pragma unroll
-                for (int i = 0; i < SB; ++i) state[i] = multiply(fk[i], x, state[i]);
+                for (int i = 0; i < SB; ++i) state[i] = multiply(across<K::PK>(ks, i * 16, s, lane, tag), x, state[i]);
             } else {
                 Fragment<T> hi, mid, lo;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = (float)fv[e] * enter[s][e];
+                    const float x = (float)fv[e] * enter[e] * steps[s];
                     hi[e] = (__bf16)x;
                     const float rest = x - (float)hi[e];
                     mid[e] = (__bf16)rest;
@@ -417,48 +448,47 @@ __global__ __launch_bounds__((Chunk<T, DK, DV, C>::THREADS)) void walk_kernel(Wa
                 }
 #pragma unroll
                 for (int i = 0; i < SB; ++i) {
-                    state[i] = multiply(fk[i], hi, state[i]);
-                    state[i] = multiply(fk[i], mid, state[i]);
-                    state[i] = multiply(fk[i], lo, state[i]);
+                    const Fragment<T> fk = across<K::PK>(ks, i * 16, s, lane, tag);
+                    state[i] = multiply(fk, hi, state[i]);
+                    state[i] = multiply(fk, mid, state[i]);
+                    state[i] = multiply(fk, lo, state[i]);
                 }
             }
         }
         if constexpr (!STATES) {
-            // lane: frame ib 32 + l % 32; registers 4 q + e: columns db 32 + 8 q + 4 half + e
-            const int row = ib * 32 + lr;
-            if (w.o.p && row < n) {
-                T* to = o + (w.back ? end - 1 - f0 - f - row : (int64_t)f0 + f + row) * w.o.frame + db * 32;
-                const int cols = vcols - db * 32;
-                if constexpr (sizeof(T) == 4) {
+            // lane: frame 16 ib + l % 16; register r: column 16 wave + 4 g + r
+            const int c = wave * 16 + 4 * g;
+            const int64_t lowest = w.back ? (int64_t)(end - 1 - f0 - f) + none - (C - 1) : (int64_t)f0 + f - none;
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(o + lowest * w.o.frame, 0, 0x7fffffff, 0x00027000);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int c = 8 * g + 4 * half;
-                        if (c + 4 <= cols) {
-                            const unsigned int x[4] = {__float_as_uint(out[4 * g]), __float_as_uint(out[4 * g + 1]), __float_as_uint(out[4 * g + 2]),
-                                                       __float_as_uint(out[4 * g + 3])};
-                            store_words<4>(to + c, x);
-                        } else {
+            for (int ib = 0; ib < IB; ++ib) {
+                const int row = ib * 16 + lr;
+                if (w.adds || w.leaves) {
+                    float* const part = w.part + ((video * (int64_t)w.t + lowest + (w.back ? C - 1 - row : row)) * w.h + head) * w.dv + c0 + c;
+                    if (row >= none && w.o.p)
 #pragma unroll
-                            for (int e = 0; e < 3; ++e)
-                                if (c + e < cols) to[c + e] = out[4 * g + e];
-                        }
+                        for (int e = 0; e < 4; ++e)
+                            if (c + e < vcols) {
+                                if (w.adds) out[ib][e] += part[e];
+                                if (w.leaves) part[e] = out[ib][e];
+                            }
+                    if (w.leaves) continue;
+                }
+                const bool goes = row >= none && w.o.p;
+                const int apart = (w.back ? IB - 1 - ib : ib) * 16 * (int)w.o.frame * K::E;
+                if (EXACT || c + 4 <= vcols || c >= vcols) {
+                    const unsigned to = goes && c < vcols ? o_at : NOWHERE;
+                    if constexpr (sizeof(T) == 4) {
+                        const u32x4 x = {__float_as_uint(out[ib][0]), __float_as_uint(out[ib][1]), __float_as_uint(out[ib][2]), __float_as_uint(out[ib][3])};
+                        __builtin_amdgcn_raw_buffer_store_b128(x, buffer, to, apart, 0);
+                    } else {
+                        const u32x2 x = {bf16_pair(out[ib][0], out[ib][1]), bf16_pair(out[ib][2], out[ib][3])};
+                        __builtin_amdgcn_raw_buffer_store_b64(x, buffer, to, apart, 0);
                     }
-                } else {
+                } else if (goes) {
 #pragma unroll
-                    for (int g = 0; g < 4; g += 2) {
-                        // a lane gets the eight columns 8 (g + half) on: its own four of them and those of the lane 32 from it
-                        const auto lo = __builtin_amdgcn_permlane32_swap(bf16_pair(out[4 * g], out[4 * g + 1]), bf16_pair(out[4 * g + 4], out[4 * g + 5]), false, false);
-                        const auto hi = __builtin_amdgcn_permlane32_swap(bf16_pair(out[4 * g + 2], out[4 * g + 3]), bf16_pair(out[4 * g + 6], out[4 * g + 7]), false, false);
-                        const unsigned int x[4] = {lo[0], hi[0], lo[1], hi[1]};
-                        const int c = 8 * (g + half);
-                        if (c + 8 <= cols) {
-                            store_words<4>(to + c, x);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 7; ++e)
-                                if (c + e < cols) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(x[e >> 1] >> (16 * (e & 1))));
-                        }
-                    }
+                    for (int e = 0; e < 3; ++e)
+                        if (c + e < vcols) store_elem((T*)((unsigned char*)(o + lowest * w.o.frame) + (o_at + (unsigned)apart)) + e, out[ib][e]);
                 }
             }
         }
@@ -468,15 +498,17 @@ __global__ __launch_bounds__((Chunk<T, DK, DV, C>::THREADS)) void walk_kernel(Wa
     if (STATES) keep = st.states + ((int64_t)stretch * w.n * w.h + pair) * area;
     else if (w.s_out && stretch == last) keep = const_cast<float*>(w.s_out) + pair * area;
     if (keep && col < w.dv) {
+        int g4 = 4 * g;
+        asm("" : "+v"(g4));  // (or the places of all values are held from where the state was read)
 #pragma unroll
         for (int i = 0; i < SB; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = state_at(i, r);
-                if (row < w.dk) keep[place(row)] = state[i][r];
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * i + g4 + r;
+                if (row < w.dk) keep[corner + row * row_step] = state[i][r];
             }
     }
-    if (!STATES && w.o.p) {  // behind a video's end
+    if (!STATES && w.o.p && !w.leaves) {  // behind a video's end
         const int cols = vcols < DV ? vcols : DV, z0 = end > f0 ? end : f0;
         const int z1 = w.t - f0 < st.frames ? w.t : f0 + st.frames;
         for (int64_t i = (int64_t)z0 * DV + tid; i < (int64_t)z1 * DV; i += K::THREADS) {
@@ -494,11 +526,16 @@ __global__ __launch_bounds__(256) void stretches_kernel(Walk w, Stretches st, in
         const int end = frames_of(w, video), last = end > 0 ? (end - 1) / st.frames : 0;
         const float carry = power(st.frames, log2_of(w.log_decay[head]));
         float s = w.s_in ? w.s_in[i] : 0.0f;
-#pragma unroll 8
-        for (int j = 0; j < last; ++j) {
-            float* at = st.states + j * total + i;
-            s = carry * s + *at;
-            *at = s;
+        float* at = st.states + i;
+        for (int j = 0; j < last; j += 16) {  // sixteen on their way at once
+            float adds[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) adds[e] = j + e < last ? at[(j + e) * total] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s = carry * s + adds[e];
+                if (j + e < last) at[(j + e) * total] = s;
+            }
         }
     }
 }
@@ -514,35 +551,39 @@ hipError_t launch_steps(const Walk& w, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Padded sizes of a walk's kernel: keys of 64, 128 or 256 features; tiles of 64 columns of the state, or of 128 where those leave none empty
-// (fp32: 64, as LDS holds no more); chunks of 64 frames, for fp32 keys of more than 128 features 32, for the same reason.
+// Padded sizes of a walk's kernel: 64 or 128 keys, tiles of 64 columns of the state, or of 128 for more than 64 keys where those leave none empty
 template <typename T, typename F>
 void with_chunk(const Walk& w, F&& f) {
-    constexpr bool WIDE = sizeof(T) == 4;
-    const bool two = !WIDE && ((w.dv + 63) / 64) % 2 == 0;
-    if (w.dk <= 64) {
-        if (two) f(Chunk<T, 64, WIDE ? 64 : 128, 64>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, WIDE ? 64 : 128>{}, std::integral_constant<int, 64>{});
-        else f(Chunk<T, 64, 64, 64>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
-    } else if (w.dk <= 128) {
-        if (two) f(Chunk<T, 128, WIDE ? 64 : 128, 64>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, WIDE ? 64 : 128>{}, std::integral_constant<int, 64>{});
-        else f(Chunk<T, 128, 64, 64>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
-    } else {
-        if (two) f(Chunk<T, 256, WIDE ? 64 : 128, WIDE ? 32 : 64>{}, std::integral_constant<int, 256>{}, std::integral_constant<int, WIDE ? 64 : 128>{}, std::integral_constant<int, WIDE ? 32 : 64>{});
-        else f(Chunk<T, 256, 64, WIDE ? 32 : 64>{}, std::integral_constant<int, 256>{}, std::integral_constant<int, 64>{}, std::integral_constant<int, WIDE ? 32 : 64>{});
-    }
+    const std::integral_constant<int, 64> c64;
+    const std::integral_constant<int, 128> c128;
+    if (w.dk <= 64) f(c64, c64);
+    else if (((w.dv + 63) / 64) % 2) f(c128, c64);
+    else f(c128, c128);
 }
+// More keys than that are taken half by half: a state's rows have nothing to do with each other, and results are sums over them.
+constexpr int MOST_KEYS = 128;
 
 // A frame or two of live videos: the state is the traffic, and each of its values is used once
 bool few_frames(int t) { return t <= 2; }
+// ... and frames that lie backwards or very far apart, which the chunks' 32-bit offsets do not reach, or rows of less than 16 bytes
+bool by_steps(const rrm_decay_desc& d) {
+    if (few_frames(d.t) || d.dk < 8 || d.dv < 8) return true;
+    for (int64_t frame : {d.q_frame, d.k_frame, d.v_frame, d.o_frame})
+        if (frame < 0 || frame > (1 << 22)) return true;
+    return false;
+}
 
 // How the time axis is cut where n * h states alone would leave compute units without work.  A stretch costs what some four chunks do: its own state is written,
 // joined and read, so it has eight at least.
 Stretches stretches_of(const rrm_decay_desc& d, float* states) {
     Stretches st{1, 0x7fffff00, states};
-    if (few_frames(d.t)) return st;
+    if (by_steps(d)) {
+        st.count = 0;
+        return st;
+    }
     const int64_t groups = (int64_t)d.n * d.h;
     const int chunks = (d.t + 63) / 64, most = chunks / 8;
-    int64_t count = OP_CUS / groups;
+    int64_t count = 2 * OP_CUS / groups;
     if (count > most) count = most;
     if (count < 2) return st;
     const int per = (int)((chunks + count - 1) / count);
@@ -552,16 +593,31 @@ Stretches stretches_of(const rrm_decay_desc& d, float* states) {
 }
 
 template <typename T, bool STATES>
-hipError_t launch_chunks(const Walk& w, const Stretches& st, hipStream_t s) {
-    with_chunk<T>(w, [&](auto chunk, auto dk, auto dv, auto c) {
-        using K = decltype(chunk);
+void launch_chunk(const Walk& w, const Stretches& st, hipStream_t s) {
+    constexpr int C = 64;
+    with_chunk<T>(w, [&](auto dk, auto dv) {
+        constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
+        using K = Chunk<T, DK, DV, C>;
         const unsigned units = (unsigned)((int64_t)w.n * w.h * st.count);
-        const int64_t slices = (w.dv + decltype(dv)::value - 1) / decltype(dv)::value;
+        const int64_t slices = (w.dv + DV - 1) / DV;
         in_parts(((int64_t)units + 7) / 8 * 8 * slices, [&](unsigned first, unsigned count) {
-            hipLaunchKernelGGL((walk_kernel<T, decltype(dk)::value, decltype(dv)::value, decltype(c)::value, STATES>), dim3(count), dim3(K::THREADS), 0, s, w, st,
-                               units, first);
+            if (w.dk % K::EPC == 0 && w.dv % K::EPC == 0)
+                hipLaunchKernelGGL((walk_kernel<T, DK, DV, C, STATES, true>), dim3(count), dim3(K::THREADS), 0, s, w, st, units, first);
+            else
+                hipLaunchKernelGGL((walk_kernel<T, DK, DV, C, STATES, false>), dim3(count), dim3(K::THREADS), 0, s, w, st, units, first);
         });
     });
+}
+template <typename T, bool STATES>
+hipError_t launch_chunks(const Walk& all, const Stretches& st, hipStream_t s) {
+    const int half = all.dk <= MOST_KEYS ? all.dk : ((all.dk + 1) / 2 + 7) / 8 * 8;  // (57 to 128 keys: whole pieces)
+    for (int k = 0; k < all.dk; k += half) {
+        Walk w = all;
+        w.first_key = k, w.keys = all.dk, w.dk = all.dk - k < half ? all.dk - k : half;
+        w.q.p = (const T*)all.q.p + k, w.k.p = (const T*)all.k.p + k;
+        w.adds = k > 0, w.leaves = k + half < all.dk;
+        launch_chunk<T, STATES>(w, st, s);
+    }
     return hipGetLastError();
 }
 // What the stretches of a walk begin with
@@ -574,8 +630,12 @@ hipError_t launch_states(const Walk& w, const Stretches& st, int elem, hipStream
     return hipGetLastError();
 }
 hipError_t launch_walk(const Walk& w, const Stretches& st, int elem, hipStream_t s) {
-    if (few_frames(w.t)) return elem == RRM_F32 ? launch_steps<float>(w, s) : launch_steps<__bf16>(w, s);
+    if (st.count == 0) return elem == RRM_F32 ? launch_steps<float>(w, s) : launch_steps<__bf16>(w, s);
     return elem == RRM_F32 ? launch_chunks<float, false>(w, st, s) : launch_chunks<__bf16, false>(w, st, s);
+}
+// What a walk's first half of the keys leaves
+size_t part_bytes(const rrm_decay_desc& d, int keys, int cols) {
+    return by_steps(d) || keys <= MOST_KEYS ? 0 : round256((size_t)d.n * d.t * d.h * cols * 4);
 }
 size_t states_bytes(const rrm_decay_desc& d) {
     const Stretches st = stretches_of(d, nullptr);
@@ -584,8 +644,11 @@ size_t states_bytes(const rrm_decay_desc& d) {
 
 }  // namespace
 
-// forward: [states of the stretches]; backward: those of S, those of D
-size_t decay_scratch(const rrm_decay_desc& d, bool backward) { return states_bytes(d) * (backward ? 2 : 1); }
+// forward: [states of the stretches][part]; backward: [those of S][those of D][part]
+size_t decay_scratch(const rrm_decay_desc& d, bool backward) {
+    const size_t forward = part_bytes(d, d.dk, d.dv), back = part_bytes(d, d.dv, d.dk);
+    return states_bytes(d) * (backward ? 2 : 1) + (backward && back > forward ? back : forward);
+}
 
 hipError_t launch_decay_attention(const rrm_decay_desc& d, const void* q, const void* k, const void* v, const float* log_decay, const float* s0,
                                   const int32_t* lengths, void* o, float* s_last, void* ws, hipStream_t s) {
@@ -597,6 +660,7 @@ hipError_t launch_decay_attention(const rrm_decay_desc& d, const void* q, const 
     w.taken = 1.0f, w.given = d.scale;
     w.log_decay = log_decay, w.lengths = lengths;
     const Stretches st = stretches_of(d, (float*)ws);
+    w.part = (float*)((unsigned char*)ws + states_bytes(d));
     const hipError_t e = launch_states(w, st, d.elem, s);
     return e == hipSuccess ? launch_walk(w, st, d.elem, s) : e;
 }
@@ -608,6 +672,7 @@ hipError_t launch_decay_attention_backward(const rrm_decay_desc& d, const void* 
     const Operand odo{d_o, d.o_video, d.o_frame, d.o_head};
     Walk w{};
     w.n = d.n, w.t = d.t, w.h = d.h, w.log_decay = log_decay, w.lengths = lengths;
+    w.part = (float*)((unsigned char*)ws + 2 * states_bytes(d));
     hipError_t e = hipSuccess;
     if (dq && d.t > 0) {
         const Stretches st = stretches_of(d, (float*)ws);
