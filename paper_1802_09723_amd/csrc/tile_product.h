@@ -39,12 +39,14 @@ struct Product {
     float* part;            // [splits][rows][cols, to whole fours] (gated, halves: [splits][2][rows][..])
 };
 
-// BLEND: out = alpha * the product + beta * blend, of half-precision operands.  `blend` lies [rows][cols] in rows of whole eights.
+// BLEND: out = alpha * the product + beta * blend, of half-precision operands.  `blend` lies [rows][cols] in rows of whole eights, what its rounding left
+// off beside it where with_rest is not NULL; out's lies by out's row at out_rest.
 struct Blend {
-    const _Float16* with;  // (not read where beta is 0)
+    const _Float16 *with, *with_rest;  // (not read where beta is 0)
     int64_t row;
     float alpha, beta;
     bool to_bf16;  // out is bfloat16, else half precision like the operands
+    _Float16* out_rest;
 };
 
 enum Kind : int { GATED = 0, PLAIN = 1, HALVES = 2, BLEND = 3 };
@@ -423,21 +425,31 @@ __device__ __forceinline__ void tile_product(const Product& a, unsigned char* ld
                 leave(i, a.out3, a.out2_row, [&](int j, int e) { return acc[i][2 * j + 1][e]; });
             }
         } else if constexpr (KIND == BLEND) {
-            u32x2 d[NT][4];
             const int r = m0 + (wm * MT + i) * 32 + lr;
+            auto blended = [&](const _Float16* with) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = c0 + j * 32 + 8 * q + lc;
+                        const u32x2 d = r < a.rows && c < a.cols ? *reinterpret_cast<const u32x2*>(with + r * blend.row + c) : u32x2{0, 0};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const unsigned int pair = e & 2 ? d.y : d.x;
+                            acc[i][j][4 * q + e] += blend.beta * (float)__builtin_bit_cast(_Float16, (unsigned short)(pair >> (16 * (e & 1))));
+                        }
+                    }
+            };
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int c = c0 + j * 32 + 8 * q + lc;
-                    const bool in = blend.beta != 0.0f && r < a.rows && c < a.cols;
-                    d[j][q] = in ? *reinterpret_cast<const u32x2*>(blend.with + r * blend.row + c) : u32x2{0, 0};
-                }
-            leave(i, a.out, a.out_row, [&](int j, int e) {
-                const unsigned int pair = (e & 2) ? d[j][e >> 2].y : d[j][e >> 2].x;
-                const _Float16 v = __builtin_bit_cast(_Float16, (unsigned short)(pair >> (16 * (e & 1))));
-                return blend.alpha * acc[i][j][e] + blend.beta * (float)v;
-            });
+                for (int e = 0; e < 16; ++e) acc[i][j][e] *= blend.alpha;
+            if (blend.beta != 0.0f) {
+                if (blend.with_rest) blended(blend.with_rest);
+                blended(blend.with);
+            }
+            leave(i, a.out, a.out_row, [&](int j, int e) { return acc[i][j][e]; });
+            if (blend.out_rest) leave(i, (__bf16*)blend.out_rest, a.out_row, [&](int j, int e) { return acc[i][j][e] - (float)(_Float16)acc[i][j][e]; });
         } else {
             leave(i, half ? a.out2 : a.out, half ? a.out2_row : a.out_row, [&](int j, int e) { return acc[i][j][e]; });
         }
