@@ -17,29 +17,69 @@ namespace {
 
 constexpr int VEC = 8;  // neighbouring features of a thread
 
-// up to VEC elements, zeros behind the row's end
-template <typename T>
-__device__ __forceinline__ void load_part(const T* p, int have, float (&v)[VEC]) {
-    if (have >= VEC) {
-        load_vec<VEC>(p, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = i < have ? load_elem(p + i) : 0.0f;
+// What weights that are NULL read: the sums below then have no branch (a branch for each cost the backward pass the registers of two wavefronts)
+constexpr int MOST_COLUMNS = 16384;
+struct Ones {
+    float v[MOST_COLUMNS];
+    constexpr Ones() : v() {
+        for (float& e : v) e = 1.0f;
     }
-}
-template <typename T>
-__device__ __forceinline__ void store_part(T* p, int have, const float (&v)[VEC]) {
-    if (have >= VEC) {
-        store_vec<VEC>(p, v);
+};
+__device__ const Ones g_ones{};
+
+// How a thread's vector lies in its row.  WHOLE: rows are whole vectors.  EARLY: the last vector of a row begins early; what it has before `first` is another
+// thread's, and counts as zeros.  SHORT: rows of fewer than VEC features, element by element.
+enum Lie : int { WHOLE = 0, EARLY = 1, SHORT = 2 };
+template <int LIE>
+struct Place {
+    int at, first;  // the vector's first feature; this thread's first one of it (VEC: none)
+    __device__ __forceinline__ Place(int c, int cols) : at(c), first(c < cols ? 0 : VEC) {
+        if (LIE == EARLY && c < cols && c + VEC > cols) at = cols - VEC, first = c - at;
+        if (LIE == SHORT && c < cols) first = cols;  // (the one thread's: features 0 .. cols)
+    }
+};
+// VEC elements as they lie in memory: not converted until they are used, so that loads stay on their way; zeros where this thread has none
+template <typename T, int LIE>
+struct Raw {
+    static constexpr int WORDS = VEC * (int)sizeof(T) / 4;
+    unsigned int w[WORDS];
+    __device__ __forceinline__ void load(const T* row, const Place<LIE>& p, bool live) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
+        if (LIE == SHORT) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (live && p.first < VEC && e < p.first) {
+                    if constexpr (sizeof(T) == 4) w[e] = __float_as_uint((float)row[e]);
+                    else w[e >> 1] |= (unsigned int)__builtin_bit_cast(unsigned short, row[e]) << (16 * (e & 1));
+                }
+        } else if (live && p.first < VEC) {
+            load_words<WORDS>(row + p.at, w);
+        }
+    }
+    __device__ __forceinline__ float get(int e, const Place<LIE>& p) const {
+        float v;
+        if constexpr (sizeof(T) == 4) v = __uint_as_float(w[e]);
+        else v = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
+        return LIE == EARLY && e < p.first ? 0.0f : v;
+    }
+};
+template <typename T, int LIE>
+__device__ __forceinline__ void put(T* row, const Place<LIE>& p, bool live, const float (&v)[VEC]) {
+    if (!live || p.first >= VEC) return;
+    if (LIE == WHOLE) {
+        store_vec<VEC>(row + p.at, v);
+    } else if (LIE == EARLY) {
+        store_some<VEC>(row + p.at, v, p.first);
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (i < have) store_elem(p + i, v[i]);
+        for (int e = 0; e < VEC; ++e)
+            if (e < p.first) store_elem(row + e, v[e]);
     }
 }
 
-// Sums over the TPR threads of a row, N at once, in one order; `place`: LDS for [2][N][waves], `turn` flips between calls
-template <int TPR, int N>
+// Sums over the TPR threads of a row, N at once, in one order; `place`: LDS for [2][rows][N][wavefronts of a row], `turn` flips between calls
+template <int TPR, int N, int THREADS>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* place, int& turn) {
 #pragma unroll
     for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1)
@@ -47,10 +87,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* place, int& turn)
         for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], m);
     if constexpr (TPR > 64) {
         constexpr int WAVES = TPR / 64;
-        float* mine = place + turn * N * WAVES;
+        float* mine = place + turn * N * (THREADS / 64) + (int)threadIdx.x / TPR * N * WAVES;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) mine[k * WAVES + (threadIdx.x >> 6)] = v[k];
+            for (int k = 0; k < N; ++k) mine[k * WAVES + ((int)threadIdx.x % TPR >> 6)] = v[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -64,7 +104,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* place, int& turn)
 }
 
 // TPR threads hold a row, ITER vectors each; THREADS / TPR rows a workgroup at a time.
-template <typename X, typename B, int TPR, int ITER, int THREADS>
+template <typename X, typename B, int TPR, int ITER, int THREADS, int LIE, bool GATE>
 __global__ __launch_bounds__(THREADS) void residual_kernel(rrm_residual_desc d, const X* x, const B* b, const B* gate, const float* scale, const float* post,
                                                            const float* pre, X* r, B* u, float* stats) {
     __shared__ float place[2 * 16];
@@ -72,44 +112,47 @@ __global__ __launch_bounds__(THREADS) void residual_kernel(rrm_residual_desc d, 
     const int t = (int)threadIdx.x % TPR;
     const float inv = 1.0f / d.c;
     int turn = 0;
+    if (!scale) scale = g_ones.v;
+    if (!post) post = g_ones.v;
+    if (!pre) pre = g_ones.v;
     for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < d.m; row0 += (int64_t)gridDim.x * RPW) {
         const int64_t row = row0 + (int)threadIdx.x / TPR;
         const bool live = row < d.m;
-        float rv[ITER][VEC], bv[ITER][VEC], gv[ITER][VEC];
-        float sums[1] = {0.0f};
+        Raw<X, LIE> xw[ITER];
+        Raw<B, LIE> bw[ITER], gw[ITER];
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-            load_part(x + row * d.x_row + c, have, rv[i]);
-            if (b) load_part(b + row * d.b_row + c, have, bv[i]);
-            if (gate) load_part(gate + row * d.gate_row + c, have, gv[i]);
+            const Place<LIE> p((i * TPR + t) * VEC, d.c);
+            xw[i].load(x + row * d.x_row, p, live);
+            bw[i].load(b + row * d.b_row, p, live && b);
+            if (GATE) gw[i].load(gate + row * d.gate_row, p, live);
         }
+        float rv[ITER][VEC];
+        float sums[1] = {0.0f};
         float rb = 1.0f;
-        if (b) {
-            if (d.post_norm) {
-#pragma unroll
-                for (int i = 0; i < ITER; ++i)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) sums[0] += bv[i][e] * bv[i][e];
-                row_sums<TPR, 1>(sums, place, turn);
-                rb = 1.0f / sqrtf(sums[0] * inv + d.eps);
-            }
+        if (d.post_norm) {
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
-                const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-                float sv[VEC], pv[VEC];
-                if (scale) load_part(scale + c, have, sv);
-                if (post) load_part(post + c, have, pv);
+                const Place<LIE> p((i * TPR + t) * VEC, d.c);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float p = bv[i][e] * rb;
-                    if (post) p *= pv[e];
-                    if (gate) p *= sigmoid(gv[i][e]);
-                    if (scale) p *= sv[e];
-                    if (e < have) rv[i][e] += p;
-                }
-                if (r) store_part(r + row * d.r_row + c, have, rv[i]);
+                for (int e = 0; e < VEC; ++e) sums[0] += bw[i].get(e, p) * bw[i].get(e, p);
             }
+            row_sums<TPR, 1, THREADS>(sums, place, turn);
+            rb = 1.0f / sqrtf(sums[0] * inv + d.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const Place<LIE> p((i * TPR + t) * VEC, d.c);
+            Raw<float, LIE> sw, pw;
+            sw.load(scale, p, true);
+            pw.load(post, p, true);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float add = bw[i].get(e, p) * rb * pw.get(e, p) * sw.get(e, p);
+                if (GATE) add *= sigmoid(gw[i].get(e, p));
+                rv[i][e] = xw[i].get(e, p) + add;
+            }
+            if (r) put(r + row * d.r_row, p, live, rv[i]);
         }
         float rr = 1.0f;
         if (u) {
@@ -118,26 +161,28 @@ __global__ __launch_bounds__(THREADS) void residual_kernel(rrm_residual_desc d, 
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sums[0] += rv[i][e] * rv[i][e];
-            row_sums<TPR, 1>(sums, place, turn);
+            row_sums<TPR, 1, THREADS>(sums, place, turn);
             rr = 1.0f / sqrtf(sums[0] * inv + d.eps);
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
-                const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-                float wv[VEC];
-                if (pre) load_part(pre + c, have, wv);
+                const Place<LIE> p((i * TPR + t) * VEC, d.c);
+                Raw<float, LIE> ww;
+                ww.load(pre, p, true);
+                float out[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) wv[e] = pre ? rv[i][e] * rr * wv[e] : rv[i][e] * rr;
-                store_part(u + row * d.u_row + c, have, wv);
+                for (int e = 0; e < VEC; ++e) out[e] = rv[i][e] * rr * ww.get(e, p);
+                put(u + row * d.u_row, p, live, out);
             }
         }
         if (stats && live && t == 0) stats[2 * row] = rb, stats[2 * row + 1] = rr;
     }
 }
 
-// Sums over rows of three kinds, a workgroup's each: part [workgroup][3][c]
-template <typename X, typename B, int TPR, int ITER, int THREADS>
+// The backward pass, and sums over rows of three kinds, a workgroup's each: part [workgroup][3][c].  One reduction a row: dx is linear in mean(w rh), so
+// what db needs of dx is put together of two sums that do not wait for it.
+template <typename X, typename B, int TPR, int ITER, int THREADS, int LIE, bool GATE>
 __global__ __launch_bounds__(THREADS) void residual_back_kernel(rrm_residual_desc d, const X* dr, const B* du, const X* x, const B* b, const float* stats,
-                                                                const B* gate, const float* scale, const float* post, const float* pre, X* dx, B* db,
+                                                                const B* gate, const float* scale_, const float* post_, const float* pre_, X* dx, B* db,
                                                                 B* dgate, float* part) {
     constexpr int RPW = THREADS / TPR;
     __shared__ float place[2 * 3 * 16];
@@ -155,78 +200,76 @@ __global__ __launch_bounds__(THREADS) void residual_back_kernel(rrm_residual_des
     for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < d.m; row0 += (int64_t)gridDim.x * RPW) {
         const int64_t row = row0 + sub;
         const bool live = row < d.m;
+        // (weights are read again for each row, out of the nearest cache: held over the loop they would cost the registers of a wavefront more)
+        const float *scale = scale_ ? scale_ : g_ones.v, *post = post_ ? post_ : g_ones.v, *pre = pre_ ? pre_ : g_ones.v;
+        asm volatile("" : "+s"(scale), "+s"(post), "+s"(pre));
+        Raw<X, LIE> xw[ITER], rw[ITER];
+        Raw<B, LIE> bw[ITER], gw[ITER], uw[ITER];
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const Place<LIE> p((i * TPR + t) * VEC, d.c);
+            xw[i].load(x + row * d.x_row, p, live);
+            bw[i].load(b + row * d.b_row, p, live && b);
+            if (GATE) gw[i].load(gate + row * d.gate_row, p, live);
+            rw[i].load(dr + row * d.r_row, p, live && dr);
+            uw[i].load(du + row * d.u_row, p, live && du);
+        }
         float rb = 0.0f, rr = 0.0f;
         if (live) rb = stats[2 * row], rr = stats[2 * row + 1];
-        float xv[ITER][VEC], bv[ITER][VEC], gv[ITER][VEC], rv[ITER][VEC], uv[ITER][VEC];
-#pragma unroll
-        for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-            load_part(x + row * d.x_row + c, have, xv[i]);
-            if (b) load_part(b + row * d.b_row + c, have, bv[i]);
-            if (gate) load_part(gate + row * d.gate_row + c, have, gv[i]);
-            if (dr) load_part(dr + row * d.r_row + c, have, rv[i]);
-            if (du) load_part(du + row * d.u_row + c, have, uv[i]);
-        }
-        // sums of w rh, of (dr + rr w) times what db weighs it with, and of rr rh so weighed: dx is linear in the first's mean
+        // sums of w rh, of (dr + rr w) times what db weighs it with, and of rr rh so weighed
         float sums[3] = {0.0f, 0.0f, 0.0f};
+        float rh[ITER][VEC], first[ITER][VEC];
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-            float sv[VEC], pv[VEC], wv[VEC];
-            if (scale) load_part(scale + c, have, sv);
-            if (post) load_part(post + c, have, pv);
-            if (pre) load_part(pre + c, have, wv);
+            const Place<LIE> p((i * TPR + t) * VEC, d.c);
+            Raw<float, LIE> sw, pw, ww;
+            sw.load(scale, p, true);
+            pw.load(post, p, true);
+            ww.load(pre, p, true);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float bh = b ? bv[i][e] * rb : 0.0f;
-                const float p = post ? bh * pv[e] : bh;
-                const float sg = gate ? sigmoid(gv[i][e]) : 1.0f;
-                const float q = scale ? sv[e] * sg : sg;
-                const float rh = b ? (xv[i][e] + q * p) * rr : xv[i][e] * rr;
-                const float w = !du ? 0.0f : pre ? uv[i][e] * wv[e] : uv[i][e];
-                const float first = (dr ? rv[i][e] : 0.0f) + rr * w;
-                xv[i][e] = rh;
-                rv[i][e] = first;
-                sums[0] += w * rh;
-                sums[1] += first * q * p;
-                sums[2] += rr * rh * q * p;
-                if (du) cs[2][i][e] += uv[i][e] * rh;
+                float weighed = bw[i].get(e, p) * rb * pw.get(e, p) * sw.get(e, p);  // q p
+                if (GATE) weighed *= sigmoid(gw[i].get(e, p));
+                rh[i][e] = (xw[i].get(e, p) + weighed) * rr;
+                const float ue = uw[i].get(e, p), w = ue * ww.get(e, p);
+                first[i][e] = rw[i].get(e, p) + rr * w;
+                sums[0] += w * rh[i][e];
+                sums[1] += first[i][e] * weighed;
+                sums[2] += rh[i][e] * weighed;
+                cs[2][i][e] += ue * rh[i][e];
             }
         }
-        row_sums<TPR, 3>(sums, place, turn);
-        const float m1 = sums[0] * inv, m2 = (sums[1] - m1 * sums[2]) * inv;
+        row_sums<TPR, 3, THREADS>(sums, place, turn);
+        const float m1 = sums[0] * inv * rr, m2 = d.post_norm ? (sums[1] - m1 * sums[2]) * inv : 0.0f;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TPR + t) * VEC, have = live ? d.c - c : 0;
-            float sv[VEC], pv[VEC];
-            if (scale) load_part(scale + c, have, sv);
-            if (post) load_part(post + c, have, pv);
+            const Place<LIE> p((i * TPR + t) * VEC, d.c);
+            Raw<float, LIE> sw, pw;
+            sw.load(scale, p, true);
+            pw.load(post, p, true);
             float out[VEC], og[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float dxe = rv[i][e] - rr * xv[i][e] * m1;
-                rv[i][e] = dxe;
-                if (!b) continue;
-                const float bh = bv[i][e] * rb;
-                const float p = post ? bh * pv[e] : bh;
+                const float dxe = first[i][e] - rh[i][e] * m1;
+                first[i][e] = dxe;
+                const float bh = bw[i].get(e, p) * rb, pv = pw.get(e, p);
                 float sg = 1.0f, rest = 0.0f;
-                if (gate) gate_pair(gv[i][e], sg, rest);
-                const float q = scale ? sv[e] * sg : sg;
-                const float dp = dxe * q;
-                cs[0][i][e] += dxe * sg * p;
+                if (GATE) gate_pair(gw[i].get(e, p), sg, rest);
+                const float gated = dxe * sg, dp = gated * sw.get(e, p);
+                cs[0][i][e] += gated * (bh * pv);
                 cs[1][i][e] += dp * bh;
-                og[e] = dp * p * rest;
-                const float weighed = post ? dp * pv[e] : dp;
-                out[e] = d.post_norm ? rb * (weighed - bh * m2) : weighed;
+                if (GATE) og[e] = dp * (bh * pv) * rest;
+                out[e] = rb * (dp * pv - bh * m2);
             }
-            if (dx) store_part(dx + row * d.dx_row + c, have, rv[i]);
-            if (db) store_part(db + row * d.db_row + c, have, out);
-            if (dgate) store_part(dgate + row * d.dgate_row + c, have, og);
+            if (dx) put(dx + row * d.dx_row, p, live, first[i]);
+            if (db) put(db + row * d.db_row, p, live, out);
+            if (GATE && dgate) put(dgate + row * d.dgate_row, p, live, og);
         }
     }
     if (!part) return;
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
+        float* to = part + ((int64_t)blockIdx.x * 3 + k) * d.c;
         if constexpr (RPW > 1) {  // the workgroup's rows, in their order
             __syncthreads();
 #pragma unroll
@@ -234,17 +277,16 @@ __global__ __launch_bounds__(THREADS) void residual_back_kernel(rrm_residual_des
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) columns[(sub * ITER * TPR + i * TPR + t) * VEC + e] = cs[k][i][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < TPR * ITER * VEC; c += THREADS) {
+            for (int v = threadIdx.x; v < TPR * ITER * VEC; v += THREADS) {
+                const Place<LIE> p(v / VEC * VEC, d.c);
                 float s = 0.0f;
-                for (int j = 0; j < RPW; ++j) s += columns[j * TPR * ITER * VEC + c];
-                if (c < d.c) part[((int64_t)blockIdx.x * 3 + k) * d.c + c] = s;
+                for (int j = 0; j < RPW; ++j) s += columns[j * TPR * ITER * VEC + v];
+                const int e = v % VEC;
+                if (LIE == SHORT ? p.first < VEC && e < p.first : e >= p.first) to[p.at + e] = s;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < ITER; ++i) {
-                const int c = (i * TPR + t) * VEC;
-                store_part(part + ((int64_t)blockIdx.x * 3 + k) * d.c + c, d.c - c, cs[k][i]);
-            }
+            for (int i = 0; i < ITER; ++i) put(to, Place<LIE>((i * TPR + t) * VEC, d.c), true, cs[k][i]);
         }
     }
 }
@@ -258,7 +300,13 @@ __global__ __launch_bounds__(1024) void residual_columns_kernel(const float* par
     const int col = (int)blockIdx.x * 64 + lane;
     float s = 0.0f;
     if (col < c)
-        for (int g = slot; g < groups; g += 16) s += part[((int64_t)g * 3 + kind) * c + col];
+        for (int g = slot; g < groups; g += 128) {  // eight on their way at once
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = g + 16 * i < groups ? part[((int64_t)(g + 16 * i) * 3 + kind) * c + col] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
     sums[slot][lane] = s;
     __syncthreads();
     if (slot == 0 && col < c) {
@@ -272,16 +320,22 @@ template <int T, int I, int TH>
 struct Form {
     static constexpr int TPR = T, ITER = I, THREADS = TH;
 };
-// The fewest threads that hold a row in two vectors each at the most, by whole wavefronts where a row has more than 16 vectors
+// The fewest threads that hold a row, a vector each (two beyond 8192 features)
 template <typename F>
 void with_form(int c, F&& f) {
     if (c <= 128) f(Form<16, 1, 256>{});
     else if (c <= 512) f(Form<64, 1, 256>{});
-    else if (c <= 1024) f(Form<64, 2, 256>{});
+    else if (c <= 1024) f(Form<128, 1, 256>{});
     else if (c <= 2048) f(Form<256, 1, 256>{});
-    else if (c <= 4096) f(Form<256, 2, 256>{});
+    else if (c <= 4096) f(Form<512, 1, 512>{});
     else if (c <= 8192) f(Form<1024, 1, 1024>{});
     else f(Form<1024, 2, 1024>{});
+}
+template <typename F, typename G>
+void with_lie(int c, F, G&& g) {
+    if (c % VEC == 0) g(std::integral_constant<int, WHOLE>{});
+    else if (c > VEC) g(std::integral_constant<int, EARLY>{});
+    else if constexpr (F::TPR == 16) g(std::integral_constant<int, SHORT>{});
 }
 template <typename F>
 void with_types(const rrm_residual_desc& d, F&& f) {
@@ -291,11 +345,12 @@ void with_types(const rrm_residual_desc& d, F&& f) {
     else f((__bf16)0.0f, (__bf16)0.0f);
 }
 
-constexpr int FORWARD_GROUPS = 2048, BACK_GROUPS = 512;
-int groups_of(const rrm_residual_desc& d, int most) {
+// Workgroups of a pass: as many as run at once, of the backward pass, each of which leaves sums to be joined
+int groups_of(const rrm_residual_desc& d, bool backward) {
     int groups = 0;
     with_form(d.c, [&](auto form) {
         constexpr int RPW = decltype(form)::THREADS / decltype(form)::TPR;
+        const int most = !backward ? 2048 : decltype(form)::THREADS > 256 ? OP_CUS : 3 * OP_CUS;
         const int all = (int)(((int64_t)d.m + RPW - 1) / RPW);
         groups = all < most ? all : most;
     });
@@ -304,7 +359,7 @@ int groups_of(const rrm_residual_desc& d, int most) {
 
 }  // namespace
 
-size_t residual_scratch(const rrm_residual_desc& d) { return round256((size_t)groups_of(d, BACK_GROUPS) * 3 * d.c * sizeof(float)); }
+size_t residual_scratch(const rrm_residual_desc& d) { return round256((size_t)groups_of(d, true) * 3 * d.c * sizeof(float)); }
 
 hipError_t launch_residual_norm(const rrm_residual_desc& d, const void* x, const void* b, const void* gate, const float* scale, const float* post,
                                 const float* pre, void* r, void* u, float* stats, hipStream_t s) {
@@ -313,8 +368,14 @@ hipError_t launch_residual_norm(const rrm_residual_desc& d, const void* x, const
         using B = decltype(bt);
         with_form(d.c, [&](auto form) {
             using F = decltype(form);
-            hipLaunchKernelGGL((residual_kernel<X, B, F::TPR, F::ITER, F::THREADS>), dim3((unsigned)groups_of(d, FORWARD_GROUPS)), dim3(F::THREADS), 0, s, d,
-                               (const X*)x, (const B*)b, (const B*)gate, scale, post, pre, (X*)r, (B*)u, stats);
+            with_lie(d.c, form, [&](auto lie) {
+                auto launch = [&](auto gated) {
+                    hipLaunchKernelGGL((residual_kernel<X, B, F::TPR, F::ITER, F::THREADS, decltype(lie)::value, decltype(gated)::value>),
+                                       dim3((unsigned)groups_of(d, false)), dim3(F::THREADS), 0, s, d, (const X*)x, (const B*)b, (const B*)gate, scale,
+                                       post, pre, (X*)r, (B*)u, stats);
+                };
+                gate ? launch(std::true_type{}) : launch(std::false_type{});
+            });
         });
     });
     return hipGetLastError();
@@ -325,7 +386,7 @@ hipError_t launch_residual_norm_backward(const rrm_residual_desc& d, const void*
                                          void* dx, void* db, void* dgate, float* dscale, float* dpost, float* dpre, void* ws, hipStream_t s) {
     const bool sums = dscale || dpost || dpre;
     float* part = sums && d.m > 0 ? (float*)ws : nullptr;
-    const int groups = d.m > 0 ? groups_of(d, BACK_GROUPS) : 0;
+    const int groups = d.m > 0 ? groups_of(d, true) : 0;
     hipError_t e = hipSuccess;
     if (d.m > 0) {
         with_types(d, [&](auto xt, auto bt) {
@@ -333,9 +394,14 @@ hipError_t launch_residual_norm_backward(const rrm_residual_desc& d, const void*
             using B = decltype(bt);
             with_form(d.c, [&](auto form) {
                 using F = decltype(form);
-                hipLaunchKernelGGL((residual_back_kernel<X, B, F::TPR, F::ITER, F::THREADS>), dim3((unsigned)groups), dim3(F::THREADS), 0, s, d,
-                                   (const X*)dr, (const B*)du, (const X*)x, (const B*)b, stats, (const B*)gate, scale, post, pre, (X*)dx, (B*)db, (B*)dgate,
-                                   part);
+                with_lie(d.c, form, [&](auto lie) {
+                    auto launch = [&](auto gated) {
+                        hipLaunchKernelGGL((residual_back_kernel<X, B, F::TPR, F::ITER, F::THREADS, decltype(lie)::value, decltype(gated)::value>),
+                                           dim3((unsigned)groups), dim3(F::THREADS), 0, s, d, (const X*)dr, (const B*)du, (const X*)x, (const B*)b, stats,
+                                           (const B*)gate, scale, post, pre, (X*)dx, (B*)db, (B*)dgate, part);
+                    };
+                    gate ? launch(std::true_type{}) : launch(std::false_type{});
+                });
             });
         });
         if ((e = hipGetLastError()) != hipSuccess) return e;
