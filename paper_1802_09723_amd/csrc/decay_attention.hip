@@ -573,8 +573,8 @@ bool by_steps(const rrm_decay_desc& d) {
     return false;
 }
 
-// How the time axis is cut where n * h states alone would leave compute units without work.  A stretch costs what some four chunks do: its own state is written,
-// joined and read, so it has eight at least.
+// How the time axis is cut where n * h states alone would leave compute units without work.  A stretch costs its own state, written, joined and read, and two launches:
+// some four chunks of bf16, one of fp32 (whose products take ten times as long), so it has eight, or three, at least.
 Stretches stretches_of(const rrm_decay_desc& d, float* states) {
     Stretches st{1, 0x7fffff00, states};
     if (by_steps(d)) {
@@ -582,7 +582,7 @@ Stretches stretches_of(const rrm_decay_desc& d, float* states) {
         return st;
     }
     const int64_t groups = (int64_t)d.n * d.h;
-    const int chunks = (d.t + 63) / 64, most = chunks / 8;
+    const int chunks = (d.t + 63) / 64, most = chunks / (d.elem == RRM_F32 ? 3 : 8);
     int64_t count = 2 * OP_CUS / groups;
     if (count > most) count = most;
     if (count < 2) return st;
