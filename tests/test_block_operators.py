@@ -649,3 +649,421 @@ def test_orthogonalize_matrices_strides_and_nothing():
     ok = torch.isfinite(got.float()).view(6, -1).all(-1).tolist()
     assert ok == [True, True, False, True, True, True]
     assert torch.equal(got[3], every.view(6, 40, 56)[3])
+
+
+# -- together, on streams and in graphs ------------------------------------------------------------------------------------
+
+def chain_inputs(n=3, t=150, h=2, d=32, seed=0):
+    g = gen(seed)
+    c = h * d
+    x = {k: torch.randn(n, t, c, generator=g).bfloat16().cuda() for k in ("q", "k", "v", "gate")}
+    x["x"] = torch.randn(n, t, c, generator=g).cuda()
+    x["w"] = [torch.rand(c, generator=g).cuda() + 0.5 for _ in range(3)]
+    x["s0"] = torch.randn(n, h, d, d, generator=g).cuda()
+    x["ld"] = decays(h).cuda()
+    x["du"] = torch.randn(n, t, c, generator=g).bfloat16().cuda()
+    x["g"] = torch.randn(2, 40, 100, generator=g).cuda()
+    return x
+
+
+def chain(x, stream=None):
+    """Forward and backward of a part of a block, and an update"""
+    n, t, c = x["q"].shape
+    h = x["ld"].shape[0]
+    heads = [x[k].view(n, t, h, c // h) for k in ("q", "k", "v")]
+    o, s = rrm.decay_attention(*heads, x["ld"], s0=x["s0"], stream=stream)
+    stats = torch.empty(n, t, 2, device="cuda")
+    r, u = rrm.residual_norm(x["x"], o.view(n, t, c), x["gate"], *x["w"], stats=stats, stream=stream)
+    grads = rrm.residual_norm_backward(r, x["du"], x["x"], o.view(n, t, c), stats, x["gate"], *x["w"], stream=stream)
+    back = rrm.decay_attention_backward(grads[1].view(n, t, h, c // h), *heads, x["ld"], s0=x["s0"], ds_last=s, stream=stream)
+    return (o, s, r, u, *grads, *back, rrm.orthogonalize(x["g"], stream=stream))
+
+
+@gpu
+def test_block_on_a_stream_of_its_own_and_in_a_graph():
+    """Another stream than the current one, by object and by handle; two at once; a captured chain replayed over changing inputs, with eager calls between."""
+    x = chain_inputs()
+    want = [v.clone() for v in chain(x)]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in (sides[0], sides[0].cuda_stream):
+        got = chain(x, s)
+        sides[0].synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    other = chain_inputs(seed=1)
+    want2 = [v.clone() for v in chain(other)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        one, two = chain(x, sides[0]), chain(other, sides[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(one, want)) and all(torch.equal(a, b) for a, b in zip(two, want2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = chain(x)
+    for k in range(4):
+        for name in ("q", "x", "du", "g"):
+            x[name].copy_(torch.randn(x[name].shape, generator=gen(10 + k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in held]
+        want = chain(x)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+def test_long_attention_on_two_streams_and_in_graphs_that_share_memory():
+    """Stretches hand their states on through the workspace: calls at once have their own, captured ones replayed in turn give what eager ones give."""
+    x = [{k: torch.randn(1, 3000, 1, 64, generator=gen(i)).bfloat16().cuda() for k in "qkv"} for i in range(2)]
+    ld = torch.tensor([-0.01], device="cuda")
+
+    def call(i, stream=None):
+        return rrm.decay_attention(x[i]["q"], x[i]["k"], x[i]["v"], ld, stream=stream)
+
+    want = [[v.clone() for v in call(i)] for i in range(2)]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = [call(i, sides[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    pool = torch.cuda.graph_pool_handle()
+    graphs, held = [], []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], pool=pool):
+            held.append([v.clone() for v in call(i)])
+    for _ in range(3):
+        for i in range(2):
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(held[i][0], want[i][0]) and torch.equal(held[i][1], want[i][1])
+
+
+@gpu
+def test_calls_give_the_same_bits_every_time():
+    x = chain_inputs(2, 300, 3, 40)
+    want = [v.clone() for v in chain(x)]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(chain(x), want))
+
+
+@gpu
+def test_attention_offsets_beyond_32_bits():
+    """Frames four gigabytes and more apart from the first, and frames so far apart that a chunk's offsets need more than 32 bits."""
+    t, h, d = 70000, 1, 16
+    stride = 40000  # elements between frames: 2.8e9 in all
+    room = torch.empty(t * stride, dtype=torch.bfloat16, device="cuda")
+    q = room.as_strided((1, t, h, d), (t * stride, stride, d, 1))
+    small = torch.randn(1, t, h, d, generator=gen(1)).bfloat16().cuda()
+    q.copy_(small)
+    ld = torch.tensor([-0.02], device="cuda")
+    k, v = (torch.randn(1, t, h, d, generator=gen(i)).bfloat16().cuda() for i in (2, 3))
+    out = room.as_strided((1, t, h, d), (t * stride, stride, d, 1), 64)
+    got, s = rrm.decay_attention(q, k, v, ld, out=out)
+    want, s2 = rrm.decay_attention(small, k, v, ld)
+    assert torch.equal(got, want) and torch.equal(s, s2)
+    t2, far = 300, 1 << 23
+    q = room.as_strided((1, t2, h, d), (t2 * far, far, d, 1))
+    q.copy_(small[:, :t2])
+    got, s = rrm.decay_attention(q, k[:, :t2], v[:, :t2], ld)
+    want, s2 = rrm.decay_attention(small[:, :t2], k[:, :t2], v[:, :t2], ld)
+    # (frame by frame, where the other call takes chunks)
+    a = [z[:, :t2].double() for z in (small, k, v)]
+    so, ss = attend_slack(*a, ld, d ** -0.5, torch.zeros(1, h, d, d, dtype=F64, device="cuda"), [t2], False, "bf16")
+    check(got, want.double(), 2 * so + V * want.double().abs(), "o")
+    check(s, s2.double(), 2 * ss, "s_last")
+
+
+@gpu
+def test_residual_offsets_beyond_32_bits():
+    m, c, stride = 70000, 24, 40000
+    room = torch.empty(m * stride, dtype=torch.bfloat16, device="cuda")
+    b = room.as_strided((m, c), (stride, 1))
+    small = torch.randn(m, c, generator=gen(1)).bfloat16().cuda()
+    b.copy_(small)
+    x = torch.randn(m, c, generator=gen(2)).cuda()
+    w = torch.rand(c, device="cuda") + 0.5
+    u = room.as_strided((m, c), (stride, 1), 100)
+    r, _ = rrm.residual_norm(x, b, None, None, w, w, u=u)
+    r2, u2 = rrm.residual_norm(x, small, None, None, w, w)
+    assert torch.equal(r, r2) and torch.equal(u, u2)
+
+
+# -- the example ---------------------------------------------------------------------------------------------------------------
+
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "video_block.py")
+    spec = importlib.util.spec_from_file_location("video_block", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@gpu
+def test_the_example_serves_what_it_trains():
+    """Live frames against the clip (attention in steps and in chunks), and every gradient against autograd in 64 bits on the same weights.
+
+    Between the operators values are bfloat16: some twenty roundings lie on the longest way, each off by at most v and, as their errors are independent, by v / 2 in
+    the root mean square of one; sqrt(20) v / 2 = 0.009, and three times that is allowed in the norm."""
+    ex = example()
+    block = ex.Block(c=64, h=2, d=32, f=96)
+    n, t, c = 3, 80, 64
+    x = torch.randn(n, t, c, generator=gen(1)).cuda()
+    dy = torch.randn(n, t, c, generator=gen(2)).bfloat16().cuda()
+    y, _ = block.clip(x)
+    state = block.state(n)
+    for j in range(t):
+        live = block.frame(x[:, j].contiguous(), state)
+        assert float((live.float() - y[:, j].float()).norm()) <= 0.027 * float(y[:, j].float().norm())
+    lengths = torch.tensor([t, 33, 0], dtype=torch.int32, device="cuda")
+    y, kept = block.clip(x, lengths)
+    grads = block.gradients(dy, kept)
+    names = [k for k in grads if k != "x"]
+    p = {k: getattr(block, k).detach().double().cpu().requires_grad_() for k in names}
+    x64 = x.double().cpu().requires_grad_()
+    norm = lambda z, w: z / torch.sqrt((z * z).mean(-1, keepdim=True) + ex.EPS) * w  # noqa: E731
+    u = norm(x64, p["before"])
+    q, k, v = ((u @ p[w].t()).view(n, t, 2, 32) for w in ("wq", "wk", "wv"))
+    o, _ = attend64(q, k, v, block.log_decay.cpu(), 32 ** -0.5, torch.zeros(n, 2, 32, 32, dtype=F64), lengths.tolist())
+    r, u1 = residual64(x64, o.flatten(2) @ p["wo"].t(), u @ p["wz"].t(), p["scale1"], p["post1"], p["pre1"], ex.EPS)
+    g = u1 @ p["wg"].t()
+    hidden = g * torch.sigmoid(g) * (u1 @ p["wu"].t())
+    _, want = residual64(r, hidden @ p["wd"].t(), None, p["scale2"], p["post2"], p["pre2"], ex.EPS)
+    assert float((y.cpu().double() - want.detach()).norm()) <= 0.027 * float(want.detach().norm())
+    wants = torch.autograd.grad(want, [x64] + list(p.values()), dy.cpu().double())
+    for name, w in zip(["x"] + names, wants):
+        err = float((grads[name].cpu().double() - w).norm())
+        assert err <= 0.027 * float(w.norm()), f"{name}: {err / float(w.norm())}"
+    before = block.wg.clone()
+    ex.update(block, grads, {})
+    assert torch.isfinite(block.wg.float()).all() and not torch.equal(before, block.wg)
+    losses, off = ex.main()
+    assert len(losses) == 20 and off <= 0.027
+
+
+# -- refusals ------------------------------------------------------------------------------------------------------------------
+
+def test_descriptors_of_the_block_operators_match_the_header():
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "rrm.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    kinds = {"int": ctypes.c_int, "float": ctypes.c_float, "int64_t": ctypes.c_int64}
+    for name, cls in (("rrm_decay_desc", ops.DecayDesc), ("rrm_residual_desc", ops.ResidualDesc), ("rrm_orth_desc", ops.OrthDesc)):
+        body = re.search(r"typedef struct \{([^}]*)\}\s*%s;" % name, text, flags=re.S).group(1)
+        fields = [(f.strip(), kinds[kind]) for kind, names in re.findall(r"\b(int64_t|int|float)\s+([a-z_0-9, \n]+);", body) for f in names.split(",")]
+        assert fields == list(cls._fields_), name
+
+
+def decay_desc(**kw):
+    v = dict(n=2, t=5, h=3, dk=4, dv=6, elem=0, scale=1.0)
+    for x, f in (("q", 4), ("k", 4), ("v", 6), ("o", 6), ("dq", 4), ("dk", 4), ("dv", 6)):
+        v.update({f"{x}_video": 15 * f, f"{x}_frame": 3 * f, f"{x}_head": f})
+    v.update(kw)
+    return ops.DecayDesc(**v)
+
+
+def residual_desc(**kw):
+    v = dict(m=3, c=8, x_elem=0, b_elem=1, post_norm=1, eps=1e-6, **{f"{x}_row": 8 for x in ("x", "b", "gate", "r", "u", "dx", "db", "dgate")})
+    v.update(kw)
+    return ops.ResidualDesc(**v)
+
+
+def orth_desc(**kw):
+    v = dict(n=2, rows=4, cols=6, elem=0, steps=5, a=3.0, b=-4.0, c=2.0, eps=1e-7, g_matrix=24, g_row=6, x_matrix=24, x_row=6)
+    v.update(kw)
+    return ops.OrthDesc(**v)
+
+
+def test_refusals_come_back_as_status_codes():
+    """No call below reaches the device: pointers are made up."""
+    L = rrm.lib()
+    P, big = 1 << 20, 1 << 40
+    ref = ctypes.byref
+
+    def decay(q=P, k=P, v=P, ld=P, s0=None, lengths=None, o=P, last=None, ws=P, have=big, **kw):
+        return L.rrm_decay_attention(ref(decay_desc(**kw)), q, k, v, ld, s0, lengths, o, last, ws, have, None)
+
+    assert L.rrm_decay_attention(None, P, P, P, P, None, None, P, None, P, big, None) == -1
+    assert decay(q=None) == -1 and decay(k=None) == -1 and decay(v=None) == -1 and decay(ld=None) == -1 and decay(o=None) == -1
+    assert decay(n=-1) == -2 and decay(t=-1) == -2 and decay(h=-1) == -2 and decay(dk=0) == -2 and decay(dv=0) == -2
+    assert decay(dk=257) == -2 and decay(dv=257) == -2 and decay(t=0x7fffffff) == -2 and decay(n=1 << 16, h=1 << 13) == -2
+    assert decay(elem=2) == -3 and decay(scale=math.nan) == -8 and decay(scale=math.inf) == -8
+    assert decay(o_head=5) == -2 and decay(o_frame=0) == -2 and decay(o_video=18) == -2 and decay(o_frame=-18) == -2
+    assert decay(q_video=1 << 62) == -2 and decay(k_head=-(1 << 63)) == -2
+    assert decay(q=P + 2) == -9 and decay(q=P + 1, elem=1) == -9 and decay(s0=P + 2) == -9 and decay(lengths=P + 1) == -9 and decay(ld=P + 2) == -9
+    assert decay(s0=P, last=P) == -6
+    assert decay(n=0) == 0 and decay(h=0) == 0 and decay(t=0) == 0
+    long = dict(n=1, t=20000, h=1, dk=64, dv=64)
+    need = L.rrm_decay_attention_workspace(ref(decay_desc(**long)), 0)
+    assert need > 0 and L.rrm_decay_attention_workspace(ref(decay_desc(**long)), 1) == 2 * need
+    fits = {f"{x}_{a}": s for x in ("q", "k", "v", "o") for a, s in (("video", 20000 * 64), ("frame", 64), ("head", 64))}
+    assert decay(ws=None, **long, **fits) == -1 and decay(ws=P + 16, **long, **fits) == -9 and decay(have=need - 1, **long, **fits) == -10
+    assert L.rrm_decay_attention_workspace(ref(decay_desc(dk=0)), 0) == 0
+
+    def decay_back(do=P, last=None, dq=P, dk_=P, dv_=P, ds0=P, q=P, **kw):
+        return L.rrm_decay_attention_backward(ref(decay_desc(**kw)), q, P, P, P, None, None, do, last, dq, dk_, dv_, ds0, P, big, None)
+
+    assert decay_back(do=None) == -1 and decay_back(q=None) == -1 and decay_back(dq_head=3) == -2 and decay_back(dv_video=17) == -2
+    assert decay_back(dk_=P + 2) == -9 and decay_back(last=P + 1) == -9 and decay_back(last=P, ds0=P) == -6
+    assert decay_back(dq=None, dk_=None, dv_=None, ds0=None) == 0
+
+    def norm(x=P, b=P, gate=None, scale=None, post=None, pre=None, r=P, u=P, stats=None, **kw):
+        return L.rrm_residual_norm(ref(residual_desc(**kw)), x, b, gate, scale, post, pre, r, u, stats, None)
+
+    assert L.rrm_residual_norm(None, P, P, None, None, None, None, P, P, None, None) == -1
+    assert norm(x=None) == -1 and norm(r=None, u=None) == -1 and norm(b=None) == -1 and norm(b=None, post_norm=0) == -1
+    assert norm(b=None, r=None, post_norm=0, gate=P) == -1 and norm(post=P, post_norm=0) == -8
+    assert norm(m=-1) == -2 and norm(c=0) == -2 and norm(c=16385) == -2 and norm(r_row=7) == -2 and norm(u_row=0) == -2 and norm(x_row=1 << 62) == -2
+    assert norm(x_elem=2) == -3 and norm(b_elem=-1) == -3 and norm(eps=0.0) == -8 and norm(eps=math.nan) == -8
+    assert norm(x=P + 2) == -9 and norm(b=P + 1) == -9 and norm(scale=P + 2) == -9 and norm(stats=P + 1) == -9
+    assert norm(r=P, x_row=16) == -6 and norm(m=0) == 0
+
+    def norm_back(dr=P, du=P, x=P, b=P, stats=P, gate=None, post=None, dx=P, dgate=None, dscale=P, dpost=P, ws=P, have=big, **kw):
+        return L.rrm_residual_norm_backward(ref(residual_desc(**kw)), dr, du, x, b, stats, gate, None, post, None, dx, P, dgate, dscale, dpost, P, ws, have, None)
+
+    need = L.rrm_residual_norm_workspace(ref(residual_desc()))
+    assert need > 0
+    assert norm_back(x=None) == -1 and norm_back(stats=None) == -1 and norm_back(b=None) == -1 and norm_back(dgate=P) == -1
+    assert norm_back(post_norm=0) == -8 and norm_back(dx_row=7) == -2 and norm_back(db_row=3) == -2
+    assert norm_back(ws=None) == -1 and norm_back(ws=P + 8) == -9 and norm_back(have=need - 1) == -10 and norm_back(dscale=P + 2) == -9
+
+    def orth(g=P, x=P, ws=P, have=big, **kw):
+        return L.rrm_orthogonalize(ref(orth_desc(**kw)), g, x, ws, have, None)
+
+    need = L.rrm_orthogonalize_workspace(ref(orth_desc()))
+    assert need > 0
+    assert L.rrm_orthogonalize(None, P, P, P, big, None) == -1 and orth(g=None) == -1 and orth(x=None) == -1 and orth(ws=None) == -1
+    assert orth(n=-1) == -2 and orth(n=65536) == -2 and orth(rows=0) == -2 and orth(cols=65537) == -2 and orth(n=60000, rows=60000, cols=60000) == -2
+    assert orth(elem=3) == -3 and orth(steps=0) == -8 and orth(steps=101) == -8 and orth(a=math.nan) == -8 and orth(eps=-1.0) == -8 and orth(c=math.inf) == -8
+    assert orth(x_row=5) == -2 and orth(x_matrix=20) == -2 and orth(g_row=1 << 62) == -2
+    assert orth(g=P + 2) == -9 and orth(x=P + 1) == -9 and orth(ws=P + 128) == -9 and orth(have=need - 1) == -10 and orth(n=0) == 0
+
+
+def test_the_binding_refuses_what_the_calls_cannot_take():
+    x = torch.zeros(2, 3, 4, 8)
+    ld = torch.zeros(4)
+    for call in (lambda: rrm.decay_attention(x, x, x, ld), lambda: rrm.decay_attention_backward(x, x, x, x, ld), lambda: rrm.residual_norm(x, x),
+                 lambda: rrm.residual_norm_backward(x, None, x, x, x[..., :2]), lambda: rrm.orthogonalize(x)):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
+    with pytest.raises(ValueError, match="expected \\[n, t, h, features\\]"):
+        rrm.decay_attention(x[0], x[0], x[0], ld)
+    with pytest.raises(ValueError, match="without b"):
+        rrm.residual_norm(x, gate=x, pre=ld)
+    with pytest.raises(ValueError, match="one of them"):
+        rrm.residual_norm(x)
+    with pytest.raises(ValueError, match="without pre"):
+        rrm.residual_norm_backward(None, x, x, x, x[..., :2])
+    with pytest.raises(ValueError, match="no such input"):
+        rrm.residual_norm_backward(x, None, x, x, x[..., :2], dgate=x)
+
+
+@gpu
+def test_the_binding_refuses_wrong_tensors():
+    x = torch.zeros(2, 3, 4, 8, device="cuda")
+    ld, w = torch.zeros(4, device="cuda"), torch.ones(8, device="cuda")
+    for bad in (lambda: rrm.decay_attention(x, x, x[:, :2], ld), lambda: rrm.decay_attention(x, x.bfloat16(), x, ld), lambda: rrm.decay_attention(x, x, x, ld[:3]),
+                lambda: rrm.decay_attention(x, x, x, ld.double()), lambda: rrm.decay_attention(x.half(), x.half(), x.half(), ld),
+                lambda: rrm.decay_attention(x.transpose(2, 3), x.transpose(2, 3), x.transpose(2, 3), torch.zeros(8, device="cuda")),
+                lambda: rrm.decay_attention(x, x, x, ld, s0=torch.zeros(2, 4, 8, 7, device="cuda")),
+                lambda: rrm.decay_attention(x, x, x, ld, lengths=torch.zeros(2, device="cuda", dtype=torch.int64)),
+                lambda: rrm.decay_attention(x, x, x, ld.clone().requires_grad_()),
+                lambda: rrm.residual_norm(x, x[..., :4]), lambda: rrm.residual_norm(x, x, x.bfloat16()), lambda: rrm.residual_norm(x, x, pre=w[:4]),
+                lambda: rrm.residual_norm(x, x, pre=w, stats=torch.zeros(2, 3, 2, device="cuda")), lambda: rrm.residual_norm(x, x, pre=w, u=x.bfloat16()),
+                lambda: rrm.residual_norm(x, x[:, :, :3].expand(2, 3, 3, 8)), lambda: rrm.orthogonalize(x.half()), lambda: rrm.orthogonalize(ld),
+                lambda: rrm.orthogonalize(x, out=x), lambda: rrm.orthogonalize(x[..., :0]), lambda: rrm.orthogonalize(x.transpose(-1, -2))):
+        with pytest.raises(ValueError):
+            bad()
+    wide = torch.zeros(1, 1, 1, 300, device="cuda")
+    for bad in (lambda: rrm.decay_attention(wide, wide, x[:1, :1, :1], ld[:1]), lambda: rrm.orthogonalize(x, steps=0), lambda: rrm.residual_norm(x, x, eps=0.0),
+                lambda: rrm.residual_norm(torch.zeros(1, 20000, device="cuda"), pre=torch.ones(20000, device="cuda"))):
+        with pytest.raises(RRMError):
+            bad()
+
+
+BF = torch.bfloat16
+CALLS = {
+    "decay": (lambda t, **kw: rrm.decay_attention(t[0], t[1], t[2], t[3], s0=t[4], **kw), [(2, 70, 2, 8)] * 3 + [(2,), (2, 2, 8, 8)]),
+    "decay_back": (lambda t, **kw: rrm.decay_attention_backward(t[0], t[1], t[2], t[3], t[4], s0=t[5], ds_last=t[6], **kw),
+                   [(2, 70, 2, 8)] * 4 + [(2,), (2, 2, 8, 8), (2, 2, 8, 8)]),
+    "residual": (lambda t, **kw: rrm.residual_norm(*t, **kw), [(3, 4, 8)] * 3 + [(8,)] * 3),
+    "residual_back": (lambda t, **kw: rrm.residual_norm_backward(*t, **kw), [(3, 4, 8)] * 4 + [(3, 4, 2)] + [(3, 4, 8)] + [(8,)] * 3),
+    "orth": (lambda t, **kw: rrm.orthogonalize(t[0], **kw), [(2, 4, 6)]),
+}
+
+
+class Device(torch.Tensor):
+    is_cuda = True
+    device = torch.device("cuda", 0)
+
+
+class OtherDevice(torch.Tensor):
+    is_cuda = True
+    device = torch.device("cuda", 1)
+
+
+@pytest.fixture
+def without_a_device(monkeypatch):
+    """Calls end at a library that does nothing; tensors are CPU ones that say otherwise."""
+    class Library:
+        def __getattr__(self, name):
+            return (lambda *a: 0)
+
+    monkeypatch.setattr(ops, "lib", Library)
+    monkeypatch.setattr(ops, "_plans", {})
+    monkeypatch.setattr(ops, "_stream_ptr", lambda stream, device=None: 0x100)
+
+
+def inputs_of(name):
+    call, shapes = CALLS[name]
+    return call, [torch.zeros(shape).as_subclass(Device) for shape in shapes]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_gradients_are_not_lost_in_silence(name, without_a_device):
+    """Every input that requires a gradient is refused where autograd records, also when the same call has been made without."""
+    call, inputs = inputs_of(name)
+    call(inputs)
+    for t in inputs:
+        t.requires_grad_()
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(inputs)
+        with torch.no_grad():
+            call(inputs)
+        t.requires_grad_(False)
+    call(inputs)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_tensors_of_several_devices_are_refused(name, without_a_device):
+    call, inputs = inputs_of(name)
+    call(inputs)
+    for k in range(1, len(inputs)):
+        with pytest.raises(ValueError, match="several devices"):
+            call([t.as_subclass(OtherDevice) if i == k else t for i, t in enumerate(inputs)])
+
+
+@gpu
+@pytest.mark.parametrize("name", CALLS)
+def test_a_call_on_another_stream_beside_one_that_uses_freed_memory(name):
+    """With stream= results and workspace are that stream's memory: a block that the current stream has freed but still fills is not handed out."""
+    call, shapes = CALLS[name]
+    inputs = [torch.randn(shape, generator=gen(i)).cuda() for i, shape in enumerate(shapes)]
+    several = lambda got: [t for t in (got if isinstance(got, tuple) else (got,)) if t is not None]  # noqa: E731
+    want = [t.clone() for t in several(call(inputs))]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for size in {t.numel() * t.element_size() for t in want} | {1 << 16}:
+            late = torch.empty(size, dtype=torch.uint8, device="cuda")
+            torch.cuda._sleep(2_000_000)
+            late.fill_(255)
+            del late
+        got = several(call(inputs, stream=side))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
