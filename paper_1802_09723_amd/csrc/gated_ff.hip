@@ -240,42 +240,6 @@ hipError_t launch_tiles(Product& a, hipStream_t s) {
                        dim3(WM * WN * 64), 0, s, a);
     return hipGetLastError();
 }
-struct Plan {
-    int shape, splits, splits2;  // parts of the summed axis (of the second product)
-    float us;
-};
-constexpr float LAUNCH_US = 6.0f;  // what a launch of tiles takes beside its steps: its start, its first copies, its results
-struct Work {  // a product of rows x cols, `ways` of them, over `steps` steps each
-    int rows, cols, steps, ways;
-};
-// The least estimate for a product, or two in one launch (b.steps > 0); `bytes`: what comes from memory at the least, at some 4 TB/s.
-Plan plan_products(const Work& a, const Work& b, float bytes) {
-    Plan best{SMALL, 1, 1, 1e30f};
-    for (int w = BIG; w <= SMALL; ++w) {
-        const Shape& h = SHAPES[w];
-        const int64_t ta = (int64_t)tiles(a.rows, h.bm) * tiles(a.cols, h.bn) * a.ways;
-        const int64_t tb = b.steps ? (int64_t)tiles(b.rows, h.bm) * tiles(b.cols, h.bn) * b.ways : 0;
-        for (int sa = 1; sa <= 16 && (sa == 1 || a.steps / sa >= 4); sa *= 2)
-            for (int sb = 1; sb <= 16 && (sb == 1 || b.steps / sb >= 4); sb *= 2) {
-                const int ea = tiles(a.steps, sa), eb = tiles(b.steps, sb), longest = ea > eb ? ea : eb;
-                const int64_t groups = ta * sa + tb * sb, all = ta * sa * ea + tb * sb * eb;
-                // rounds of the longest workgroups' steps; two products share them by their steps
-                const int64_t rounds = (groups + h.at_once - 1) / h.at_once;
-                float steps = (float)rounds * longest;
-                if (b.steps && rounds > 1) steps = (float)all / h.at_once + 0.5f * longest;
-                float us = steps * h.first + (float)all / OP_CUS * h.second;
-                if (us < bytes / 4e6f) us = bytes / 4e6f;
-                // the sums' way through memory and the launch that joins them
-                if (sa > 1 || sb > 1) us += 5.0f;
-                if (sa > 1) us += (float)sa * a.ways * a.rows * (float)a.cols * 8.0f / 6e6f;
-                if (sb > 1) us += (float)sb * b.ways * b.rows * (float)b.cols * 8.0f / 6e6f;
-                us += LAUNCH_US;
-                if (us < best.us) best = Plan{w, sa, sb, us};
-            }
-    }
-    return best;
-}
-
 template <int KIND, int ACT, bool PT, bool QT>
 hipError_t launch_product(Product& a, int shape, hipStream_t s) {
     switch (shape) {

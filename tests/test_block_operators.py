@@ -579,7 +579,7 @@ def newton_schulz(g, steps, co, eps):
 
 FAST = (3.4445, -4.7750, 2.0315)
 SURE = (1.875, -1.25, 0.375)
-ORTH = [(1, 1), (1, 9), (9, 1), (5, 7), (16, 16), (33, 130), (130, 33), (64, 512), (128, 128), (129, 127), (257, 300), (300, 70), (520, 264)]
+ORTH = [(1, 1), (1, 9), (9, 1), (5, 7), (16, 16), (33, 130), (130, 33), (64, 512), (128, 128), (129, 127), (257, 300), (300, 70), (520, 264), (48, 1500), (2100, 90), (300, 1111), (127, 511), (512, 100)]
 
 
 @gpu
@@ -935,13 +935,15 @@ def test_refusals_come_back_as_status_codes():
     def orth(g=P, x=P, ws=P, have=big, **kw):
         return L.rrm_orthogonalize(ref(orth_desc(**kw)), g, x, ws, have, None)
 
-    need = L.rrm_orthogonalize_workspace(ref(orth_desc()))
+    assert L.rrm_orthogonalize_workspace(ref(orth_desc())) == 0  # (one launch)
+    wide = dict(rows=200, cols=600, g_matrix=120000, g_row=600, x_matrix=120000, x_row=600)
+    need = L.rrm_orthogonalize_workspace(ref(orth_desc(**wide)))
     assert need > 0
-    assert L.rrm_orthogonalize(None, P, P, P, big, None) == -1 and orth(g=None) == -1 and orth(x=None) == -1 and orth(ws=None) == -1
+    assert L.rrm_orthogonalize(None, P, P, P, big, None) == -1 and orth(g=None) == -1 and orth(x=None) == -1 and orth(ws=None, **wide) == -1
     assert orth(n=-1) == -2 and orth(n=65536) == -2 and orth(rows=0) == -2 and orth(cols=65537) == -2 and orth(n=60000, rows=60000, cols=60000) == -2
     assert orth(elem=3) == -3 and orth(steps=0) == -8 and orth(steps=101) == -8 and orth(a=math.nan) == -8 and orth(eps=-1.0) == -8 and orth(c=math.inf) == -8
     assert orth(x_row=5) == -2 and orth(x_matrix=20) == -2 and orth(g_row=1 << 62) == -2
-    assert orth(g=P + 2) == -9 and orth(x=P + 1) == -9 and orth(ws=P + 128) == -9 and orth(have=need - 1) == -10 and orth(n=0) == 0
+    assert orth(g=P + 2) == -9 and orth(x=P + 1) == -9 and orth(ws=P + 128, **wide) == -9 and orth(have=need - 1, **wide) == -10 and orth(n=0) == 0
 
 
 def test_the_binding_refuses_what_the_calls_cannot_take():
