@@ -235,10 +235,9 @@ struct Chunk {
     static constexpr int PK = DK * E + 16, PV = DV * E + 32, PP = C * E + 16;             // bytes between rows in LDS: reads of a wavefront meet different banks
     static constexpr int QK_BYTES = C * PK, V_BYTES = C * PV, P_BYTES = C * PP;
     static constexpr int LDS = 2 * QK_BYTES + V_BYTES + P_BYTES, LDS_STATES = QK_BYTES + V_BYTES;
-    static constexpr int NK = C * DK / EPC / THREADS, NV = C * DV / EPC / THREADS;        // 16-byte pieces a thread stages ..
-    static constexpr int RK = THREADS / (DK / EPC), RV = THREADS / (DV / EPC);            // .. of rows so far apart
-    static constexpr int AT_ONCE = WAVES * (163840 / LDS < 2 ? 1 : 2) / 4;                // wavefronts on a SIMD
-    static_assert(NK * RK == C && NV * RV == C, "whole pieces a thread");
+    static constexpr int RK = THREADS / (DK / EPC), RV = THREADS / (DV / EPC);            // rows staged at once, a thread 16 bytes ..
+    static constexpr int NK = (C + RK - 1) / RK, NV = (C + RV - 1) / RV;                  // .. and how many times
+    static constexpr int AT_ONCE = (WAVES * (163840 / LDS < 2 ? 1 : 2) + 3) / 4;           // wavefronts on a SIMD
 };
 
 // STATES: what a stretch alone adds to the state (q and the results are not touched).  EXACT: rows of q, k and v are whole pieces of 16 bytes.
@@ -296,14 +295,15 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     // pieces make up begins early.  (frames lie at most 2^22 elements apart: offsets within a chunk have 32 bits)
     struct Part {
         int row, c;
-        bool in, whole;
+        bool in, whole, idle;
         unsigned at;  // bytes from the lowest of the chunk's frames in memory ..
         int apart;    // .. and between the rows
     };
     auto part_of = [&](int per, int rows, int64_t frame, int c0, int cols) {  // per: pieces in a row of LDS; columns c0 .. c0 + cols
         Part p;
         p.row = tid / per, p.c = tid % per * EPC;
-        p.in = p.c < cols, p.whole = p.c + EPC <= cols;
+        p.idle = p.row >= rows;
+        p.in = p.c < cols && !p.idle, p.whole = p.c + EPC <= cols;
         if (!EXACT && !p.whole) p.c = cols - EPC;
         p.at = (unsigned)(((w.back ? rows - 1 - p.row : p.row) * frame + c0 + p.c) * K::E);
         p.apart = (int)(rows * frame * K::E);
@@ -315,12 +315,13 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     auto fetch_rows = [&](u32x4* held, auto count, auto rows, const T* p, int64_t frame, const Part& part, int f) __attribute__((always_inline)) {
         constexpr int N = decltype(count)::value, R = decltype(rows)::value;
         const int none = have - f < C ? C - (have - f) : 0;
-        const int64_t lowest = w.back ? (int64_t)(end - 1 - f0 - f) + none - (C - 1) : (int64_t)f0 + f - none;
+        const int64_t lowest = w.back ? (int64_t)(end - 1 - f0 - f) + none - (N * R - 1) : (int64_t)f0 + f - none;
         const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + lowest * frame), 0, 0x7fffffff, 0x00027000);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            held[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, part.in && part.row + i * R >= none ? part.at : NOWHERE,
-                                                            (w.back ? N - 1 - i : i) * part.apart, 0);
+            const int row = part.row + i * R;
+            const bool there = part.in && row >= none && (N * R == C || row < C);
+            held[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, there ? part.at : NOWHERE, (w.back ? N - 1 - i : i) * part.apart, 0);
         }
     };
     const std::integral_constant<int, K::NK> nk;
@@ -333,7 +334,8 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
         if constexpr (!STATES) fetch_rows(hq, nk, rk, q, w.q.frame, pq, f);
         fetch_rows(hv, nv, rv, v, w.v.frame, pv, f);
     };
-    auto put_row = [&](unsigned char* to, const Part& part, const u32x4& x) __attribute__((always_inline)) {
+    auto put_row = [&](unsigned char* to, const Part& part, const u32x4& x, bool there) __attribute__((always_inline)) {
+        if (!there) return;
         if (EXACT || part.whole) {
             *reinterpret_cast<u32x4*>(to + part.c * K::E) = x;  // (behind the last column: zeros)
         } else if (part.in) {
@@ -348,11 +350,16 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     auto put = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < K::NK; ++i) {
-            put_row(ks + (pk.row + i * K::RK) * K::PK, pk, hk[i]);
-            if constexpr (!STATES) put_row(qs + (pk.row + i * K::RK) * K::PK, pk, hq[i]);
+            const int row = pk.row + i * K::RK;
+            const bool there = (K::THREADS % (DK / EPC) == 0 || !pk.idle) && (K::NK * K::RK == C || row < C);
+            put_row(ks + row * K::PK, pk, hk[i], there);
+            if constexpr (!STATES) put_row(qs + row * K::PK, pk, hq[i], there);
         }
 #pragma unroll
-        for (int i = 0; i < K::NV; ++i) put_row(vs + (pv.row + i * K::RV) * K::PV, pv, hv[i]);
+        for (int i = 0; i < K::NV; ++i) {
+            const int row = pv.row + i * K::RV;
+            put_row(vs + row * K::PV, pv, hv[i], (K::THREADS % (DV / EPC) == 0 || !pv.idle) && (K::NV * K::RV == C || row < C));
+        }
     };
     // once: zeros behind the last column, and above the diagonal of the scores
     if (!EXACT) {
@@ -551,17 +558,27 @@ hipError_t launch_steps(const Walk& w, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Padded sizes of a walk's kernel: 64 or 128 keys, tiles of 64 columns of the state, or of 128 for more than 64 keys where those leave none empty
+// Padded sizes of a walk's kernel: 64, 96, 128 or 160 keys (fp32: 64 or 128), and tiles of the state of 64, 96 or 128 columns: those with the fewest in all, the widest
+// of them.  Up to 64 keys, and for more than 128, tiles are of 64: registers and LDS hold two workgroups of those.
 template <typename T, typename F>
 void with_chunk(const Walk& w, F&& f) {
     const std::integral_constant<int, 64> c64;
+    const std::integral_constant<int, 96> c96;
     const std::integral_constant<int, 128> c128;
-    if (w.dk <= 64) f(c64, c64);
-    else if (((w.dv + 63) / 64) % 2) f(c128, c64);
-    else f(c128, c128);
+    const std::integral_constant<int, 160> c160;
+    auto padded = [&](int tile) { return (w.dv + tile - 1) / tile * tile; };
+    if (w.dk <= 64) return f(c64, c64);
+    if constexpr (sizeof(T) == 4) {
+        padded(128) <= padded(64) ? f(c128, c128) : f(c128, c64);
+    } else {
+        if (w.dk > 128) return f(c160, c64);
+        const bool wide = padded(128) <= padded(64) && padded(128) <= padded(96), middle = padded(96) <= padded(64);
+        if (w.dk > 96) return wide ? f(c128, c128) : middle ? f(c128, c96) : f(c128, c64);
+        wide ? f(c96, c128) : middle ? f(c96, c96) : f(c96, c64);
+    }
 }
 // More keys than that are taken half by half: a state's rows have nothing to do with each other, and results are sums over them.
-constexpr int MOST_KEYS = 128;
+int most_keys(int elem) { return elem == RRM_F32 ? 128 : 160; }
 
 // A frame or two of live videos: the state is the traffic, and each of its values is used once
 bool few_frames(int t) { return t <= 2; }
@@ -610,7 +627,7 @@ void launch_chunk(const Walk& w, const Stretches& st, hipStream_t s) {
 }
 template <typename T, bool STATES>
 hipError_t launch_chunks(const Walk& all, const Stretches& st, hipStream_t s) {
-    const int half = all.dk <= MOST_KEYS ? all.dk : ((all.dk + 1) / 2 + 7) / 8 * 8;  // (57 to 128 keys: whole pieces)
+    const int half = all.dk <= most_keys(sizeof(T) == 4 ? RRM_F32 : RRM_BF16) ? all.dk : ((all.dk + 1) / 2 + 7) / 8 * 8;  // (57 to 128 keys: whole pieces)
     for (int k = 0; k < all.dk; k += half) {
         Walk w = all;
         w.first_key = k, w.keys = all.dk, w.dk = all.dk - k < half ? all.dk - k : half;
@@ -635,7 +652,7 @@ hipError_t launch_walk(const Walk& w, const Stretches& st, int elem, hipStream_t
 }
 // What a walk's first half of the keys leaves
 size_t part_bytes(const rrm_decay_desc& d, int keys, int cols) {
-    return by_steps(d) || keys <= MOST_KEYS ? 0 : round256((size_t)d.n * d.t * d.h * cols * 4);
+    return by_steps(d) || keys <= most_keys(d.elem) ? 0 : round256((size_t)d.n * d.t * d.h * cols * 4);
 }
 size_t states_bytes(const rrm_decay_desc& d) {
     const Stretches st = stretches_of(d, nullptr);

@@ -153,6 +153,10 @@ ATTENTION = [
     (2, 129, 1, 200, 200),
     (1, 66, 1, 255, 17),
     (2, 256, 2, 31, 31),
+    (2, 140, 1, 96, 96),
+    (1, 130, 2, 144, 88),
+    (1, 70, 1, 90, 150),
+    (1, 200, 1, 160, 161),
 ]
 
 
