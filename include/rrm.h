@@ -388,6 +388,8 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
  * are 0 there, and s_last is the state after its last frame (s0 for a video of no frames).  One frame of live videos is t = 1, with s0 the state
  * before and s_last the state after it; there s_last may be s0.  Inputs of several heads may be one (a head's stride of 0); their gradients come head
  * by head.  log_decay is at most 0 in a memory that fades (minus infinity: nothing of the frames before); its decays are not learned, there is no gradient.
+ * Infinities and not-a-numbers reach what the formulas take them into, a frame's neighbours of other videos, heads and times never; an infinity may come out
+ * as a not-a-number.
  *
  * A bfloat16 call multiplies on the matrix cores in bfloat16: the scores with their decays, and the state where a query reads it, are rounded to
  * it; the state itself, and what it takes up of each frame, are held in 32 bits. */

@@ -213,7 +213,11 @@ __device__ __forceinline__ v8f across(const unsigned char* tile, int c0, int ste
 }
 __device__ __forceinline__ float power(int e, float log2_decay) { return __builtin_amdgcn_exp2f((float)e * log2_decay); }
 // (a decay of 0: its zeroth power is 1)
-__device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.44269504088896f, -16384.0f); }
+__device__ __forceinline__ float log2_of(float log_decay) {
+    const float x = log_decay * 1.44269504088896f;
+    return x < -16384.0f ? -16384.0f : x;  // (a not-a-number stays one)
+}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 // Stretches of the time axis, of `frames` frames each (whole chunks), a workgroup each (none: the walk goes frame by frame): states[s] is the state before stretch
 // s + 1, [pair][k][v] as the forward pass lays them, or what stretch s alone adds to it.
@@ -403,7 +407,7 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int d = (ib - jb) * 16 + lr - 4 * g - r;
-                    x[r] = p[r] * (d >= 0 ? w.given * w.taken * power(d, decay) : 0.0f);
+                    x[r] = d >= 0 ? p[r] * (w.given * w.taken * power(d, decay)) : 0.0f;  // (q . k of frames to come may be infinite)
                 }
                 if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
                 else *reinterpret_cast<u32x2*>(to) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
@@ -515,6 +519,50 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
                 if (row < w.dk) keep[corner + row * row_step] = state[i][r];
             }
     }
+    if constexpr (!STATES) {
+        // Masked places are zeros among a chunk's scores, and 0 times a v that is not finite has reached the chunk's frames before it.  Such a v stays in the state:
+        // where the state has ended so, the frames before the first of them are made again, as the recurrence stands, by this wavefront for its columns.
+        const bool ended = col < w.dv && 4 * g < w.dk && !finite(state[0][0]);
+        if (w.o.p && __any(ended)) {
+            __threadfence();  // (behind the results as they are)
+            const float lambda = power(1, decay);
+            int g4 = 4 * g;
+            asm volatile("" : "+v"(g4));  // (or conditions of rows are held from here on)
+#pragma unroll
+            for (int i = 0; i < SB; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * i + g4 + r;
+                    state[i][r] = from && row < w.dk && col < w.dv ? from[corner + row * row_step] : 0.0f;
+                }
+            for (int f = 0; f < have && __any(ended && finite(state[0][0])); ++f) {
+                const int64_t at = w.back ? end - 1 - f0 - f : f0 + f;
+                const float vf = col < w.dv ? w.taken * load_elem(v + at * w.v.frame + col) : 0.0f;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < SB; ++i) {
+                    asm volatile("" : "+v"(g4));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = 16 * i + g4 + r;
+                        if (row >= w.dk) continue;
+                        if (!w.back) state[i][r] *= lambda;
+                        state[i][r] += load_elem(k + at * w.k.frame + row) * vf;
+                        sum += load_elem(q + at * w.q.frame + row) * state[i][r];
+                        if (w.back) state[i][r] *= lambda;
+                    }
+                }
+                sum += __shfl_xor(sum, 16);
+                sum = w.given * (sum + __shfl_xor(sum, 32));
+                if (g == 0 && col < w.dv) {
+                    float* const part = w.part + ((video * (int64_t)w.t + at) * w.h + head) * w.dv + col;
+                    if (w.adds) sum += *part;
+                    if (w.leaves) *part = sum;
+                    else store_elem(o + at * w.o.frame + wave * 16 + lr, sum);
+                }
+            }
+        }
+    }
     if (!STATES && w.o.p && !w.leaves) {  // behind a video's end
         const int cols = vcols < DV ? vcols : DV, z0 = end > f0 ? end : f0;
         const int z1 = w.t - f0 < st.frames ? w.t : f0 + st.frames;
@@ -585,7 +633,7 @@ bool few_frames(int t) { return t <= 2; }
 // ... and frames that lie backwards or very far apart, which the chunks' 32-bit offsets do not reach, or rows of less than 16 bytes
 bool by_steps(const rrm_decay_desc& d) {
     if (few_frames(d.t) || d.dk < 8 || d.dv < 8) return true;
-    for (int64_t frame : {d.q_frame, d.k_frame, d.v_frame, d.o_frame})
+    for (int64_t frame : {d.q_frame, d.k_frame, d.v_frame, d.o_frame, d.dq_frame, d.dk_frame, d.dv_frame})
         if (frame < 0 || frame > (1 << 22)) return true;
     return false;
 }

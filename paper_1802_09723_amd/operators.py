@@ -616,6 +616,7 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     made = out is None
     if made:
         out = torch.empty_like(g, dtype=torch.bfloat16, memory_format=torch.contiguous_format)
+    coefficients = tuple(coefficients)
     key = ("orth", steps, coefficients, eps, _look(g), made or _look(out))
     plan = _plans.get(key)
     if plan is None:

@@ -263,9 +263,74 @@ def test_attention_is_by_video_and_head():
     o, _ = rrm.decay_attention(dev["q"], dev["k"], dev["v"], decays(3).cuda(), s0=dev["s0"])
     ok = torch.isfinite(o).all(-1).cpu()
     assert not ok[1, 90:, 2].any() and not ok[2, 130:, 0].any()
-    # (frames before theirs in the same stretch of 64 multiply them by weights of 0)
-    ok[1, 64:, 2] = ok[2, 128:, 0] = True
+    ok[1, 90:, 2] = ok[2, 130:, 0] = True
     assert ok.all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 150, 2, 64, 48), (1, 140, 1, 100, 130), (1, 130, 2, 200, 33), (2, 90, 2, 9, 8), (1, 4200, 1, 64, 64)])
+def test_attention_of_values_that_are_not_finite(shape, kind):
+    """Infinities and not-a-numbers reach the frames behind theirs (before theirs, of the gradients that go backwards), and no other: what the recurrence gives
+    finite is as far off as without them, and what it does not is not finite."""
+    n, t, h, dk, dv = shape
+    data, _ = attention_case(*shape, kind, False, 8)
+    ld, scale = decays(h), 0.3
+    plant = {"v": (20, math.inf), "k": (51, math.nan), "do": (t - 7, -math.inf), "q": (t - 30, math.nan)}
+    for name, (frame, value) in plant.items():
+        data[name][0, frame, h - 1, data[name].shape[-1] // 2] = value
+    d64 = {k: a.double() for k, a in data.items()}
+    dev = {k: a.cuda() for k, a in data.items()}
+    o, s_last = attend64(d64["q"], d64["k"], d64["v"], ld, scale, d64["s0"], [t] * n)
+    lam, rows, states, s = torch.exp(ld.double()).view(1, h, 1, 1), [None] * t, [], d64["s0"]
+    for j in range(t):
+        s = lam * s + d64["k"][:, j, ..., :, None] * d64["v"][:, j, ..., None, :]
+        states.append(s)
+    s = d64["ds_last"]
+    for j in reversed(range(t)):
+        s = s + scale * d64["q"][:, j, ..., :, None] * d64["do"][:, j, ..., None, :]
+        rows[j] = (scale * (states[j] * d64["do"][:, j, ..., None, :]).sum(-1), (s * d64["v"][:, j, ..., None, :]).sum(-1),
+                   (s * d64["k"][:, j, ..., :, None]).sum(-2))
+        s = lam * s
+    want = [torch.stack(a, 1) for a in zip(*rows)] + [s]
+    clean = {k: torch.nan_to_num(a, 0.0, 0.0, 0.0) for k, a in d64.items()}
+    turned = {k: clean[k].transpose(-1, -2) for k in ("s0", "ds_last")}
+    so, ss = attend_slack(clean["q"], clean["k"], clean["v"], ld, scale, clean["s0"], [t] * n, False, kind)
+    sq, _ = attend_slack(clean["do"], clean["v"], clean["k"], ld, scale, turned["s0"], [t] * n, False, kind)
+    sk, _ = attend_slack(clean["v"], clean["do"], scale * clean["q"], ld, 1.0, turned["ds_last"], [t] * n, True, kind)
+    sv, s0s = attend_slack(clean["k"], scale * clean["q"], clean["do"], ld, 1.0, clean["ds_last"], [t] * n, True, kind)
+    got = list(rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"]))
+    got += rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"], ds_last=dev["ds_last"])
+    for g, w, slack, what in zip(got, [o, s_last] + want, (so, ss, sq, sk, sv, s0s), ("o", "s_last", "dq", "dk", "dv", "ds0")):
+        ok = torch.isfinite(w)
+        assert torch.equal(torch.isfinite(g.cpu()), ok), what
+        zero = torch.zeros((), dtype=F64)
+        check(torch.where(ok, g.cpu(), zero.to(g.dtype)), torch.where(ok, w, zero), torch.where(ok, slack, zero), what)
+    o, _ = rrm.decay_attention(dev["q"], dev["k"], dev["v"], torch.full((h,), math.nan, device="cuda"))
+    assert not torch.isfinite(o).any()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attention_gradients_with_frames_far_apart(kind):
+    """Gradients whose frames lie further apart than 32 bits reach within a chunk"""
+    n, t, h, d = 1, 70, 1, 32
+    data, _ = attention_case(n, t, h, d, d, kind, False, 4)
+    dev = {k: a.cuda() for k, a in data.items()}
+    ld, far = decays(h).cuda(), (1 << 24) + 8
+    want = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld)
+    memory = torch.zeros(far * (t - 1) + 4 * d, device="cuda", dtype=DT[kind])
+    grads = [memory[i * d:].as_strided((n, t, h, d), (1, far, d, 1)) for i in range(3)]
+    rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld, dq=grads[0], dk=grads[1], dv=grads[2])
+    x, none = {k: a.double() for k, a in data.items()}, torch.zeros(n, h, d, d, dtype=F64)
+    scale, lengths = d ** -0.5, [t]
+    slack = (attend_slack(x["do"], x["v"], x["k"], decays(h), scale, none, lengths, False, kind)[0],
+             attend_slack(x["v"], x["do"], scale * x["q"], decays(h), 1.0, none, lengths, True, kind)[0],
+             attend_slack(x["k"], scale * x["q"], x["do"], decays(h), 1.0, none, lengths, True, kind)[0])
+    for a, b, e, name in zip(grads, want, slack, ("dq", "dk", "dv")):  # (each is off by so much, and by its rounding)
+        b = b.cpu().double()
+        check(a, b, 2 * e + (V if kind == "bf16" else U) * (b.abs() + e), name)
+    assert int(torch.count_nonzero(memory)) <= 3 * t * d
 
 
 @gpu
@@ -957,6 +1022,8 @@ def test_the_binding_refuses_what_the_calls_cannot_take():
                  lambda: rrm.residual_norm_backward(x, None, x, x, x[..., :2]), lambda: rrm.orthogonalize(x)):
         with pytest.raises(ValueError, match="CUDA"):
             call()
+    with pytest.raises(ValueError, match="CUDA"):
+        rrm.orthogonalize(x, coefficients=[1.5, -0.5, 0.0])
     with pytest.raises(ValueError, match="expected \\[n, t, h, features\\]"):
         rrm.decay_attention(x[0], x[0], x[0], ld)
     with pytest.raises(ValueError, match="without b"):
