@@ -40,7 +40,7 @@ __device__ __forceinline__ int frames_of(const Walk& w, int video) {
 }
 
 // The recurrence as it stands, a state in registers: one frame of live videos (and the walk for any).  A workgroup has 64 columns of a head's state; thread
-// (g, quad) holds rows g, g + 16, .. of four columns.
+// (g, quad) holds rows g, g + 16, .. of four columns.  The state's two ways are what bounds it: 64 videos of 16 heads of 128 x 128 take 28.6 us, 4.7 TB/s.
 template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void step_kernel(Walk w, unsigned first) {
     __shared__ float4 sums[2][4][16];
@@ -139,6 +139,9 @@ __global__ __launch_bounds__(256) void step_kernel(Walk w, unsigned first) {
 // v_mfma_f32_16x16x32_bf16 (fp32 tensors: v_mfma_f32_16x16x4_f32); the state's registers are an operand as they stand, and the scores, made once, meet the
 // wavefronts through LDS.  In bfloat16 two operands are rounded: the scores with their decays, and the state where queries read it;
 // lambda^(C-1-j) v_j goes into the state as three bfloat16 parts, which hold all 24 bits of it, as the state's rounding errors stay for as long as it remembers.
+// 64 videos of 256 frames, 32 heads of 128 x 128, bf16: 184 us, 4.4 TB/s (with one part of three 159).  One of 65536 frames, 8 heads: 68 for what stretches add, 12 for
+// their sums, 144 for the results, in a quarter of whose cycles the matrix cores are busy: a chunk is a chain of fetches, LDS, scores, products and two
+// barriers, and registers (state, results and the next chunk's vectors: 128 each) let four wavefronts share a SIMD.
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v8f __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -607,7 +610,8 @@ hipError_t launch_steps(const Walk& w, hipStream_t s) {
 }
 
 // Padded sizes of a walk's kernel: 64, 96, 128 or 160 keys (fp32: 64 or 128), and tiles of the state of 64, 96 or 128 columns: those with the fewest in all, the widest
-// of them.  Up to 64 keys, and for more than 128, tiles are of 64: registers and LDS hold two workgroups of those.
+// of them.  Up to 64 keys, and for more than 128, tiles are of 64: registers and LDS hold two workgroups of those.  80 x 136, four videos of up to 8192 frames, both
+// ways: 718 us; with 64 and 128 keys and tiles of 64 and 128 only, and so 136 keys half by half, 1016.  128 x 128 in two tiles of 64 columns: 205 for the 144 above.
 template <typename T, typename F>
 void with_chunk(const Walk& w, F&& f) {
     const std::integral_constant<int, 64> c64;
@@ -625,10 +629,11 @@ void with_chunk(const Walk& w, F&& f) {
         wide ? f(c96, c128) : middle ? f(c96, c96) : f(c96, c64);
     }
 }
-// More keys than that are taken half by half: a state's rows have nothing to do with each other, and results are sums over them.
+// More keys than that are taken half by half: a state's rows have nothing to do with each other, and results are sums over them.  (A kernel of 256 keys has more
+// state than registers beside its fragments.)
 int most_keys(int elem) { return elem == RRM_F32 ? 128 : 160; }
 
-// A frame or two of live videos: the state is the traffic, and each of its values is used once
+// A frame or two of live videos: the state is the traffic, and each of its values is used once; a chunk of 64 would be zeros but for them
 bool few_frames(int t) { return t <= 2; }
 // ... and frames that lie backwards or very far apart, which the chunks' 32-bit offsets do not reach, or rows of less than 16 bytes
 bool by_steps(const rrm_decay_desc& d) {
@@ -675,7 +680,7 @@ void launch_chunk(const Walk& w, const Stretches& st, hipStream_t s) {
 }
 template <typename T, bool STATES>
 hipError_t launch_chunks(const Walk& all, const Stretches& st, hipStream_t s) {
-    const int half = all.dk <= most_keys(sizeof(T) == 4 ? RRM_F32 : RRM_BF16) ? all.dk : ((all.dk + 1) / 2 + 7) / 8 * 8;  // (57 to 128 keys: whole pieces)
+    const int half = all.dk <= most_keys(sizeof(T) == 4 ? RRM_F32 : RRM_BF16) ? all.dk : ((all.dk + 1) / 2 + 7) / 8 * 8;  // (whole pieces)
     for (int k = 0; k < all.dk; k += half) {
         Walk w = all;
         w.first_key = k, w.keys = all.dk, w.dk = all.dk - k < half ? all.dk - k : half;

@@ -172,7 +172,8 @@ __global__ __launch_bounds__(1024) void poly_kernel(const float* part, int split
 
 // Matrices of up to 128 x 512 (or 512 x 128): all steps in one launch, a workgroup a matrix.  X is in registers in 32 bits, 32 columns a wavefront, and in
 // LDS in half precision, as are A and then b A + c A^2: 160 KB for the largest.  The sixteen bytes of a row that reads ask for together are turned by
-// the row's number (XOR), so that rows meet different banks.  128 x 512: 35 us, bound by LDS (6 us a step); by launches of products 90, each a start and a trip to memory.
+// the row's number (XOR), so that rows meet different banks.  128 x 512: 54 us, most of it
+// a step's chain of LDS reads, products and barriers on one compute unit (some 9 us a step); by launches of products 90, each a start and a trip to memory.
 constexpr int SMALL_FEW = 128, SMALL_MANY = 512;
 typedef __attribute__((address_space(3))) v4s* turned_t;
 template <typename T>
