@@ -24,39 +24,49 @@ ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 MARK_FRAMES = 64  # RRM_SCAN_MARK_FRAMES
 
 
-class NormDesc(ctypes.Structure):
+class _Desc(ctypes.Structure):
+    """A descriptor whose whole numbers are what was given: ctypes drops the bits that a field has no room for, and the call would see a small size."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        for (name, kind), value in [*zip(self._fields_, args), *((f, kw[f[0]]) for f in self._fields_ if f[0] in kw)]:
+            if kind is not ctypes.c_float and getattr(self, name) != value:
+                raise ValueError(f"{name}: {value} is beyond what a call takes ({8 * ctypes.sizeof(kind)} bits)")
+
+
+class NormDesc(_Desc):
     """``rrm_norm_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("n", "positions", "c", "groups", "x_elem", "y_elem", "act")] + [("eps", ctypes.c_float)]
                 + [(k, ctypes.c_int64) for k in ("x_sample", "x_position", "y_sample", "y_position", "dx_sample", "dx_position")])
 
 
-class ScanDesc(ctypes.Structure):
+class ScanDesc(_Desc):
     """``rrm_scan_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("n", "t", "c", "elem")]
                 + [(k, ctypes.c_int64) for k in ("x_video", "x_frame", "f_video", "f_frame", "y_video", "y_frame",
                                                  "dx_video", "dx_frame", "df_video", "df_frame")])
 
 
-class FFDesc(ctypes.Structure):
+class FFDesc(_Desc):
     """``rrm_ff_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("m", "k", "f", "act")]
                 + [(k, ctypes.c_int64) for k in ("x_row", "wg_row", "wu_row", "h_row", "gu_row", "dx_row", "dwg_row", "dwu_row")]
                 + [("unaligned", ctypes.c_int)])
 
 
-class DecayDesc(ctypes.Structure):
+class DecayDesc(_Desc):
     """``rrm_decay_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("n", "t", "h", "dk", "dv", "elem")] + [("scale", ctypes.c_float)]
                 + [(f"{x}_{axis}", ctypes.c_int64) for x in ("q", "k", "v", "o", "dq", "dk", "dv") for axis in ("video", "frame", "head")])
 
 
-class ResidualDesc(ctypes.Structure):
+class ResidualDesc(_Desc):
     """``rrm_residual_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("m", "c", "x_elem", "b_elem", "post_norm")] + [("eps", ctypes.c_float)]
                 + [(f"{x}_row", ctypes.c_int64) for x in ("x", "b", "gate", "r", "u", "dx", "db", "dgate")])
 
 
-class OrthDesc(ctypes.Structure):
+class OrthDesc(_Desc):
     """``rrm_orth_desc``"""
     _fields_ = ([(k, ctypes.c_int) for k in ("n", "rows", "cols", "elem", "steps")] + [(k, ctypes.c_float) for k in ("a", "b", "c", "eps")]
                 + [(k, ctypes.c_int64) for k in ("g_matrix", "g_row", "x_matrix", "x_row")])

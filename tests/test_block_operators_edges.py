@@ -1,0 +1,71 @@
+"""The operators of residual blocks where calls are odd: sizes beyond what a call counts, numbers that come in tensors, axes of nothing, memories that grow,
+values that are not finite late in a long video, and updates of several steps held to what their roundings come to.  Tolerances are those of test_block_operators
+where nothing else is said."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_1802_09723_amd as rrm
+from paper_1802_09723_amd import operators as ops
+from test_block_operators import Device, without_a_device  # noqa: F401
+
+gpu = pytest.mark.gpu
+F64 = torch.float64
+
+
+# -- sizes beyond 31 bits ------------------------------------------------------------------------------------------------------
+
+HUGE = (1 << 32) + 8
+
+
+class Spread(Device):
+    """A tensor of any size in the memory of one row (the library is a stand-in: nothing looks at the places)"""
+    def is_contiguous(self, *args, **kw):
+        return True
+
+
+def spread(*shape, dtype=torch.float32):
+    return torch.zeros(shape[-1], dtype=dtype).expand(shape).as_subclass(Spread)
+
+
+def huge_calls():
+    def attention(n, t, h):
+        q, state, ld = spread(n, t, h, 2), spread(n, h, 2, 2), spread(h)
+        return (lambda: rrm.decay_attention(q, q, q, ld, out=q, s_last=state),
+                lambda: rrm.decay_attention_backward(q, q, q, q, ld, dq=q, dk=q, dv=q, ds0=state))
+
+    x, w, stats = spread(HUGE, 1), torch.zeros(1).as_subclass(Device), spread(HUGE, 2)
+    g = spread(HUGE, 1, 2, dtype=torch.bfloat16)
+    bf = spread(HUGE, 2, dtype=torch.bfloat16)
+    weight = spread(2, 2, dtype=torch.bfloat16)
+    return {
+        "attention frames": attention(1, HUGE, 1)[0], "attention frames back": attention(1, HUGE, 1)[1],
+        "attention videos": attention(HUGE, 1, 1)[0], "attention videos back": attention(HUGE, 1, 1)[1],
+        "residual": lambda: rrm.residual_norm(x, x, pre=w, out=x, u=x),
+        "residual back": lambda: rrm.residual_norm_backward(x, x, x, x, stats, pre=w, dx=x, db=x, dpre=w),
+        "orthogonalize": lambda: rrm.orthogonalize(g, out=g),
+        "steps": lambda: rrm.orthogonalize(g[:1], steps=HUGE, out=g[:1]),
+        "norm": lambda: rrm.group_norm_act(spread(HUGE, 1), 1, out=x),
+        "norm groups": lambda: rrm.group_norm_act(x[:2], HUGE, out=x[:2]),
+        "scan": lambda: rrm.gated_scan(spread(1, HUGE, 1), spread(1, HUGE, 1), out=spread(1, HUGE, 1)),
+        "feed-forward": lambda: rrm.gated_ff(bf, weight, weight, out=bf),
+    }
+
+
+@pytest.mark.parametrize("name", huge_calls())
+def test_sizes_beyond_31_bits_are_refused(name, without_a_device):  # noqa: F811
+    """A size reaches the C call whole or not at all: cut to 32 bits it would be a small one, and the rows behind it would never be made."""
+    with pytest.raises(ValueError, match="beyond"):
+        huge_calls()[name]()
+
+
+def test_descriptors_hold_what_they_are_given():
+    top = (1 << 31) - 1
+    assert ops.ResidualDesc(top, 8).m == top and ops.OrthDesc(n=-1).n == -1 and ops.DecayDesc(1, 2, 3, 4, 5, 1, 0.5, -7).q_video == -7
+    for cls, field, _ in ((c, *f) for c in (ops.NormDesc, ops.ScanDesc, ops.FFDesc, ops.DecayDesc, ops.ResidualDesc, ops.OrthDesc) for f in c._fields_):
+        kind = dict(cls._fields_)[field]
+        if kind is not ctypes.c_float:
+            with pytest.raises(ValueError, match=f"{field}: .* beyond"):
+                cls(**{field: 1 << (8 * ctypes.sizeof(kind) - 1)})
