@@ -72,7 +72,7 @@ class OrthDesc(_Desc):
                 + [(k, ctypes.c_int64) for k in ("g_matrix", "g_row", "x_matrix", "x_row")])
 
 
-# (descriptor, reference to it, bytes of workspace, device) by what the checks looked at.  Emptied when it has grown past what a program's
+# (descriptor, reference to it, bytes of workspace, device) by what the checks looked at, numbers by their values.  Emptied when it has grown past what a program's
 # shapes come to.
 _plans: dict = {}
 
@@ -203,6 +203,7 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
     made = out is None
     if made:
         out = torch.empty_like(x, dtype=out_dtype)
+    groups, eps = int(groups), float(eps)
     key = ("norm", groups, act, eps, out_dtype, _look(x), made or _look(out), _look(gamma), _look(beta), _look(stats))
     plan = _plans.get(key)
     if plan is None:
@@ -215,7 +216,7 @@ def group_norm_act(x, groups: int, gamma=None, beta=None, act: str = "none", eps
         _dense(beta, "beta", (c,), torch.float32)
         _dense(stats, "stats", (n, groups, 2), torch.float32)
         positions = x.numel() // (n * c) if n and c else 0
-        plan = _keep(key, NormDesc(n, positions, c, int(groups), _elem(x), _elem(out), _act(act), float(eps), *_outer_inner(x, "x"),
+        plan = _keep(key, NormDesc(n, positions, c, groups, _elem(x), _elem(out), _act(act), eps, *_outer_inner(x, "x"),
                                    *_outer_inner(out, "out"), 0, 0), "rrm_group_norm_workspace", 0, x, out, gamma, beta, stats)
     ws = _workspace(plan[2], x.device)
     _check(lib().rrm_group_norm_act(plan[1], x.data_ptr(), _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
@@ -234,6 +235,7 @@ def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "non
     made = out is None
     if made:
         out = torch.empty((n, h, w, c), dtype=torch.bfloat16, device="cuda")
+    groups, eps = int(groups), float(eps)
     key = ("norm of", groups, act, eps, n, h, w, c, made or _look(out), _look(gamma), _look(beta), _look(stats))
     plan = _plans.get(key)
     if plan is None:
@@ -241,7 +243,7 @@ def group_norm_act_of(layer, groups: int, gamma=None, beta=None, act: str = "non
         _dense(gamma, "gamma", (c,), torch.float32)
         _dense(beta, "beta", (c,), torch.float32)
         _dense(stats, "stats", (n, groups, 2), torch.float32)
-        plan = _keep(key, NormDesc(n, h * w, c, int(groups), 0, 1, _act(act), float(eps), h * w * c, c, *_outer_inner(out, "out"), 0, 0),
+        plan = _keep(key, NormDesc(n, h * w, c, groups, 0, 1, _act(act), eps, h * w * c, c, *_outer_inner(out, "out"), 0, 0),
                      "rrm_group_norm_workspace", 0, out, gamma, beta, stats)
     ws = _workspace(plan[2], out.device)
     _check(lib().rrm_group_norm_act(plan[1], layer.snapshot_ptrs()[1], _ptr(gamma), _ptr(beta), out.data_ptr(), _ptr(stats), _ptr(ws), plan[2],
@@ -455,6 +457,7 @@ def decay_attention(q, k, v, log_decay, scale=None, s0=None, lengths=None, out=N
         out = v.new_empty((n, t, h, dv))
     if s_last is None:
         s_last = q.new_empty((n, h, dk, dv), dtype=torch.float32)
+    scale = max(dk, 1) ** -0.5 if scale is None else float(scale)
     key = ("decay", scale, _look(q), _look(k), _look(v), _look(log_decay), _look(s0), _look(lengths), made[0] or _look(out), made[1] or _look(s_last))
     plan = _plans.get(key)
     if plan is None:
@@ -466,7 +469,7 @@ def decay_attention(q, k, v, log_decay, scale=None, s0=None, lengths=None, out=N
         _dense(s0, "s0", (n, h, dk, dv), torch.float32)
         _dense(s_last, "s_last", (n, h, dk, dv), torch.float32)
         _dense(lengths, "lengths", (n,), torch.int32)
-        plan = _keep(key, DecayDesc(n, t, h, dk, dv, _elem(q), dk ** -0.5 if scale is None else float(scale), *_heads(q, "q"), *_heads(k, "k"),
+        plan = _keep(key, DecayDesc(n, t, h, dk, dv, _elem(q), scale, *_heads(q, "q"), *_heads(k, "k"),
                                     *_heads(v, "v"), *_heads(out, "out"), *[0] * 9), "rrm_decay_attention_workspace", 0, q, k, v, log_decay, s0, lengths,
                      out, s_last)
     ws = _workspace(plan[2], q.device)
@@ -493,6 +496,7 @@ def decay_attention_backward(do, q, k, v, log_decay, scale=None, s0=None, length
         dv = v.new_empty((n, t, h, fv))
     if ds0 is None:
         ds0 = q.new_empty((n, h, fk, fv), dtype=torch.float32)
+    scale = max(fk, 1) ** -0.5 if scale is None else float(scale)
     key = ("decay back", scale, _look(do), _look(q), _look(k), _look(v), _look(log_decay), _look(s0), _look(lengths), _look(ds_last),
            made[0] or _look(dq), made[1] or _look(dk), made[2] or _look(dv), made[3] or _look(ds0))
     plan = _plans.get(key)
@@ -503,7 +507,7 @@ def decay_attention_backward(do, q, k, v, log_decay, scale=None, s0=None, length
         for x, what in ((s0, "s0"), (ds_last, "ds_last"), (ds0, "ds0")):
             _dense(x, what, (n, h, fk, fv), torch.float32)
         _dense(lengths, "lengths", (n,), torch.int32)
-        plan = _keep(key, DecayDesc(n, t, h, fk, fv, _elem(q), fk ** -0.5 if scale is None else float(scale), *_heads(q, "q"), *_heads(k, "k"),
+        plan = _keep(key, DecayDesc(n, t, h, fk, fv, _elem(q), scale, *_heads(q, "q"), *_heads(k, "k"),
                                     *_heads(v, "v"), *_heads(do, "do"), *_heads(dq, "dq"), *_heads(dk, "dk"), *_heads(dv, "dv")),
                      "rrm_decay_attention_workspace", 1, do, q, k, v, log_decay, s0, lengths, ds_last, dq, dk, dv, ds0)
     ws = _workspace(plan[2], q.device)
@@ -545,6 +549,7 @@ def residual_norm(x, b=None, gate=None, scale=None, post=None, pre=None, eps: fl
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     if made[1]:
         u = torch.empty_like(x, dtype=u_dtype or (x.dtype if b is None else b.dtype), memory_format=torch.contiguous_format)
+    eps = float(eps)
     key = ("residual", eps, u_dtype, _look(x), _look(b), _look(gate), _look(scale), _look(post), _look(pre), made[0] or _look(out), made[1] or _look(u), _look(stats))
     plan = _plans.get(key)
     if plan is None:
@@ -567,7 +572,7 @@ def residual_norm(x, b=None, gate=None, scale=None, post=None, pre=None, eps: fl
             _dense(w, what, (c,), torch.float32)
         _dense(stats, "stats", (*x.shape[:-1], 2), torch.float32)
         row = [0 if t is None else _rows(t, what) for t, what in ((x, "x"), (b, "b"), (gate, "gate"), (out, "out"), (u, "u"))]
-        plan = _keep(key, ResidualDesc(x.numel() // c if c else 0, c, _elem(x), _elem(u if b is None else b), post is not None, float(eps), *row, 0, 0, 0), None, None,
+        plan = _keep(key, ResidualDesc(x.numel() // c if c else 0, c, _elem(x), _elem(u if b is None else b), post is not None, eps, *row, 0, 0, 0), None, None,
                      x, b, gate, scale, post, pre, out, u, stats)
     _check(lib().rrm_residual_norm(plan[1], x.data_ptr(), _ptr(b), _ptr(gate), _ptr(scale), _ptr(post), _ptr(pre), _ptr(out), _ptr(u), _ptr(stats),
                                    _stream_ptr(None, plan[3])))
@@ -626,7 +631,7 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     made = out is None
     if made:
         out = torch.empty_like(g, dtype=torch.bfloat16, memory_format=torch.contiguous_format)
-    coefficients = tuple(coefficients)
+    steps, coefficients, eps = int(steps), tuple(map(float, coefficients)), float(eps)
     key = ("orth", steps, coefficients, eps, _look(g), made or _look(out))
     plan = _plans.get(key)
     if plan is None:
@@ -653,7 +658,7 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
                     raise ValueError(f"{what}: the axes before the last two must collapse to one")
                 lead *= size
             places += [step, t.stride(-2) if rows > 1 else cols]
-        plan = _keep(key, OrthDesc(n, rows, cols, _elem(g), int(steps), float(a), float(b), float(c), float(eps), *places), "rrm_orthogonalize_workspace", None, g, out)
+        plan = _keep(key, OrthDesc(n, rows, cols, _elem(g), steps, a, b, c, eps, *places), "rrm_orthogonalize_workspace", None, g, out)
     ws = _workspace(plan[2], g.device)
     _check(lib().rrm_orthogonalize(plan[1], g.data_ptr(), out.data_ptr(), _ptr(ws), plan[2], _stream_ptr(None, plan[3])))
     return out

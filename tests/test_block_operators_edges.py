@@ -69,3 +69,38 @@ def test_descriptors_hold_what_they_are_given():
         if kind is not ctypes.c_float:
             with pytest.raises(ValueError, match=f"{field}: .* beyond"):
                 cls(**{field: 1 << (8 * ctypes.sizeof(kind) - 1)})
+
+
+# -- numbers that come in tensors ----------------------------------------------------------------------------------------------
+
+NUMBERS = {
+    "attention": (lambda x, w, v: rrm.decay_attention(x, x, x, w, scale=v), "scale", 0.5),
+    "attention back": (lambda x, w, v: rrm.decay_attention_backward(x, x, x, x, w, scale=v), "scale", 0.5),
+    "residual": (lambda x, w, v: rrm.residual_norm(x, pre=w, eps=v), "eps", 0.5),
+    "orthogonalize eps": (lambda x, w, v: rrm.orthogonalize(x, eps=v), "eps", 0.5),
+    "orthogonalize steps": (lambda x, w, v: rrm.orthogonalize(x, v), "steps", 2),
+    "orthogonalize coefficients": (lambda x, w, v: rrm.orthogonalize(x, coefficients=[1.0, v, 0.0]), "b", 0.5),
+    "norm": (lambda x, w, v: rrm.group_norm_act(x, 2, eps=v), "eps", 0.5),
+    "norm groups": (lambda x, w, v: rrm.group_norm_act(x, v), "groups", 2),
+}
+
+
+@pytest.mark.parametrize("name", NUMBERS)
+def test_a_number_in_a_tensor_counts_as_it_is_now(name, without_a_device, monkeypatch):  # noqa: F811
+    """Descriptors are kept by what they were made of: a number's value, not the tensor that held it."""
+    seen = []
+
+    class Library:
+        def __getattr__(self, entry):
+            return lambda *a: 0 if entry.endswith("workspace") else seen.append(getattr(a[0]._obj, field)) or 0
+
+    monkeypatch.setattr(ops, "lib", Library)
+    call, field, value = NUMBERS[name]
+    x, w = torch.zeros(2, 3, 4, 4).as_subclass(Device), torch.zeros(4).as_subclass(Device)
+    number = torch.tensor(value)
+    call(x, w, number)
+    number += number
+    call(x, w, number)
+    call(x, w, 2 * value)
+    assert seen == [value, 2 * value, 2 * value]
+    assert len(ops._plans) == 2
