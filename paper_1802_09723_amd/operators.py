@@ -137,8 +137,8 @@ def _outer_inner(t, what: str):
     """Strides of the first axis and of the axes between it and the last, which have to collapse to one."""
     _adjacent(t, what)
     shape, strides = t.shape, t.stride()
-    if t.dim() == 2:
-        return strides[0], shape[1]
+    if t.dim() == 2 or not t.numel():
+        return strides[0], shape[-1]
     inner = strides[-2]
     rows = shape[-2]
     for size, stride in zip(shape[-3:0:-1], strides[-3:0:-1]):
@@ -524,6 +524,8 @@ def _rows(t, what: str):
     _adjacent(t, what)
     if t.dim() < 2:
         raise ValueError(f"{what}: expected [.., c]")
+    if not t.numel():  # (strides of nothing)
+        return t.shape[-1]
     rows, step = 1, 0
     for size, stride in zip(t.shape[-2::-1], t.stride()[-2::-1]):
         if size == 1:
@@ -650,7 +652,7 @@ def orthogonalize(g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
             lead = 1
             step = 0
             for size, stride in zip(t.shape[-3::-1], t.stride()[-3::-1]):
-                if size == 1:
+                if size == 1 or n == 0:
                     continue
                 if lead == 1:
                     step = stride

@@ -104,3 +104,44 @@ def test_a_number_in_a_tensor_counts_as_it_is_now(name, without_a_device, monkey
     call(x, w, 2 * value)
     assert seen == [value, 2 * value, 2 * value]
     assert len(ops._plans) == 2
+
+
+# -- axes of nothing -----------------------------------------------------------------------------------------------------------
+
+NOTHING = [(0, 8), (2, 0, 8), (0, 2, 8), (3, 0, 2, 8), (2, 3, 0, 8), (0, 0, 8)]
+
+
+def of_nothing(shape, make):
+    """Tensors without elements: as they are made, and as parts of larger ones, whose axes would not collapse"""
+    whole = make(*(max(s, 1) + 2 for s in shape[:-1]), shape[-1])
+    return make(*shape), whole[tuple(slice(s) for s in shape[:-1])]
+
+
+def run_on_nothing(shape, make, sums):
+    c = shape[-1]
+    w = make(c)
+    for x in of_nothing(shape, make):
+        stats = make(*shape[:-1], 2)
+        r, u = rrm.residual_norm(x, x, x, w, w, w, stats=stats)
+        assert r.shape == u.shape == shape
+        assert rrm.residual_norm(x, pre=w)[1].shape == shape
+        got = rrm.residual_norm_backward(x, x, x, x, stats, x, w, w, w)
+        assert [g.shape for g in got] == [shape] * 3 + [(c,)] * 3 and not (sums and any(g.any() for g in got[3:]))
+        if len(shape) > 2:
+            assert rrm.group_norm_act(x, 2).shape == shape
+            got = rrm.group_norm_act_backward(x, x, make(shape[0], 2, 2), w)
+            assert got[0].shape == shape and not (sums and (got[1].any() or got[2].any()))
+    for x in of_nothing((*shape[:-1], 3, 5), make):
+        if x.shape[-2] == 3:
+            assert rrm.orthogonalize(x).shape == (*shape[:-1], 3, 5)
+
+
+@pytest.mark.parametrize("shape", NOTHING)
+def test_calls_of_nothing_are_taken_whatever_their_axes(shape, without_a_device):  # noqa: F811
+    run_on_nothing(shape, lambda *s: torch.zeros(s).as_subclass(Device), False)
+
+
+@gpu
+@pytest.mark.parametrize("shape", NOTHING)
+def test_calls_of_nothing(shape):
+    run_on_nothing(shape, lambda *s: torch.ones(s, device="cuda"), True)
