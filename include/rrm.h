@@ -387,7 +387,9 @@ rrm_status rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const v
  * A video of lengths[i] < t frames ends there: what q, k, v and do hold behind is not looked at (not-a-numbers included), o, dq, dk and dv
  * are 0 there, and s_last is the state after its last frame (s0 for a video of no frames).  One frame of live videos is t = 1, with s0 the state
  * before and s_last the state after it; there s_last may be s0.  Inputs of several heads may be one (a head's stride of 0); their gradients come head
- * by head.  log_decay is at most 0 in a memory that fades (minus infinity: nothing of the frames before); its decays are not learned, there is no gradient.
+ * by head.  log_decay is at most 0 in a memory that fades (minus infinity: nothing of the frames before); its decays are not learned, there is no gradient.  Above 0
+ * the memory grows: what the recurrence holds in 32 bits comes out so, but a head that doubles in a frame (of a few long videos,
+ * whose frames many workgroups share: that grows by 2^64 in a workgroup's) goes frame by frame, some microseconds each.
  * Infinities and not-a-numbers reach what the formulas take them into, a frame's neighbours of other videos, heads and times never; an infinity may come out
  * as a not-a-number.
  *

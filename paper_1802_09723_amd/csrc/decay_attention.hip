@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void step_kernel(Walk w, unsigned first) {
 //
 // Of C frames at once, i and j counted from a chunk's first, W the state before it:
 //      result_i = sum over j up to i of lambda^(i-j) (q_i . k_j) v_j + lambda^(i+1) q_i W        W' = lambda^C W + sum of lambda^(C-1-j) k_j^T v_j
-// (where the state decays behind a frame: lambda^i and lambda^(C-j)).  Only non-negative powers occur, so no decay overflows.
+// (where the state decays behind a frame: lambda^i and lambda^(C-j)).  Only non-negative powers occur, so no decay overflows; memories that grow: see `grows`.
 //
 // A workgroup has a tile of DV columns of a head's state, in registers in 32 bits, and walks a stretch of frames; a wavefront has 16 of the columns and makes
 // the results of all C frames in them.  q, k, v of the next chunk are fetched into registers while this one is multiplied.  Products are
@@ -283,20 +283,31 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     const int col = c0 + wave * 16 + lr;  // of the state, this lane's
 
     // the state: block i, register r: row 16 i + 4 g + r
+    // (an offset behind the buffer's end reads a zero: with a branch for each the loads may be waited for one by one, 273 us for 187)
     v4f state[SB];
     const int64_t row_step = w.turned ? 1 : w.dv, corner = (w.turned ? (int64_t)col * w.keys : col) + w.first_key * row_step;
     const float* from = nullptr;
     if (!STATES) from = stretch == 0 ? (w.s_in ? w.s_in + pair * area : nullptr) : st.states + ((int64_t)(stretch - 1) * w.n * w.h + pair) * area;
+    {
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, from && have >= 0 ? (int)area * 4 : 0, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < SB; ++i)
+        for (int i = 0; i < SB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = 16 * i + 4 * g + r;
-            state[i][r] = from && have >= 0 && row < w.dk && col < w.dv ? from[corner + row * row_step] : 0.0f;
-        }
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * i + 4 * g + r;
+                const unsigned at = row < w.dk && col < w.dv ? (unsigned)(corner + row * row_step) * 4 : NOWHERE;
+                state[i][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
+            }
+    }
 
     const float decay = log2_of(w.t > 0 ? w.log_decay[head] : 0.0f);
     const int late = w.back ? 0 : 1;
+    // A memory that grows so fast that powers over a chunk (a stretch, where there are several) pass 2^64: they may soon be infinities, which times the zeros of
+    // absent frames are none of the results.  Such a head takes no chunks, it goes frame by frame below, all of a video in the first stretch's workgroup (128 x 128:
+    // 3.9 us a frame).
+    auto grows = [&](float decay) { return decay * (float)(st.count > 1 ? st.frames : C) > 64.0f; };
+    if (STATES && grows(decay)) return;
+    const int chunked = grows(decay) ? 0 : have;
 
     // This thread's 16 bytes of every RK-th row of q and k (of every RV-th of v): rows row + i RK, columns c on.  The last piece of a row that no whole
     // pieces make up begins early.  (frames lie at most 2^22 elements apart: offsets within a chunk have 32 bits)
@@ -321,7 +332,7 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     // (an offset behind a buffer's end reads zeros: no branches, and loads stay on their way)
     auto fetch_rows = [&](u32x4* held, auto count, auto rows, const T* p, int64_t frame, const Part& part, int f) __attribute__((always_inline)) {
         constexpr int N = decltype(count)::value, R = decltype(rows)::value;
-        const int none = have - f < C ? C - (have - f) : 0;
+        const int none = chunked - f < C ? C - (chunked - f) : 0;
         const int64_t lowest = w.back ? (int64_t)(end - 1 - f0 - f) + none - (N * R - 1) : (int64_t)f0 + f - none;
         const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + lowest * frame), 0, 0x7fffffff, 0x00027000);
 #pragma unroll
@@ -387,14 +398,14 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
     for (int s = 0; s < STEPS; ++s)
         steps[s] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(power(C - 32 - 32 * s, decay))));
 
-    if (have > 0) fetch(0);
-    for (int f = 0; f < have; f += C) {
+    if (chunked > 0) fetch(0);
+    for (int f = 0; f < chunked; f += C) {
         // a chunk of fewer frames has them in its last rows, zeros before: every power but two stays as it is
-        const int none = have - f < C ? C - (have - f) : 0;
+        const int none = chunked - f < C ? C - (chunked - f) : 0;
         const float carry = power(C - none, decay);
         if (f > 0) meet();
         put();
-        if (f + C < have) fetch(f + C);
+        if (f + C < chunked) fetch(f + C);
         meet();
         v4f out[STATES ? 1 : IB];
         if constexpr (!STATES) {
@@ -508,10 +519,14 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
         }
     }
 
+    float again = decay;
+    asm volatile("" : "+v"(again));  // (or what follows from it is held over the walk)
+    const bool growing = !STATES && grows(again);
     float* keep = nullptr;
     if (STATES) keep = st.states + ((int64_t)stretch * w.n * w.h + pair) * area;
-    else if (w.s_out && stretch == last) keep = const_cast<float*>(w.s_out) + pair * area;
-    if (keep && col < w.dv) {
+    else if (w.s_out && stretch == (growing ? 0 : last)) keep = const_cast<float*>(w.s_out) + pair * area;
+    auto leave_state = [&]() __attribute__((always_inline)) {
+        if (!keep || col >= w.dv) return;
         int g4 = 4 * g;
         asm("" : "+v"(g4));  // (or the places of all values are held from where the state was read)
 #pragma unroll
@@ -521,14 +536,17 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
                 const int row = 16 * i + g4 + r;
                 if (row < w.dk) keep[corner + row * row_step] = state[i][r];
             }
-    }
+    };
+    if (!growing) leave_state();
     if constexpr (!STATES) {
         // Masked places are zeros among a chunk's scores, and 0 times a v that is not finite has reached the chunk's frames before it.  Such a v stays in the state:
-        // where the state has ended so, the frames before the first of them are made again, as the recurrence stands, by this wavefront for its columns.
+        // where the state has ended so, the frames before the first of them are made again, as the recurrence stands, by this wavefront for its columns (128 x 128: 0.9
+        // us a frame of one head alone, 4.5 where the card is full).  All frames of a memory that grows fast are made so.
         const bool ended = col < w.dv && 4 * g < w.dk && !finite(state[0][0]);
-        if (w.o.p && __any(ended)) {
+        const int frames = growing ? (stretch == 0 ? end : 0) : have;
+        if (growing || (w.o.p && __any(ended))) {
             __threadfence();  // (behind the results as they are)
-            const float lambda = power(1, decay);
+            const float lambda = expf(w.log_decay[head]);
             int g4 = 4 * g;
             asm volatile("" : "+v"(g4));  // (or conditions of rows are held from here on)
 #pragma unroll
@@ -538,7 +556,7 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
                     const int row = 16 * i + g4 + r;
                     state[i][r] = from && row < w.dk && col < w.dv ? from[corner + row * row_step] : 0.0f;
                 }
-            for (int f = 0; f < have && __any(ended && finite(state[0][0])); ++f) {
+            for (int f = 0; f < frames && (growing || __any(ended && finite(state[0][0]))); ++f) {
                 const int64_t at = w.back ? end - 1 - f0 - f : f0 + f;
                 const float vf = col < w.dv ? w.taken * load_elem(v + at * w.v.frame + col) : 0.0f;
                 float sum = 0.0f;
@@ -557,13 +575,14 @@ void walk_kernel(Walk w, Stretches st, unsigned units, unsigned first) {
                 }
                 sum += __shfl_xor(sum, 16);
                 sum = w.given * (sum + __shfl_xor(sum, 32));
-                if (g == 0 && col < w.dv) {
+                if (g == 0 && col < w.dv && w.o.p) {
                     float* const part = w.part + ((video * (int64_t)w.t + at) * w.h + head) * w.dv + col;
                     if (w.adds) sum += *part;
                     if (w.leaves) *part = sum;
                     else store_elem(o + at * w.o.frame + wave * 16 + lr, sum);
                 }
             }
+            if (growing) leave_state();
         }
     }
     if (!STATES && w.o.p && !w.leaves) {  // behind a video's end

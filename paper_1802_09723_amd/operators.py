@@ -444,8 +444,9 @@ def _heads(t, what: str):
 def decay_attention(q, k, v, log_decay, scale=None, s0=None, lengths=None, out=None, s_last=None, stream=None):
     """``rrm_decay_attention``: (o, s_last) of linear attention over the frames, ``q`` and ``k`` [n, t, h, dk], ``v`` [n, t, h, dv] float32 or
     bfloat16 (dk and dv up to 256), with the decay exp(``log_decay``) a frame of each head (float32 [h]), from the state ``s0`` (float32 [n, h, dk, dv]; None:
-    zeros).  ``scale``: of the scores, None: dk ** -0.5.  ``lengths`` int32 [n]: frames of each video.  For one frame (t = 1) ``s_last`` may be
-    ``s0``.  Heads that share queries, keys or values take them expanded (a stride of 0)."""
+    zeros).  ``log_decay`` is meant to be at most 0; memories that grow fast are right, but slow (``include/rrm.h``).  ``scale``: of the scores,
+    None: dk ** -0.5.  ``lengths`` int32 [n]: frames of each video.  For one frame (t = 1) ``s_last`` may be ``s0``.  Heads that share queries, keys or
+    values take them expanded (a stride of 0)."""
     if stream is not None:
         return _elsewhere(stream, decay_attention, q, k, v, log_decay, scale, s0, lengths, out, s_last)
     if q.dim() != 4 or v.dim() != 4:

@@ -9,7 +9,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_block_operators import Device, without_a_device  # noqa: F401
+from test_block_operators import (Device, attend64, attend_slack, attention_case, check, run_attention, without_a_device)  # noqa: F401
 
 gpu = pytest.mark.gpu
 F64 = torch.float64
@@ -145,3 +145,54 @@ def test_calls_of_nothing_are_taken_whatever_their_axes(shape, without_a_device)
 @pytest.mark.parametrize("shape", NOTHING)
 def test_calls_of_nothing(shape):
     run_on_nothing(shape, lambda *s: torch.ones(s, device="cuda"), True)
+
+
+# -- memories that grow --------------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("growth,t", [(0.05, 150), (0.4, 150), (0.69, 80), (0.7, 80), (1.45, 40), (1.5, 3), (3.0, 3), (3.0, 20), (20.0, 3)])
+@pytest.mark.parametrize("dk,dv", [(64, 48), (100, 130), (200, 33)])
+def test_attention_of_a_memory_that_grows(dk, dv, growth, t, kind):
+    """A decay above 1 beside one below: as far as the recurrence fits 32 bits so do the results, whatever the powers in places that nothing stands in."""
+    data, lengths = attention_case(3, t, 2, dk, dv, kind, True, 21)
+    run_attention(data, lengths, torch.tensor([growth, -0.2]), 0.1, kind)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("growth", [0.005, 0.02, 0.2, 0.6])
+@pytest.mark.parametrize("d", [64, 200])
+def test_attention_of_a_long_memory_that_grows(d, growth, kind):
+    """A time axis in stretches whose keys and queries are zeros but for those of the last frames (of the first ones, for the gradients of the frames before):
+    the powers over the zeros pass 32 bits, what the memory holds does not."""
+    n, t, h, some = 2, 4300, 1, 90
+    data, _ = attention_case(n, some, h, d, d, kind, False, 22)
+    ld, scale, ends = torch.tensor([growth]), 0.1, [some] * n
+    d64 = {k: a.double() for k, a in data.items()}
+    none = torch.zeros(n, h, d, d, dtype=F64)
+    padded = {k: torch.zeros(n, t, h, d, dtype=a.dtype) for k, a in data.items() if k in ("q", "k", "v", "do")}
+    for k, a in padded.items():
+        a[:, t - some:] = data[k]
+    dev = {k: a.cuda() for k, a in padded.items()}
+    o, s_last = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld.cuda(), scale)
+    want, last = attend64(d64["q"], d64["k"], d64["v"], ld, scale, none, ends)
+    so, ss = attend_slack(d64["q"], d64["k"], d64["v"], ld, scale, none, ends, False, kind)
+    assert not o[:, :t - some].any()
+    check(o[:, t - some:], want, so, "o")
+    check(s_last, last, ss, "s_last")
+    # backwards the memory begins with the last frame: a video that holds all it has in its first ones
+    for k, a in padded.items():
+        a.zero_()
+        a[:, :some] = data[k]
+    dev = {k: a.cuda() for k, a in padded.items()}
+    dq, dk, dv, ds0 = rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld.cuda(), scale)
+    leaves = [d64[k].clone().requires_grad_() for k in ("q", "k", "v")] + [none.clone().requires_grad_()]
+    o, _ = attend64(leaves[0], leaves[1], leaves[2], ld, scale, leaves[3], ends)
+    wants = torch.autograd.grad(o, leaves, d64["do"])
+    sk, _ = attend_slack(d64["v"], d64["do"], scale * d64["q"], ld, 1.0, none, ends, True, kind)
+    sv, s0s = attend_slack(d64["k"], scale * d64["q"], d64["do"], ld, 1.0, none, ends, True, kind)
+    assert not dk[:, some:].any() and not dv[:, some:].any()
+    check(dk[:, :some], wants[1], sk, "dk")
+    check(dv[:, :some], wants[2], sv, "dv")
+    check(ds0, wants[3], s0s, "ds0")
