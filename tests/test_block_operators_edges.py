@@ -9,7 +9,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_block_operators import (Device, attend64, attend_slack, attention_case, check, run_attention, without_a_device)  # noqa: F401
+from test_block_operators import (DT, FAST, ORTH, SURE, V, W, Device, attend64, attend_slack, attention_case, check, gen, run_attention, without_a_device)  # noqa: F401
 
 gpu = pytest.mark.gpu
 F64 = torch.float64
@@ -196,3 +196,84 @@ def test_attention_of_a_long_memory_that_grows(d, growth, kind):
     check(dk[:, :some], wants[1], sk, "dk")
     check(dv[:, :some], wants[2], sv, "dv")
     check(ds0, wants[3], s0s, "ds0")
+
+
+# -- orthogonal updates of several steps ---------------------------------------------------------------------------------------
+
+def iterate(g, steps, co, eps, rounded=lambda x: x):
+    """The iteration in 64 bits; `rounded`: what X (at 256 times its size) as a product's operand, A and b A + c A^2 are passed through, a X being made of
+    the whole X"""
+    x = g.double() / (torch.linalg.norm(g.double()) + eps)
+    if x.shape[0] > x.shape[1]:
+        return iterate(g.t(), steps, co, eps, rounded).t()
+    a, b, c = co
+    for _ in range(steps):
+        h = rounded(256 * x) / 256
+        gram = rounded(h @ h.t())
+        x = a * x + rounded(b * gram + c * gram @ gram) @ h
+    return x
+
+
+def through(dtype):
+    return lambda x: x.to(dtype).double()
+
+
+def held_to(got, g, steps, co, eps):
+    """`got` against the iteration in 64 bits, in the Frobenius norm.  What the result may be off by is taken from the roundings themselves, made one for one on the
+    CPU: X, A and b A + c A^2 to half precision, the result to bfloat16.  Sums in another order turn some of these roundings the other way; where there are many, the
+    norm of what they come to stays, and where there are few, most of them are the very same.  Twice is allowed, and half a rounding of the result.  That is less than a
+    fiftieth of the result, and after five fast steps less than an iteration in bfloat16 is off by (fewer steps raise what is off less; at 1 a step forgets it)."""
+    want = iterate(g, steps, co, eps)
+    size = float(torch.linalg.norm(want))
+    off = [float(torch.linalg.norm(through(torch.bfloat16)(iterate(g, steps, co, eps, through(t))) - want)) for t in (torch.float16, torch.bfloat16)]
+    limit = 2 * off[0] + 2.0 ** -9 * size
+    assert limit < 0.02 * size and (min(g.shape) < 16 or steps < 5 or co != FAST or limit < 0.7 * off[1]), "a limit that says nothing"
+    err = float(torch.linalg.norm(got.double().cpu() - want))
+    assert err <= limit, f"{err / size} of the result off, {limit / size} allowed"
+
+
+LAUNCHES = [(257, 300), (300, 257), (130, 700), (700, 130), (48, 1500), (1500, 48), (131, 2053), (2053, 131), (100, 4100)]
+
+
+def update(shape, kind, seed):
+    return (1e-3 * torch.randn(2, *shape, generator=gen(seed)) * torch.exp(0.5 * torch.randn(2, shape[0], 1, generator=gen(1)))).to(DT[kind])
+
+
+@pytest.mark.parametrize("shape", [(16, 16), (130, 33), (257, 300), (48, 1500)])
+def test_the_limits_of_orthogonal_updates_say_something(shape):
+    for g in update(shape, "f32", 5):
+        held_to(iterate(g, 5, FAST, 1e-7).bfloat16(), g, 5, FAST, 1e-7)
+        for wrong in (torch.zeros(shape), iterate(g, 5, FAST, 1e-7, through(torch.bfloat16)), iterate(g, 4, FAST, 1e-7), iterate(g, 5, SURE, 1e-7)):
+            with pytest.raises(AssertionError, match="off"):
+                held_to(wrong, g, 5, FAST, 1e-7)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", sorted({*ORTH, *LAUNCHES}))
+def test_orthogonalize_of_several_steps(shape, kind):
+    g = update(shape, kind, sum(shape) + 1)
+    for steps in (3, 5, 6):
+        got = rrm.orthogonalize(g.cuda(), steps)
+        for i in range(2):
+            held_to(got[i], g[i], steps, FAST, 1e-7)
+
+
+@gpu
+@pytest.mark.parametrize("shape", LAUNCHES)
+def test_orthogonalize_converges_in_launches(shape):
+    """Fourteen steps of the polynomial that keeps 1 where it is, beyond the sizes of one launch"""
+    u, _, vh = torch.linalg.svd(torch.randn(*shape, generator=gen(2), dtype=F64), full_matrices=False)
+    g = ((u * torch.linspace(0.5, 1.5, min(shape), dtype=F64)) @ vh).float()
+    got = rrm.orthogonalize(g.cuda(), 14, SURE)
+    held_to(got, g, 14, SURE, 1e-7)
+    polar = u @ vh
+    assert float(torch.linalg.norm(got.double().cpu() - polar)) <= (4 * W * sum(map(abs, SURE)) + W + V) * math.sqrt(min(shape)) * 1.1  # (the last step's roundings: the slope at 1 is 0)
+
+
+@gpu
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e20])
+@pytest.mark.parametrize("shape", [(48, 80), (257, 300), (60, 900), (900, 60)])
+def test_orthogonalize_has_no_scale_in_any_form(shape, size):
+    g = (torch.randn(shape, generator=gen(3)).double() * size).float()
+    held_to(rrm.orthogonalize(g.cuda(), eps=0.0), g, 5, FAST, 0.0)
