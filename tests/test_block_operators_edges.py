@@ -9,7 +9,7 @@ import torch
 
 import paper_1802_09723_amd as rrm
 from paper_1802_09723_amd import operators as ops
-from test_block_operators import (DT, FAST, ORTH, SURE, V, W, Device, attend64, attend_slack, attention_case, check, gen, run_attention, without_a_device)  # noqa: F401
+from test_block_operators import (DT, FAST, ORTH, SURE, U, V, W, Device, attend64, attend_slack, attention_case, check, gen, run_attention, without_a_device)  # noqa: F401
 
 gpu = pytest.mark.gpu
 F64 = torch.float64
@@ -198,19 +198,55 @@ def test_attention_of_a_long_memory_that_grows(d, growth, kind):
     check(ds0, wants[3], s0s, "ds0")
 
 
+# -- values that are not finite, late in a long video --------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [16, 72])
+def test_attention_of_an_infinity_late_in_a_long_video(d, kind):
+    """Heads enough that a workgroup walks a whole video: an infinity near the end of its walk leaves the many chunks before it as they were, within their
+    roundings, and other heads to the bit; backwards, one near the beginning."""
+    n, t, h, scale = 1, 1500, 260, 0.2
+    data, _ = attention_case(n, t, h, d, d, kind, False, 31)
+    ld = torch.linspace(-0.3, -0.01, h)
+    dev = {k: a.cuda() for k, a in data.items()}
+    d64 = {k: a.double() for k, a in dev.items()}
+    clean = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"])
+    clean += rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"], ds_last=dev["ds_last"])
+    late, early = t - 37, 29
+    dev["v"][0, late, h - 1, 3] = math.inf
+    dev["do"][0, early, 0, 5] = -math.inf
+    got = rrm.decay_attention(dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"])
+    got += rrm.decay_attention_backward(dev["do"], dev["q"], dev["k"], dev["v"], ld.cuda(), scale, s0=dev["s0"], ds_last=dev["ds_last"])
+    ldd, turned = ld.cuda(), d64["ds_last"].transpose(-1, -2)
+    so, _ = attend_slack(d64["q"], d64["k"], d64["v"], ldd, scale, d64["s0"], [t], False, kind)
+    sk, _ = attend_slack(d64["v"], d64["do"], scale * d64["q"], ldd, 1.0, turned, [t], True, kind)
+    sv, _ = attend_slack(d64["k"], scale * d64["q"], d64["do"], ldd, 1.0, d64["ds_last"], [t], True, kind)
+    for what, at, head, side, slack in (("o", 0, h - 1, slice(0, late), so), ("dk", 3, 0, slice(early + 1, t), sk), ("dv", 4, 0, slice(early + 1, t), sv)):
+        a, b = got[at], clean[at].double()
+        rest = [j for j in range(h) if j != head and not (what != "o" and j == h - 1)]
+        assert torch.equal(a[:, :, rest], clean[at][:, :, rest]), what
+        # (each is off by so much, and by its rounding)
+        e = slack[:, side, head]
+        check(a[:, side, head], b[:, side, head], 2 * e + (V if kind == "bf16" else U) * (b[:, side, head].abs() + e), what)
+    assert not torch.isfinite(got[0][0, late:, h - 1, 3]).any() and torch.isfinite(got[0][0, :, h - 1, :3]).all()
+    assert not torch.isfinite(got[4][0, :early + 1, 0, 5]).any() and torch.isfinite(got[4][0, :, 0, :5]).all()
+    assert not torch.isfinite(got[3][0, early, 0]).any()
+
+
 # -- orthogonal updates of several steps ---------------------------------------------------------------------------------------
 
-def iterate(g, steps, co, eps, rounded=lambda x: x):
+def iterate(g, steps, co, eps, rounded=lambda x: x, whole=True):
     """The iteration in 64 bits; `rounded`: what X (at 256 times its size) as a product's operand, A and b A + c A^2 are passed through, a X being made of
-    the whole X"""
+    the whole X (or of the rounded one)"""
     x = g.double() / (torch.linalg.norm(g.double()) + eps)
     if x.shape[0] > x.shape[1]:
-        return iterate(g.t(), steps, co, eps, rounded).t()
+        return iterate(g.t(), steps, co, eps, rounded, whole).t()
     a, b, c = co
     for _ in range(steps):
         h = rounded(256 * x) / 256
         gram = rounded(h @ h.t())
-        x = a * x + rounded(b * gram + c * gram @ gram) @ h
+        x = a * (x if whole else h) + rounded(b * gram + c * gram @ gram) @ h
     return x
 
 
@@ -277,3 +313,16 @@ def test_orthogonalize_converges_in_launches(shape):
 def test_orthogonalize_has_no_scale_in_any_form(shape, size):
     g = (torch.randn(shape, generator=gen(3)).double() * size).float()
     held_to(rrm.orthogonalize(g.cuda(), eps=0.0), g, 5, FAST, 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(128, 512), (256, 256), (512, 264), (100, 1400)])
+def test_orthogonalize_carries_the_whole_x(shape):
+    """Where a few directions stand far above the others, what a step rounds off X, if it stayed off, would be raised by every step behind it: a X is made of X in
+    two parts.  Tens of thousands of roundings are nearly independent here, and the norm of what they come to hardly varies (by 2% at most, for the same matrix changed by
+    1e-4 of itself, eight times on the CPU): a tenth is allowed."""
+    g = torch.randn(shape, generator=gen(6)) + 2 * torch.randn(shape[0], 8, generator=gen(7)) @ torch.randn(8, shape[1], generator=gen(8))
+    want, got = iterate(g, 5, FAST, 1e-7), rrm.orthogonalize(g.cuda()).double().cpu()
+    two, one = (float(torch.linalg.norm(through(torch.bfloat16)(iterate(g, 5, FAST, 1e-7, through(torch.float16), whole)) - want)) for whole in (True, False))
+    assert 1.1 * two < 0.98 * one, "a limit that says nothing"
+    assert float(torch.linalg.norm(got - want)) <= 1.1 * two
